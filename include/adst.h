@@ -84,7 +84,8 @@ typedef enum {
   ADST_VARDIFF2D9 = 2,
   ADST_GAUSSSEIDEL2D5 = 3
 } adst_kind;
-typedef enum { ADST_F64 = 0, ADST_F32 = 1 } adst_dtype;
+/* BF16 and F16: the sequence operators only (the stencil kinds take F64 and F32). */
+typedef enum { ADST_F64 = 0, ADST_F32 = 1, ADST_BF16 = 2, ADST_F16 = 3 } adst_dtype;
 
 /* Checkpoint schedules (Sec. IV: store-all default, a manual choice, or an
  * automatic one within the memory limit).
@@ -460,6 +461,176 @@ adst_status adst_trace_kernels(adst_kernel_stat* out, int32_t cap, int32_t* n_ou
  * Errors: ADST_ERR_ARG (NULL pointer with bytes > 0, misaligned pointer or
  * size, overlapping ranges), ADST_ERR_HIP. */
 adst_status adst_copy(void* dst, const void* src, uint64_t bytes, hipStream_t stream);
+
+/* ---- Sequence operators ------------------------------------------------
+ * The time loop of a sequence layer with its vector-Jacobian product, the
+ * normalisation around it, and the optimizer step that consumes gradients
+ * (these operators' and adst_vjp's). The conventions at the top of this file
+ * hold: the caller owns all device memory, calls only enqueue on the stream,
+ * argument errors are found before anything is enqueued, outputs are
+ * overwritten (AdamW's parameters and states, and the recurrence step's state
+ * pool, are updated in place). Every result is the same bit for bit from call
+ * to call: no sum's order depends on timing.
+ *
+ * Element types: F64, F32, BF16, F16. Sums, states, statistics and all
+ * arithmetic between loads and stores are in 32 bits ("accumulation type"
+ * below), in 64 for F64; a 16-bit result is rounded once, to nearest even.
+ * Arrays need the alignment of one element. */
+
+/* Gated linear recurrence, per batch row b and channel d, t = 1..steps:
+ *   ADST_GATE_COEFF    h_t = a_t * h_{t-1} + u_t
+ *   ADST_GATE_SIGMOID  h_t = s_t * h_{t-1} + (1 - s_t) * u_t,  s_t = 1 / (1 + exp(-a_t))
+ * (1 - s_t is evaluated as 1 / (1 + exp(a_t)).) The time axis is cut into
+ * spans whose maps h -> A*h + H are joined, so the products of up to `steps`
+ * consecutive coefficients have to stay in the accumulation type's range,
+ * which |a_t| <= 1 ensures. */
+typedef enum { ADST_GATE_COEFF = 0, ADST_GATE_SIGMOID = 1 } adst_gate;
+
+typedef struct {
+  int32_t dtype;      /* adst_dtype of a, u, h, dh, da, du */
+  int32_t gate;       /* adst_gate */
+  int64_t batch;      /* >= 0 */
+  int64_t steps;      /* >= 0 */
+  int64_t channels;   /* >= 0 */
+  int64_t stride_a[2];  /* elements between batch rows and between steps of the input a; */
+  int64_t stride_u[2];  /* of u, */
+  int64_t stride_dh[2]; /* and of dh. Channels are contiguous; any strides >= 0, 0 repeats */
+} adst_recurrence_problem;
+
+typedef struct {
+  int64_t span;              /* steps between checkpoints */
+  uint64_t ck_bytes;         /* checkpoints: the state at the start of each span */
+  uint64_t workspace_bytes;  /* ws of adst_recurrence_forward, and of _vjp given checkpoints */
+  uint64_t vjp_workspace_bytes; /* ws of adst_recurrence_vjp without checkpoints (ck = NULL) */
+} adst_recurrence_info;
+
+/* Sizes of a problem's buffers (host only). Errors: ADST_ERR_ARG (NULL,
+ * unknown dtype or gate, a negative extent or stride), ADST_ERR_UNSUPPORTED
+ * (steps >= 2^31 - 2^16, or more spans than a launch holds). */
+adst_status adst_recurrence_plan(const adst_recurrence_problem* prob, adst_recurrence_info* out);
+
+/* h [batch][steps][channels] (contiguous, optional), and the last state hT
+ * [batch][channels] (optional). h0 (optional, zero if NULL), hT and ck are in
+ * the accumulation type. lens (optional, device int32 [batch]): row b runs
+ * lens[b] steps (clamped to [0, steps]); its a and u beyond are not read, its
+ * h beyond is 0 and hT is the state after lens[b] steps (h0 for none). ck
+ * (optional, ck_bytes) receives the checkpoints that adst_recurrence_vjp
+ * recomputes the states from: the states themselves need not be kept.
+ * Errors: as adst_recurrence_plan; ADST_ERR_ARG for a missing a or u or for
+ * overlapping ranges, ADST_ERR_WORKSPACE, ADST_ERR_HIP. */
+adst_status adst_recurrence_forward(const adst_recurrence_problem* prob, const void* a,
+                                    const void* u, const void* h0, const int32_t* lens, void* h,
+                                    void* hT, void* ck, void* ws, uint64_t ws_bytes,
+                                    hipStream_t stream);
+
+/* The vector-Jacobian product. dh: dL/dh [batch][steps][channels]; dhT
+ * (optional): dL/dhT, in the accumulation type. With G_t = dL/dh_t in full
+ * (G_t = dh_t + c_{t+1} G_{t+1}, c the coefficient):
+ *   COEFF    da_t = G_t h_{t-1},  du_t = G_t
+ *   SIGMOID  da_t = G_t (h_{t-1} - u_t) s_t (1 - s_t),  du_t = G_t (1 - s_t)
+ *   dh0 = c_1 G_1 (dhT of a row without steps)
+ * da and du [batch][steps][channels] (contiguous), zero beyond lens[b], where
+ * dh is not read; dh0 (optional) in the accumulation type. An input that
+ * repeats (stride 0) gets the gradients of its uses, one for each. ck: the
+ * checkpoints of adst_recurrence_forward with the same problem, inputs and
+ * lens, or NULL: they are then recomputed into ws (vjp_workspace_bytes).
+ * Errors: as adst_recurrence_forward. */
+adst_status adst_recurrence_vjp(const adst_recurrence_problem* prob, const void* a, const void* u,
+                                const void* h0, const int32_t* lens, const void* ck,
+                                const void* dh, const void* dhT, void* da, void* du, void* dh0,
+                                void* ws, uint64_t ws_bytes, hipStream_t stream);
+
+/* One step of each batch row (prob->steps must be 1) on a pool of states
+ * [nstates][channels] in the accumulation type, updated in place; h
+ * [batch][channels] (optional) receives the new states rounded to the dtype.
+ * slots (optional, device int32 [batch]): row b's state is row slots[b] of the
+ * pool (row b if NULL, and then nstates >= batch). A slot outside
+ * [0, nstates) is an idle row: no state changes and its h is 0. No two rows
+ * may have the same slot. Errors: as adst_recurrence_forward, without
+ * ADST_ERR_WORKSPACE. */
+adst_status adst_recurrence_step(const adst_recurrence_problem* prob, const void* a, const void* u,
+                                 const int32_t* slots, void* state, int64_t nstates, void* h,
+                                 hipStream_t stream);
+
+/* Layer norm over the last axis of x [rows][n]:
+ *   y = (x - mean) * rstd * w + b,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ * w and b (each optional: 1 and 0) are of weight_dtype: the dtype itself, or
+ * F32 beside BF16 and F16. mean and rstd [rows] (optional), accumulation type. */
+typedef struct {
+  int32_t dtype;        /* of x, y, dy, dx */
+  int32_t weight_dtype; /* of w, b, dw, db */
+  int64_t rows;         /* >= 0 */
+  int64_t n;            /* >= 1 */
+  int64_t stride_x;     /* elements between rows of x (>= 0) */
+  int64_t stride_dy;    /* and of dy; y and dx are contiguous */
+  double eps;           /* >= 0, finite */
+} adst_norm_problem;
+
+/* Errors: ADST_ERR_ARG (NULL problem, x or y, bad types, extents, strides or
+ * eps, overlapping ranges; y may be x itself where their layouts agree),
+ * ADST_ERR_UNSUPPORTED (n or rows >= 2^31 - 2^16), ADST_ERR_HIP. */
+adst_status adst_layer_norm_forward(const adst_norm_problem* prob, const void* x, const void* w,
+                                    const void* b, void* y, void* mean, void* rstd,
+                                    hipStream_t stream);
+
+/* With xhat = (x - mean) * rstd and e = dy * w:
+ *   dx = (e - mean_n(e) - xhat * mean_n(e * xhat)) * rstd,
+ *   dw = sum over rows of dy * xhat,  db = sum over rows of dy.
+ * mean and rstd are the forward call's. dx, dw and db are each optional. ws:
+ * adst_layer_norm_workspace_bytes (0 where neither dw nor db is asked for).
+ * The rows are summed in an order that depends on the sizes alone.
+ * Errors: as adst_layer_norm_forward, plus ADST_ERR_WORKSPACE. */
+uint64_t adst_layer_norm_workspace_bytes(const adst_norm_problem* prob);
+adst_status adst_layer_norm_vjp(const adst_norm_problem* prob, const void* x, const void* dy,
+                                const void* w, const void* mean, const void* rstd, void* dx,
+                                void* dw, void* db, void* ws, uint64_t ws_bytes,
+                                hipStream_t stream);
+
+/* One AdamW step over many tensors, in place, t = 1, 2, ...:
+ *   g = grad_scale * grad
+ *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * (g * g)
+ *   p = p * (1 - lr * weight_decay)
+ *       - (lr / (1 - beta1^t)) * (m / (sqrt(v) / sqrt(1 - beta2^t) + eps))
+ * evaluated in the order written, without fused multiply-add. Parameters are
+ * F32 (F64); gradients F32, BF16 or F16 (F64 with F64), one type per call.
+ * States are in the parameters' type (bits = 32) or, with F32 parameters,
+ * coded in 8 bits (bits = 8): of each tensor's blocks of ADST_STATE_BLOCK
+ * consecutive values (the last one shorter) the largest magnitude over 448 is
+ * the block's scale, and a value is held as value / scale rounded to e4m3 (4
+ * exponent and 3 mantissa bits, OCP). Of v its square root is held, positive
+ * values of which never round to zero. A block whose magnitudes are all below
+ * 2^-100 is held as zeros. Parameters are updated with the states before they
+ * are rounded to codes. A NaN or infinity in a gradient makes its block's
+ * states NaN (its element's, with bits = 32). */
+#define ADST_STATE_BLOCK 256
+typedef struct {
+  void* p;            /* n parameters */
+  const void* grad;   /* n gradients */
+  void* m;            /* n values or codes */
+  void* v;            /* n values or codes */
+  float* m_scale;     /* bits = 8: ceil(n / ADST_STATE_BLOCK) scales */
+  float* v_scale;
+  void* copy;         /* optional: the new parameters, rounded to copy_dtype (F64 to F32 first) */
+  int64_t n;          /* >= 0 */
+  double lr, weight_decay;
+} adst_adamw_tensor;
+
+typedef struct {
+  int32_t dtype;       /* of p: ADST_F32 or ADST_F64 */
+  int32_t grad_dtype;
+  int32_t copy_dtype;  /* ADST_BF16, ADST_F16 or ADST_F32; read where a tensor has a copy */
+  int32_t bits;        /* 32 or 8 (32: states in the parameters' type) */
+  int64_t t;           /* the step's number, from 1 */
+  double beta1, beta2, eps; /* betas in [0, 1), eps >= 0 */
+  const float* grad_scale; /* optional device scalar (1 if NULL), e.g. a clipping factor; where
+                              it is not finite nothing is updated */
+} adst_adamw_problem;
+
+/* tensors: host array, read before the call returns. Errors: ADST_ERR_ARG
+ * (NULL pointers, bad values or types, overlapping ranges within a tensor),
+ * ADST_ERR_UNSUPPORTED (a tensor of 2^40 values or more), ADST_ERR_HIP. */
+adst_status adst_adamw(const adst_adamw_problem* prob, const adst_adamw_tensor* tensors,
+                       int32_t n_tensors, hipStream_t stream);
 
 /* Static description of a status code. */
 const char* adst_status_str(adst_status status);

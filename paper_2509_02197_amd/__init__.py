@@ -18,7 +18,9 @@ LIB_PATH = os.path.join(_HERE, "libadst.so")
 # enums of adst.h
 ADST_OK, ADST_ERR_ARG, ADST_ERR_BUDGET, ADST_ERR_WORKSPACE, ADST_ERR_UNSUPPORTED, ADST_ERR_HIP = range(6)
 ADST_JACOBI2D5, ADST_ALLENCAHN3D7, ADST_VARDIFF2D9, ADST_GAUSSSEIDEL2D5 = 0, 1, 2, 3
-ADST_F64, ADST_F32 = 0, 1
+ADST_F64, ADST_F32, ADST_BF16, ADST_F16 = 0, 1, 2, 3
+ADST_GATE_COEFF, ADST_GATE_SIGMOID = 0, 1
+ADST_STATE_BLOCK = 256
 ADST_SCHED_AUTO, ADST_SCHED_STORE_ALL, ADST_SCHED_UNIFORM, ADST_SCHED_BINOMIAL = 0, 1, 2, 3
 ADST_LOSS_HALF_SQ, ADST_LOSS_DOT_W, ADST_LOSS_HALF_SQ_DIFF, ADST_LOSS_SEED = 0, 1, 2, 3
 ADST_FORCE_TAPE, ADST_TRACE, ADST_NO_FUSE, ADST_LIMIT = 0x1, 0x2, 0x4, 0x8
@@ -29,7 +31,9 @@ ADST_BUF_NONE, ADST_BUF_X0, ADST_BUF_W0, ADST_BUF_W1, ADST_BUF_XT, ADST_BUF_SLOT
 EXPORTED = ("adst_plan", "adst_plan_actions", "adst_forward", "adst_vjp", "adst_ilp_solve",
             "adst_trace_kernels", "adst_copy", "adst_vjp_static_ws", "adst_status_str",
             "adst_last_error", "adst_sweep_workspace_bytes", "adst_forward_scratch",
-            "adst_vjp_scratch")
+            "adst_vjp_scratch", "adst_recurrence_plan", "adst_recurrence_forward",
+            "adst_recurrence_vjp", "adst_recurrence_step", "adst_layer_norm_forward",
+            "adst_layer_norm_vjp", "adst_layer_norm_workspace_bytes", "adst_adamw")
 ADST_STATIC_WS_BYTES = 64 << 20
 PHASE_NAMES = ("forward sweep", "recomputation", "adjoint", "loss and seed", "constants")
 ILP_EVENTS = {"alloc": 0, "free": 1, "produce": 2, "drop": 3, "recompute": 4,
@@ -87,6 +91,39 @@ class adst_kernel_stat(ctypes.Structure):
                 ("ms_max", ctypes.c_double), ("alg_bytes_sum", ctypes.c_double)]
 
 
+class adst_recurrence_problem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("batch", ctypes.c_int64),
+                ("steps", ctypes.c_int64), ("channels", ctypes.c_int64),
+                ("stride_a_batch", ctypes.c_int64), ("stride_a_step", ctypes.c_int64),
+                ("stride_u_batch", ctypes.c_int64), ("stride_u_step", ctypes.c_int64),
+                ("stride_dh_batch", ctypes.c_int64), ("stride_dh_step", ctypes.c_int64)]
+
+
+class adst_recurrence_info(ctypes.Structure):
+    _fields_ = [("span", ctypes.c_int64), ("ck_bytes", ctypes.c_uint64),
+                ("workspace_bytes", ctypes.c_uint64), ("vjp_workspace_bytes", ctypes.c_uint64)]
+
+
+class adst_norm_problem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("stride_x", ctypes.c_int64),
+                ("stride_dy", ctypes.c_int64), ("eps", ctypes.c_double)]
+
+
+class adst_adamw_tensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("lr", ctypes.c_double), ("weight_decay", ctypes.c_double)]
+
+
+class adst_adamw_problem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("copy_dtype", ctypes.c_int32), ("bits", ctypes.c_int32), ("t", ctypes.c_int64),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("grad_scale", ctypes.c_void_p)]
+
+
 class AdstError(RuntimeError):
     def __init__(self, status, detail):
         self.status = status
@@ -128,6 +165,19 @@ def lib():
         getattr(L, f).restype = ctypes.c_int
     L.adst_sweep_workspace_bytes.argtypes = [P(adst_problem), i32]
     L.adst_sweep_workspace_bytes.restype = u64
+    L.adst_recurrence_plan.argtypes = [P(adst_recurrence_problem), P(adst_recurrence_info)]
+    L.adst_recurrence_forward.argtypes = [P(adst_recurrence_problem)] + [vp] * 8 + [u64, vp]
+    L.adst_recurrence_vjp.argtypes = [P(adst_recurrence_problem)] + [vp] * 11 + [u64, vp]
+    L.adst_recurrence_step.argtypes = [P(adst_recurrence_problem)] + [vp] * 4 + [i64, vp, vp]
+    L.adst_layer_norm_forward.argtypes = [P(adst_norm_problem)] + [vp] * 7
+    L.adst_layer_norm_vjp.argtypes = [P(adst_norm_problem)] + [vp] * 9 + [u64, vp]
+    L.adst_layer_norm_workspace_bytes.argtypes = [P(adst_norm_problem)]
+    L.adst_adamw.argtypes = [P(adst_adamw_problem), P(adst_adamw_tensor), i32, vp]
+    for f in ("adst_recurrence_plan", "adst_recurrence_forward", "adst_recurrence_vjp",
+              "adst_recurrence_step", "adst_layer_norm_forward", "adst_layer_norm_vjp",
+              "adst_adamw"):
+        getattr(L, f).restype = ctypes.c_int
+    L.adst_layer_norm_workspace_bytes.restype = u64
     L.adst_status_str.argtypes = [ctypes.c_int]
     L.adst_status_str.restype = ctypes.c_char_p
     L.adst_last_error.argtypes = []
@@ -424,3 +474,10 @@ def vjp(kind, x0, coeff=None, steps=1, loss=ADST_LOSS_HALF_SQ, aux=None, budget_
                     scratch_bytes=0 if scratch is None else scratch.nbytes)
     return {"dx0": dx0, "dK": dK, "xT": xT, "loss": L, "dparams": dp, "info": info, "ws": ws,
             "scratch_bytes": 0 if scratch is None else scratch.nbytes}
+
+
+from .sequence import (AdamW, adst_adamw, adst_layer_norm_forward,  # noqa: E402,F401
+                       adst_layer_norm_vjp, adst_layer_norm_workspace_bytes,
+                       adst_recurrence_forward, adst_recurrence_plan, adst_recurrence_step,
+                       adst_recurrence_vjp, layer_norm, layer_norm_vjp, recurrence,
+                       recurrence_step, recurrence_vjp)

@@ -18,10 +18,11 @@ LIB = os.path.join(HERE, "libadst.so")
 ARCH = "gfx950"
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
-HOST_SOURCES = ["planner.cpp", "ilp.cpp", "abi.cpp"]
+HOST_SOURCES = ["planner.cpp", "ilp.cpp", "abi.cpp", "seq_abi.cpp"]
 HIP_SOURCES = ["kernels.hip", "allencahn.hip", "jacobi_march.hip", "jacobi_march_lim.hip",
                "jacobi_march_store.hip", "jacobi_pair.hip", "gauss_seidel.hip", "gs_pipe.hip",
-               "vardiff_march.hip", "static_ws.hip"]
+               "vardiff_march.hip", "static_ws.hip", "recurrence.hip", "layer_norm.hip",
+               "adamw.hip"]
 
 COMMON = ["-std=c++17", "-O3", "-fPIC", "-ffp-contract=off", "-Wall",
           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

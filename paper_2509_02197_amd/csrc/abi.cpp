@@ -17,6 +17,7 @@
 #include <rocprofiler-sdk-roctx/roctx.h>
 
 #include "adst.h"
+#include "errors.h"
 #include "kernels.h"
 #include "ilp.h"
 #include "planner.h"
@@ -922,6 +923,21 @@ adst_status forward_impl(const adst_problem* prob, const void* x0, const void* c
 }
 
 }  // namespace
+
+adst_status report(adst_status st, const char* text) {
+  try {
+    g_last_error = text;
+  } catch (...) {  // no memory for the text: the status stands alone
+    g_last_error.clear();
+  }
+  return st;
+}
+
+adst_status report_ok() {
+  g_last_error.clear();
+  return ADST_OK;
+}
+
 }  // namespace adst
 
 using namespace adst;

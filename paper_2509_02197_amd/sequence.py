@@ -1,0 +1,447 @@
+"""The sequence operators of adst.h from Python: the gated linear recurrence
+with its VJP and its one-step form, layer norm with its VJP, and AdamW over
+many tensors.
+
+The ``adst_*`` functions keep the C names and only marshal arguments. The
+others take torch tensors, check them, allocate outputs and workspaces with
+torch and make the call. Errors in the arguments are ValueError or TypeError
+before anything is launched. A call runs on torch's current stream, or on
+`stream`; then its outputs and workspaces belong to that stream, and its
+inputs are recorded as used there.
+"""
+import ctypes
+
+from . import (ADST_BF16, ADST_F16, ADST_F32, ADST_F64, ADST_GATE_COEFF, ADST_GATE_SIGMOID,
+               ADST_STATE_BLOCK, _check, _ptr, _stream, adst_adamw_problem, adst_adamw_tensor,
+               adst_norm_problem, adst_recurrence_info, adst_recurrence_problem, lib)
+
+
+# ------------------------------------------------------------ the C calls
+def adst_recurrence_plan(prob):
+    info = adst_recurrence_info()
+    _check(lib().adst_recurrence_plan(ctypes.byref(prob), ctypes.byref(info)))
+    return info
+
+
+def adst_recurrence_forward(prob, a, u, h0, lens, h, hT, ck, ws, ws_bytes, stream=None):
+    _check(lib().adst_recurrence_forward(ctypes.byref(prob), _ptr(a), _ptr(u), _ptr(h0),
+                                         _ptr(lens), _ptr(h), _ptr(hT), _ptr(ck), _ptr(ws),
+                                         ws_bytes, _stream(stream)))
+
+
+def adst_recurrence_vjp(prob, a, u, h0, lens, ck, dh, dhT, da, du, dh0, ws, ws_bytes,
+                        stream=None):
+    _check(lib().adst_recurrence_vjp(ctypes.byref(prob), _ptr(a), _ptr(u), _ptr(h0), _ptr(lens),
+                                     _ptr(ck), _ptr(dh), _ptr(dhT), _ptr(da), _ptr(du),
+                                     _ptr(dh0), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def adst_recurrence_step(prob, a, u, slots, state, nstates, h, stream=None):
+    _check(lib().adst_recurrence_step(ctypes.byref(prob), _ptr(a), _ptr(u), _ptr(slots),
+                                      _ptr(state), nstates, _ptr(h), _stream(stream)))
+
+
+def adst_layer_norm_forward(prob, x, w, b, y, mean, rstd, stream=None):
+    _check(lib().adst_layer_norm_forward(ctypes.byref(prob), _ptr(x), _ptr(w), _ptr(b), _ptr(y),
+                                         _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def adst_layer_norm_workspace_bytes(prob):
+    return int(lib().adst_layer_norm_workspace_bytes(ctypes.byref(prob)))
+
+
+def adst_layer_norm_vjp(prob, x, dy, w, mean, rstd, dx, dw, db, ws, ws_bytes, stream=None):
+    _check(lib().adst_layer_norm_vjp(ctypes.byref(prob), _ptr(x), _ptr(dy), _ptr(w), _ptr(mean),
+                                     _ptr(rstd), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws),
+                                     ws_bytes, _stream(stream)))
+
+
+def adst_adamw(prob, tensors, n, stream=None):
+    """tensors: a ctypes array of adst_adamw_tensor."""
+    _check(lib().adst_adamw(ctypes.byref(prob), tensors, n, _stream(stream)))
+
+
+# ------------------------------------------------------------------ checks
+_CODES = None
+
+
+def _codes():
+    global _CODES
+    if _CODES is None:
+        import torch
+        _CODES = {torch.float64: ADST_F64, torch.float32: ADST_F32, torch.bfloat16: ADST_BF16,
+                  torch.float16: ADST_F16}
+    return _CODES
+
+
+def _code(name, t):
+    import torch
+    if not torch.is_tensor(t):
+        raise ValueError(f"{name} must be a torch tensor")
+    code = _codes().get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} has unsupported dtype {t.dtype}")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on a GPU, not {t.device}")
+    return code
+
+
+def _acc(code):
+    """The accumulation type: that of states, statistics and their gradients."""
+    import torch
+    return torch.float64 if code == ADST_F64 else torch.float32
+
+
+def _expect(name, t, shape, dtype, device, contiguous=True):
+    if t is None:
+        return
+    if not hasattr(t, "data_ptr"):
+        raise ValueError(f"{name} must be a torch tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, not {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _channels_contiguous(name, t):
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous (stride 1, not {t.stride(-1)})")
+
+
+def _call(device, stream, inputs, body):
+    """body(stream handle) on the tensors' device, allocations of body included."""
+    import torch
+    if stream is None and torch.cuda.current_device() == device.index:
+        return body(torch.cuda.current_stream(device).cuda_stream)
+    with torch.cuda.device(device):
+        if stream is None:
+            return body(torch.cuda.current_stream(device).cuda_stream)
+        handle = _stream(stream)
+        on = (torch.cuda.ExternalStream(handle, device=device) if handle
+              else torch.cuda.default_stream(device))
+        with torch.cuda.stream(on):
+            for t in inputs:
+                if t is not None:
+                    t.record_stream(on)
+            return body(handle)
+
+
+def _bytes(n, device):
+    import torch
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+# -------------------------------------------------------------- recurrence
+def _recurrence_problem(a, u, gate, dh=None):
+    code = _code("a", a)
+    if a.dim() != 3:
+        raise ValueError(f"a must be [batch, steps, channels], not {tuple(a.shape)}")
+    _expect("u", u, a.shape, a.dtype, a.device, contiguous=False)
+    _channels_contiguous("a", a)
+    _channels_contiguous("u", u)
+    B, T, D = a.shape
+    sd = (0, 0)
+    if dh is not None:
+        _expect("dh", dh, a.shape, a.dtype, a.device, contiguous=False)
+        _channels_contiguous("dh", dh)
+        sd = (dh.stride(0), dh.stride(1))
+    return adst_recurrence_problem(code, gate, B, T, D, a.stride(0), a.stride(1), u.stride(0),
+                                   u.stride(1), *sd)
+
+
+def _check_lens(lens, a):
+    import torch
+    _expect("lens", lens, (a.shape[0],), torch.int32, a.device)
+
+
+def recurrence(a, u, h0=None, lens=None, gate=ADST_GATE_COEFF, want_h=True, want_ck=False,
+               stream=None):
+    """h_t = c_t * h_{t-1} + d_t over axis 1 of a, u [batch, steps, channels], with
+    (c, d) = (a, u), or (s, (1 - s) * u), s = sigmoid(a), for ADST_GATE_SIGMOID.
+
+    h0 [batch, channels] (zeros if None), in float32 (float64 for float64 inputs); lens
+    [batch] int32: the steps of each row. a and u may have any strides with contiguous
+    channels. Returns a dict: h (None unless want_h), hT the last states, and ck (None unless
+    want_ck) the checkpoints with which recurrence_vjp recomputes the states."""
+    import torch
+    prob = _recurrence_problem(a, u, gate)
+    B, T, D = a.shape
+    acc = _acc(prob.dtype)
+    _expect("h0", h0, (B, D), acc, a.device)
+    _check_lens(lens, a)
+    info = adst_recurrence_plan(prob)
+
+    def body(handle):
+        h = torch.empty((B, T, D), dtype=a.dtype, device=a.device) if want_h else None
+        hT = torch.empty((B, D), dtype=acc, device=a.device)
+        ck = _bytes(info.ck_bytes, a.device) if want_ck else None
+        ws = _bytes(info.workspace_bytes, a.device)
+        adst_recurrence_forward(prob, a, u, h0, lens, h, hT, ck, ws, info.workspace_bytes, handle)
+        return {"h": h, "hT": hT, "ck": ck}
+
+    return _call(a.device, stream, (a, u, h0, lens), body)
+
+
+def recurrence_vjp(a, u, dh, h0=None, lens=None, dhT=None, ck=None, gate=ADST_GATE_COEFF,
+                   stream=None):
+    """The VJP of recurrence: dh = dL/dh, dhT = dL/dhT (optional). ck: the checkpoints that
+    recurrence gave for the same a, u, h0, lens and gate; None recomputes them, at the price of
+    one more pass over a and u. Returns a dict: da, du [batch, steps, channels] and dh0."""
+    import torch
+    if dh is None:
+        raise ValueError("dh is required")
+    prob = _recurrence_problem(a, u, gate, dh)
+    B, T, D = a.shape
+    acc = _acc(prob.dtype)
+    _expect("h0", h0, (B, D), acc, a.device)
+    _expect("dhT", dhT, (B, D), acc, a.device)
+    _check_lens(lens, a)
+    info = adst_recurrence_plan(prob)
+    _expect("ck", ck, (info.ck_bytes,), torch.uint8, a.device)
+    need = info.workspace_bytes if ck is not None else info.vjp_workspace_bytes
+
+    def body(handle):
+        da, du = (torch.empty((B, T, D), dtype=a.dtype, device=a.device) for _ in range(2))
+        dh0 = torch.empty((B, D), dtype=acc, device=a.device)
+        ws = _bytes(need, a.device)
+        adst_recurrence_vjp(prob, a, u, h0, lens, ck, dh, dhT, da, du, dh0, ws, need, handle)
+        return {"da": da, "du": du, "dh0": dh0}
+
+    return _call(a.device, stream, (a, u, dh, h0, lens, dhT, ck), body)
+
+
+def recurrence_step(a, u, state, slots=None, gate=ADST_GATE_COEFF, stream=None):
+    """One step of every row of a, u [batch, channels] on the pool of states
+    [nstates, channels] (float32, float64 for float64 inputs), updated in place. slots [batch]
+    int32: each row's state, no two the same; None: row b's is state[b]. Rows whose slot is
+    outside the pool are idle: their h is 0. Returns h [batch, channels]."""
+    import torch
+    code = _code("a", a)
+    if a.dim() != 2:
+        raise ValueError(f"a must be [batch, channels], not {tuple(a.shape)}")
+    B, D = a.shape
+    _expect("u", u, (B, D), a.dtype, a.device, contiguous=False)
+    _channels_contiguous("a", a)
+    _channels_contiguous("u", u)
+    if state is None or state.dim() != 2 or state.shape[1] != D:
+        raise ValueError(f"state must be [nstates, {D}]")
+    _expect("state", state, state.shape, _acc(code), a.device)
+    _expect("slots", slots, (B,), torch.int32, a.device)
+    prob = adst_recurrence_problem(code, gate, B, 1, D, a.stride(0), 0, u.stride(0), 0, 0, 0)
+
+    def body(handle):
+        h = torch.empty((B, D), dtype=a.dtype, device=a.device)
+        adst_recurrence_step(prob, a, u, slots, state, state.shape[0], h, handle)
+        return h
+
+    return _call(a.device, stream, (a, u, state, slots), body)
+
+
+# -------------------------------------------------------------- layer norm
+def _rows(name, t, n):
+    """Rows and row stride of t [..., n], whose leading axes have to merge into one."""
+    if t.dim() < 1 or t.shape[-1] != n:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not [..., {n}]")
+    _channels_contiguous(name, t)
+    if t.dim() == 1:
+        return 1, n
+    if t.dim() == 2 or t.is_contiguous():
+        return t.numel() // n, t.stride(0) if t.dim() == 2 else n
+    rows, stride = 1, None
+    for size, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if stride is None:
+            stride = s
+        elif s != stride * rows:
+            raise ValueError(f"{name}'s leading axes must be one axis of equally spaced rows")
+        rows *= size
+    return rows, n if stride is None else stride
+
+
+def _norm_problem(x, w, b, eps, dy=None):
+    code = _code("x", x)
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"x must be [..., n] with n >= 1, not {tuple(x.shape)}")
+    n = x.shape[-1]
+    rows, sx = _rows("x", x, n)
+    sdy = n
+    if dy is not None:
+        _expect("dy", dy, x.shape, x.dtype, x.device, contiguous=False)
+        _, sdy = _rows("dy", dy, n)
+    wcode = code
+    given = w if w is not None else b
+    if given is not None:
+        wcode = _code("w" if w is not None else "b", given)
+        if wcode != code and not (code in (ADST_BF16, ADST_F16) and wcode == ADST_F32):
+            raise ValueError(f"weights must be {x.dtype} (or float32 beside 16-bit types), "
+                             f"not {given.dtype}")
+        _expect("w", w, (n,), given.dtype, x.device)
+        _expect("b", b, (n,), given.dtype, x.device)
+    return adst_norm_problem(code, wcode, rows, n, sx, sdy, eps)
+
+
+def layer_norm(x, w=None, b=None, eps=1e-5, stream=None):
+    """Layer norm over the last axis of x [..., n]; w and b [n] of x's dtype, or float32 beside
+    16-bit types. Returns a dict: y (contiguous), and mean and rstd of each row (float32, or
+    float64 for float64) for layer_norm_vjp."""
+    import torch
+    prob = _norm_problem(x, w, b, eps)
+    acc = _acc(prob.dtype)
+
+    def body(handle):
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        mean, rstd = (torch.empty(x.shape[:-1], dtype=acc, device=x.device) for _ in range(2))
+        adst_layer_norm_forward(prob, x, w, b, y, mean, rstd, handle)
+        return {"y": y, "mean": mean, "rstd": rstd}
+
+    return _call(x.device, stream, (x, w, b), body)
+
+
+def layer_norm_vjp(x, dy, mean, rstd, w=None, want_dx=True, want_dw=True, want_db=True,
+                   stream=None):
+    """The VJP of layer_norm: mean and rstd as it gave them. Returns a dict: dx [..., n]
+    (contiguous), dw and db [n] in w's dtype (x's without w), each None unless wanted."""
+    import torch
+    if dy is None:
+        raise ValueError("dy is required")
+    prob = _norm_problem(x, w, None, 0.0, dy)
+    acc = _acc(prob.dtype)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is None:
+            raise ValueError(f"{name} is required")
+        _expect(name, t, x.shape[:-1], acc, x.device)
+    wt = w.dtype if w is not None else x.dtype
+
+    def body(handle):
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
+        dw = torch.empty(prob.n, dtype=wt, device=x.device) if want_dw else None
+        db = torch.empty(prob.n, dtype=wt, device=x.device) if want_db else None
+        need = adst_layer_norm_workspace_bytes(prob) if want_dw or want_db else 0
+        ws = _bytes(need, x.device)
+        adst_layer_norm_vjp(prob, x, dy, w, mean, rstd, dx, dw, db, ws, need, handle)
+        return {"dx": dx, "dw": dw, "db": db}
+
+    return _call(x.device, stream, (x, dy, mean, rstd, w), body)
+
+
+# ------------------------------------------------------------------- AdamW
+class AdamW:
+    """AdamW over a list of tensors, one call a step, updated in place.
+
+    params: contiguous float32 (or float64) tensors on one GPU. bits: 32 for states in the
+    parameters' type, 8 for blocks of 256 e4m3 codes with a scale each (float32 parameters).
+    state: {"m", "v"} (and "m_scale", "v_scale" with 8 bits), lists of tensors like those this
+    object holds under these names, to go on from; zeros if None. copies: contiguous tensors
+    shaped like params, one dtype of float32, bfloat16 and float16, that receive the new
+    parameters in it. lr and weight_decay: a number, or one for each tensor."""
+
+    def __init__(self, params, bits=32, state=None, copies=None, lr=1e-3, betas=(0.9, 0.999),
+                 eps=1e-8, weight_decay=0.01):
+        import torch
+        self.params = tuple(params)
+        n = len(self.params)
+        if n == 0:
+            raise ValueError("params is empty")
+        if bits not in (32, 8):
+            raise ValueError("bits must be 32 or 8")
+        first = self.params[0]
+        code = _code("params[0]", first)
+        if code not in (ADST_F32, ADST_F64) or (bits == 8 and code == ADST_F64):
+            raise TypeError(f"parameters must be float32, or float64 with 32-bit states, "
+                            f"not {first.dtype}")
+        self.device = first.device
+        for i, p in enumerate(self.params):
+            _expect(f"params[{i}]", p, getattr(p, "shape", ()), first.dtype, self.device)
+        self.copies = None if copies is None else tuple(copies)
+        copy_code = ADST_BF16
+        if self.copies is not None:
+            if len(self.copies) != n:
+                raise ValueError(f"{len(self.copies)} copies of {n} parameters")
+            if n:
+                copy_code = _code("copies[0]", self.copies[0])
+                if copy_code == ADST_F64:
+                    raise TypeError("copies must be float32, bfloat16 or float16")
+            for i, (c, p) in enumerate(zip(self.copies, self.params)):
+                _expect(f"copies[{i}]", c, p.shape, self.copies[0].dtype, self.device)
+        self.bits = bits
+        self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
+        self.t = 0
+        names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
+        for name in names:
+            shapes = [(-(-p.numel() // ADST_STATE_BLOCK),) if name.endswith("scale") else p.shape
+                      for p in self.params]
+            dtype = (torch.float32 if name.endswith("scale") else
+                     torch.float8_e4m3fn if bits == 8 else first.dtype)
+            if state is None:
+                held = tuple(torch.zeros(s, dtype=dtype, device=self.device) for s in shapes)
+            else:
+                held = tuple(state[name])
+                if len(held) != n:
+                    raise ValueError(f"{len(held)} tensors of state {name} for {n} parameters")
+                for i, (t, s) in enumerate(zip(held, shapes)):
+                    _expect(f"{name}[{i}]", t, s, dtype, self.device)
+            setattr(self, name, held)
+        self._n = n
+        self._numel = [p.numel() for p in self.params]
+        self._rows = (adst_adamw_tensor * n)()
+        for i, row in enumerate(self._rows):
+            for name in names:
+                setattr(row, name, getattr(self, name)[i].data_ptr())
+            row.n = self._numel[i]
+        self._set("lr", lr)
+        self._set("weight_decay", weight_decay)
+        self._prob = adst_adamw_problem(code, ADST_F32, copy_code, bits, 0, *self.betas, self.eps,
+                                        None)
+
+    def _set(self, name, value):
+        values = [value] * self._n if isinstance(value, (int, float)) else list(value)
+        if len(values) != self._n:
+            raise ValueError(f"{len(values)} values of {name} for {self._n} parameters")
+        setattr(self, name, value)
+        for row, x in zip(self._rows, values):
+            setattr(row, name, float(x))
+
+    def step(self, grads, lr=None, weight_decay=None, t=None, grad_scale=None, stream=None):
+        """One step with contiguous gradients like params (float32, bfloat16 or float16, one
+        dtype; float64 for float64). lr, weight_decay: from now on. t: the step's number, one more
+        than the last one's if None. grad_scale: a float32 tensor of one value that multiplies the
+        gradients; where it is not finite nothing is updated (the step's number counts on)."""
+        import torch
+        if len(grads) != self._n:
+            raise ValueError(f"{len(grads)} gradients for {self._n} parameters")
+        dtype = grads[0].dtype
+        code = _code("grads[0]", grads[0])
+        if (code == ADST_F64) != (self._prob.dtype == ADST_F64):
+            raise TypeError(f"gradients of {self.params[0].dtype} parameters in {dtype}")
+        device = self.device
+        for i, g in enumerate(grads):
+            if g.dtype is not dtype or g.device != device or g.numel() != self._numel[i] or \
+                    not g.is_contiguous():
+                raise ValueError(f"grads[{i}] must be contiguous, of {self._numel[i]} values in "
+                                 f"{dtype} on {device}")
+        if grad_scale is not None:
+            _expect("grad_scale", grad_scale, grad_scale.shape, torch.float32, device)
+            if grad_scale.numel() != 1:
+                raise ValueError("grad_scale must have one value")
+        if lr is not None:
+            self._set("lr", lr)
+        if weight_decay is not None:
+            self._set("weight_decay", weight_decay)
+        rows = self._rows
+        for row, p, g in zip(rows, self.params, grads):
+            row.p, row.grad = p.data_ptr(), g.data_ptr()
+        if self.copies is not None:
+            for row, c in zip(rows, self.copies):
+                row.copy = c.data_ptr()
+        prob = self._prob
+        prob.grad_dtype = code
+        prob.t = self.t + 1 if t is None else t
+        prob.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
+        used = () if stream is None else (*self.params, *grads, grad_scale)
+        _call(device, stream, used, lambda handle: adst_adamw(prob, rows, self._n, handle))
+        self.t = prob.t

@@ -590,14 +590,15 @@ adst_status adst_layer_norm_vjp(const adst_norm_problem* prob, const void* x, co
  *   g = grad_scale * grad
  *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * (g * g)
  *   p = p * (1 - lr * weight_decay)
- *       - (lr / (1 - beta1^t)) * (m / (sqrt(v) / sqrt(1 - beta2^t) + eps))
- * evaluated in the order written, without fused multiply-add. Parameters are
+ *       - (lr / (1 - beta1^t)) * (m / (sqrt(v) * (1 / sqrt(1 - beta2^t)) + eps))
+ * evaluated in the order written, without fused multiply-add; what depends on
+ * the step and the tensor alone is evaluated in double and rounded. Parameters are
  * F32 (F64); gradients F32, BF16 or F16 (F64 with F64), one type per call.
  * States are in the parameters' type (bits = 32) or, with F32 parameters,
  * coded in 8 bits (bits = 8): of each tensor's blocks of ADST_STATE_BLOCK
- * consecutive values (the last one shorter) the largest magnitude over 448 is
- * the block's scale, and a value is held as value / scale rounded to e4m3 (4
- * exponent and 3 mantissa bits, OCP). Of v its square root is held, positive
+ * consecutive values (the last one shorter) the largest magnitude times 1/448
+ * is the block's scale, and a value is held as value * ((1 / largest) * 448)
+ * rounded to e4m3 (4 exponent and 3 mantissa bits, OCP). Of v its square root is held, positive
  * values of which never round to zero. A block whose magnitudes are all below
  * 2^-100 is held as zeros. Parameters are updated with the states before they
  * are rounded to codes. A NaN or infinity in a gradient makes its block's

@@ -116,7 +116,7 @@ def _call(device, stream, inputs, body):
     """body(stream handle) on the tensors' device, allocations of body included."""
     import torch
     if stream is None and torch.cuda.current_device() == device.index:
-        return body(torch.cuda.current_stream(device).cuda_stream)
+        return body(torch._C._cuda_getCurrentRawStream(device.index))
     with torch.cuda.device(device):
         if stream is None:
             return body(torch.cuda.current_stream(device).cuda_stream)

@@ -16,16 +16,20 @@
 // a, u and dh and writing da and du is all it moves.
 //
 // Between spans: a workgroup publishes its span's map (A, H) as soon as it has
-// it, and the state at its end as soon as it knows that. To learn the state at
-// its start it takes the nearest published state before it and applies the
-// published maps of the spans between, in order: state' = A state + H. That is
-// what each of those spans computes for itself, bit for bit, so the result
-// does not depend on which states happened to be there. Spans are taken from a
-// counter per row in the order of time, so a workgroup only ever waits for
-// workgroups that have started before it, whose maps depend on nothing: every
-// wait ends. What is published is complete in itself (each word is written
-// whole, and its initial pattern is never a value), so no fence is needed; the
-// accesses are of agent scope, which the caches of the XCDs keep coherent.
+// it. Eight spans form a group; a group's last workgroup also publishes the
+// group's map, composed of its spans' in order, and the state at the group's
+// end, state' = A state + H. The state that enters a span is that of its
+// group's start with the maps of the group's earlier spans applied in order;
+// the state of a group's start is the nearest one published before it, with
+// the maps of the groups between applied in order. That is what each group
+// computes for itself, bit for bit, so results do not depend on which states
+// happened to be there. Spans are taken from a counter per row in the order of
+// the sweep, so a workgroup only ever waits for workgroups that have started
+// before it; spans' maps depend on nothing, groups' on spans', states on both:
+// every wait ends. What is published is complete in itself (each word is
+// written whole, and its initial pattern is never a value), so no fence is
+// needed; the accesses are of agent scope, which the caches of the XCDs keep
+// coherent.
 
 #include "seq_common.h"
 #include "seq_kernels.h"
@@ -33,30 +37,83 @@
 namespace adst {
 namespace {
 
-constexpr int kLanes = 16;  // along channels
-
-template <class T>
-struct Shape {
-  static constexpr int V = Vec<T>::N;               // channels of a lane
-  static constexpr int R = sizeof(T) == 2 ? 4 : 8;  // steps of a lane
-  static constexpr int C = kLanes * V;              // channels of a workgroup
-  static constexpr int span(int threads) { return threads / kLanes * R; }
+// V consecutive channels of T, at any element's address.
+template <class T, int V>
+struct Pack {
+  typedef T type __attribute__((ext_vector_type(V)));
+  typedef T unaligned __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  type v;
 };
+template <class T, int V, bool STREAM = false>
+__device__ inline Pack<T, V> load_pack(const T* p, int n) {
+  Pack<T, V> r;
+  if (n >= V) {
+    const auto* at = reinterpret_cast<const typename Pack<T, V>::unaligned*>(p);
+    if constexpr (STREAM) r.v = __builtin_nontemporal_load(at);
+    else r.v = *at;
+    return r;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.v[i] = i < n ? p[i] : T(0);
+  return r;
+}
+template <class T, int V, bool STREAM = false>
+__device__ inline void store_pack(T* p, Pack<T, V> x, int n) {
+  if (n >= V) {
+    auto* at = reinterpret_cast<typename Pack<T, V>::unaligned*>(p);
+    if constexpr (STREAM) __builtin_nontemporal_store(x.v, at);
+    else *at = x.v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < n) p[i] = x.v[i];
+}
+
+// A workgroup of NT threads: a wave's lanes lie along channels, V of them a
+// lane; each wave holds R consecutive steps.
+template <class T, int NT_, bool STREAM_>
+struct Shape {
+  typedef Acc<T> A;
+  static constexpr bool STREAM = STREAM_;
+  static constexpr int V = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int R = sizeof(T) == 8 ? 8 : 16;
+  static constexpr int W = NT_ / 64;
+  static constexpr int C = 64 * V;      // channels of a workgroup
+  static constexpr int kSpan = W * R;   // its steps
+  typedef Pack<T, V> P;
+};
+constexpr int kForward = 512, kReverse = 256;  // threads of a workgroup on long rows
+constexpr int kCkWaves = 4;  // a checkpoint at every fourth wave's steps
 
 // How a problem is laid out over workgroups of `threads`.
 struct Grid {
   int threads;
   int span;    // steps
   int spans;   // per batch row
+  int groups;  // of spans
   int slabs;   // of C channels
+  int cks;     // checkpoints of a batch row
   uint32_t chains;  // batch rows times slabs
+  uint32_t round;   // chains, to a multiple of 8: the workgroups of one span of each
 };
 
-// What a launch of several spans publishes in, all ones at its start.
+// The chain of a workgroup (past the last one: none). Consecutive workgroups
+// go to the 8 XCDs in turn; each XCD gets neighbouring chains, whose rows
+// share cache lines where a row is not a multiple of them, and keeps them.
+__device__ inline uint32_t chain_of(const Grid& g) {
+  const uint32_t x = blockIdx.x % g.round;
+  return x % 8 * (g.round / 8) + x / 8;
+}
+
+// What a launch of several spans publishes in, all ones at its start. Spans
+// are counted in the order of the sweep.
+constexpr int kGroup = 8;
 struct Board {
   int32_t* next;  // a counter per chain, 32 bytes apart, from -1
-  void* state;    // [chain][span][C] accumulation type
-  void* map;      // [chain][span][C] two of it
+  void* state;    // [chain][groups][C] accumulation type: the state at a group's end
+  void* group;    // [chain][groups][C] two of it: a group's map
+  void* map;      // [chain][spans][C] two of it: a span's
 };
 constexpr int kCounterInts = 8;
 
@@ -66,20 +123,25 @@ __device__ inline double exp_full(double x) { return exp(x); }
 __device__ inline float inverse(float x) { return __builtin_amdgcn_rcpf(x); }  // within 1 ulp
 __device__ inline double inverse(double x) { return 1.0 / x; }
 
-// min(s, 1 - s) to full relative precision, with the sign of a: with
-// e = exp(-|a|) in [0, 1], it is e / (1 + e), and the other one is 1 less it,
-// which loses nothing as it is at least a half. Behind a 16-bit value the
-// exponential may be off by |a| units of 2^-24.
+// s = 1 / (1 + exp(-a)) and q = 1 - s = 1 / (1 + exp(a)), each to full
+// relative precision. Behind a 16-bit value the exponential may be off by |a|
+// units of 2^-24, and gates below 2^-115 stop at that.
 template <class T>
-__device__ inline Acc<T> gate_of(Acc<T> a) {
+__device__ inline void gates(Acc<T> a, Acc<T>* s, Acc<T>* q) {
   typedef Acc<T> A;
-  A e;
-  if constexpr (sizeof(T) == 2)
-    e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(a));
-  else
-    e = exp_full(-__builtin_elementwise_abs(a));
-  return __builtin_elementwise_copysign(e * inverse(A(1) + e), a);
+  if constexpr (sizeof(T) == 2) {
+    const float x = -1.44269504f * a;
+    const float e = __builtin_amdgcn_exp2f(x > 115.0f ? 115.0f : x);  // NaN stays
+    *s = inverse(1.0f + e);
+    *q = e * *s;
+  } else {  // with e = exp(-|a|) in [0, 1] nothing overflows, and 0 and 1 are reached
+    const A e = exp_full(-__builtin_elementwise_abs(a));
+    const A big = inverse(A(1) + e), small = e * big;
+    *s = __builtin_signbit(a) ? small : big;
+    *q = __builtin_signbit(a) ? big : small;
+  }
 }
+
 // The compiler treats the values as new ones: it does not keep what it
 // derived from them before, which would take more registers than there are.
 template <class A, int R, int V>
@@ -89,15 +151,16 @@ __device__ inline void forget(A (&x)[R][V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) asm volatile("" : "+v"(x[r][i]));
 }
-template <class A>
-__device__ inline bool negative(A x) {
-  return __builtin_signbit(x);
-}
-template <class A>
-__device__ inline void open_gate(A gate, A* s, A* q) {
-  const A small = __builtin_elementwise_abs(gate), big = A(1) - small;
-  *s = negative(gate) ? small : big;
-  *q = negative(gate) ? big : small;
+template <class T, int V, int R>
+__device__ inline void forget(Pack<T, V> (&x)[R]) {  // and unpacks again
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      uint32_t w = __builtin_bit_cast(uint32_t, x[r].v);
+      asm volatile("" : "+v"(w));
+      x[r].v = __builtin_bit_cast(typename Pack<T, V>::type, w);
+    }
+  }
 }
 
 __device__ inline int64_t row_length(const int32_t* lens, int64_t b, int64_t T) {
@@ -107,37 +170,6 @@ __device__ inline int64_t row_length(const int32_t* lens, int64_t b, int64_t T) 
 }
 
 // ------------------------------------------------------- maps along the time
-// Inclusive composition over the wave's groups of lanes, each group's map
-// applied after those of the groups before it (FORWARD) or after it.
-template <bool FORWARD, class A, int V>
-__device__ inline void compose_wave(A (&a)[V], A (&h)[V]) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int off = kLanes; off < 64; off <<= 1) {
-    const bool has = FORWARD ? lane >= off : lane + off < 64;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const A oa = FORWARD ? __shfl_up(a[i], off, 64) : __shfl_down(a[i], off, 64);
-      const A oh = FORWARD ? __shfl_up(h[i], off, 64) : __shfl_down(h[i], off, 64);
-      h[i] = has ? fma_(a[i], oh, h[i]) : h[i];
-      a[i] = has ? a[i] * oa : a[i];
-    }
-  }
-}
-// The composition of the groups before (after) this one, from the inclusive one.
-template <bool FORWARD, class A, int V>
-__device__ inline void exclude_own(A (&a)[V], A (&h)[V]) {
-  const int lane = threadIdx.x & 63;
-  const bool has = FORWARD ? lane >= kLanes : lane + kLanes < 64;
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const A oa = FORWARD ? __shfl_up(a[i], kLanes, 64) : __shfl_down(a[i], kLanes, 64);
-    const A oh = FORWARD ? __shfl_up(h[i], kLanes, 64) : __shfl_down(h[i], kLanes, 64);
-    a[i] = has ? oa : A(1);
-    h[i] = has ? oh : A(0);
-  }
-}
-
 // Per wave and channel, in LDS: first each wave's map, then the composition of
 // the waves before (after) it.
 template <class A, int W, int C>
@@ -205,6 +237,7 @@ struct MapWords<float> {
   __device__ static void store(void* base, int64_t i, float a, float h) {
     agent_store((uint64_t*)base + i, (uint64_t)word_of(h) << 32 | word_of(a));
   }
+  __device__ float scale(float x) const { return __builtin_bit_cast(float, (uint32_t)w) * x; }
   __device__ float apply(float x) const {
     return fma_(__builtin_bit_cast(float, (uint32_t)w), x,
                 __builtin_bit_cast(float, (uint32_t)(w >> 32)));
@@ -223,71 +256,127 @@ struct MapWords<double> {
     agent_store(p, word_of(a));
     agent_store(p + 1, word_of(h));
   }
+  __device__ double scale(double x) const { return __builtin_bit_cast(double, a) * x; }
   __device__ double apply(double x) const {
     return fma_(__builtin_bit_cast(double, a), x, __builtin_bit_cast(double, h));
   }
 };
 
-// The state that enters this span, one thread a channel. `at`: this span's
-// and channel's place on the board; the span before (FORWARD) or after it is
-// `step` places away, the wave's first channel's place is `first`; `before`:
-// how many spans there are on that side, at least 1, the last of which
-// publishes its end state without waiting. Whole waves call this; a lane
-// without a channel (mine false) only takes part in the looking.
+// This span's map, the e-th of its chain.
 template <class A>
-__device__ inline A enter(const Board& bd, int64_t at, int64_t first, int64_t step, int before,
-                          bool mine) {
-  const Word<A>* states = (const Word<A>*)bd.state;
-  // Lane l looks at the span l + 1 away: the nearest one with a state, and
-  // whether all maps up to it are there.
+__device__ inline void publish(const Board& bd, const Grid& g, uint32_t chain, int e, int C,
+                               int c, A a, A h) {
+  MapWords<A>::store(bd.map, ((int64_t)chain * g.spans + e) * C + c, a, h);
+  asm volatile("" ::: "memory");  // before this wave waits for anything
+}
+
+// The state that enters this chain's e-th span, e > 0, one thread a channel;
+// whole waves call this, and a lane without a channel (mine false) only takes
+// part in the looking. first: the state that enters span 0. (oa, oh): this
+// span's map. more: spans follow, which read what the last one of a group
+// publishes. c: the channel's place in the slab.
+template <class A, int C>
+__device__ inline A enter(const Board& bd, const Grid& g, uint32_t chain, int e, bool more, int c,
+                          bool mine, A first, A oa, A oh) {
   const int lane = threadIdx.x & 63;
-  const bool there = lane < before;
-  const int64_t seen = first + (int64_t)(lane + 1) * step;
-  int k;
+  const int j = e / kGroup, i = e % kGroup;
+  const int64_t maps = ((int64_t)chain * g.spans + (e - i)) * C + c;  // the group's first span's
+  const int64_t groups = (int64_t)chain * g.groups * C + c;
+  const Word<A>* states = (const Word<A>*)bd.state;
+  const bool closes = i == kGroup - 1 && more;
+  // Lane l < 32 looks at the state of the start of the group l before this one
+  // (group 0's is `first`), lane 32 + l at the map of the group l + 1 before it.
+  const int back = lane & 31;
+  const bool looks = back < j;
+  const int64_t seen = groups - (c & 63) + (int64_t)(j - 1 - back) * C;
+  MapWords<A> m[kGroup - 1];
+#pragma unroll
+  for (int l = 0; l < kGroup - 1; ++l)
+    if (l < i) m[l] = MapWords<A>::load(bd.map, maps + (int64_t)l * C);
+  Word<A> w;
+  int dist = 0;
+  A ga = oa, gh = oh;
+  bool composed = !closes;
   for (;;) {
-    const bool s = there && ~agent_load(states + seen) != 0;
-    const bool m = there && MapWords<A>::load(bd.map, seen).full();
-    const uint64_t with_state = __ballot(s), with_map = __ballot(m);
-    if (with_state) {
-      k = __ffsll((unsigned long long)with_state) - 1;
-      const uint64_t need = (uint64_t(1) << k) - 1;
+    w = j > 0 && mine ? agent_load(states + groups + (int64_t)(j - 1) * C) : 0;
+    bool there = false;
+    if (looks)
+      there = lane < 32 ? ~agent_load(states + seen) != 0
+                        : MapWords<A>::load(bd.group, seen).full();
+    there = there || (lane < 32 && back == j);
+    const uint64_t all = __ballot(there);
+    bool missing = false;
+    if (mine) {
+#pragma unroll
+      for (int l = 0; l < kGroup - 1; ++l)
+        if (l < i) missing = missing || !m[l].full();
+    }
+    const bool have = __ballot(missing) == 0;
+    if (have && !composed) {  // the group's map, before any wait for a state
+      composed = true;
+      if (mine) {
+        A a = A(1), h = A(0);
+#pragma unroll
+        for (int l = 0; l < kGroup - 1; ++l) {
+          h = m[l].apply(h);
+          a = m[l].scale(a);
+        }
+        ga = oa * a;
+        gh = fma_(oa, h, oh);
+        MapWords<A>::store(bd.group, groups + (int64_t)j * C, ga, gh);
+      }
+    }
+    const uint32_t with_state = (uint32_t)all, with_map = (uint32_t)(all >> 32);
+    if (have && with_state) {
+      dist = __ffs((int)with_state) - 1;
+      const uint32_t need = (1u << dist) - 1u;
       if ((with_map & need) == need) break;
     }
     __builtin_amdgcn_s_sleep(1);
+    if (!have && mine) {
+#pragma unroll
+      for (int l = 0; l < kGroup - 1; ++l)
+        if (l < i && !m[l].full()) m[l] = MapWords<A>::load(bd.map, maps + (int64_t)l * C);
+    }
   }
-  A x = A(0);
-  if (!mine) return x;
+  if (!mine) return A(0);
   // The words of this lane's own channel were written with those looked at;
   // each is checked all the same.
-  int64_t j = at + (int64_t)(k + 1) * step;
-  Word<A> w;
-  do w = agent_load(states + j);
-  while (~w == 0);
-  x = __builtin_bit_cast(A, w);
-  constexpr int kAhead = 8;  // maps under way at a time
-  while (k > 0) {
-    const int n = k < kAhead ? k : kAhead;
-    MapWords<A> m[kAhead];
+  constexpr int kAhead = 4;  // maps under way at a time
+  A x = first;
+  for (int k = dist; k >= 0 && j > 0;) {  // from the start of group j - k
+    if (k == dist && k < j) {
+      const int64_t at = groups + (int64_t)(j - 1 - k) * C;
+      if (k > 0) w = agent_load(states + at);
+      while (~w == 0) w = agent_load(states + at);
+      x = __builtin_bit_cast(A, w);
+    }
+    if (k == 0) break;
+    MapWords<A> b[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (i < n) m[i] = MapWords<A>::load(bd.map, j - (int64_t)(i + 1) * step);
+    for (int l = 0; l < kAhead; ++l)
+      if (l < k) b[l] = MapWords<A>::load(bd.group, groups + (int64_t)(j - k + l) * C);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (i < n) {
-        while (!m[i].full()) m[i] = MapWords<A>::load(bd.map, j - (int64_t)(i + 1) * step);
-        x = m[i].apply(x);
+    for (int l = 0; l < kAhead; ++l)
+      if (l < k) {
+        while (!b[l].full())
+          b[l] = MapWords<A>::load(bd.group, groups + (int64_t)(j - k + l) * C);
+        x = b[l].apply(x);
       }
-    j -= (int64_t)n * step;
-    k -= n;
+    if (k <= kAhead) break;
+    k -= kAhead;
   }
+  if (closes) agent_store((Word<A>*)bd.state + groups + (int64_t)j * C, word_of(fma_(ga, x, gh)));
+#pragma unroll
+  for (int l = 0; l < kGroup - 1; ++l)
+    if (l < i) x = m[l].apply(x);
   return x;
 }
 
 // -------------------------------------------------------------- the kernels
 // Where a workgroup works, and how much of it exists.
-template <class T, int NT>
+template <class S>
 struct Place {
-  typedef Shape<T> S;
   int64_t b, len;  // the batch row and its steps
   int slab, span;
   int64_t t0;     // the span's first step
@@ -299,220 +388,198 @@ struct Place {
     b = chain / (uint32_t)g.slabs;
     slab = (int)(chain % (uint32_t)g.slabs);
     len = row_length(r.lens, b, r.T);
-    constexpr int kSpan = S::span(NT);
-    t0 = (int64_t)span * kSpan;
-    mine = t0 + threadIdx.x / kLanes * S::R;
-    c0 = slab * S::C + (int)(threadIdx.x % kLanes) * S::V;
+    t0 = (int64_t)span * S::kSpan;
+    mine = t0 + threadIdx.x / 64 * S::R;
+    c0 = slab * S::C + (int)(threadIdx.x & 63) * S::V;
     const int64_t left = r.D - c0;
     n = left < 0 ? 0 : left < S::V ? (int)left : S::V;
-    whole = (int64_t)(slab + 1) * S::C <= r.D && t0 + kSpan <= len;
+    whole = (int64_t)(slab + 1) * S::C <= r.D && t0 + S::kSpan <= len;
   }
 };
 
-// This lane's R vectors of a strided array; zero where steps or channels end.
-template <class T, int NT>
-__device__ inline void load_steps(const void* base, int64_t sb, int64_t stp,
-                                  const Place<T, NT>& at, Vec<T> (&v)[Shape<T>::R]) {
+// This lane's R packs of a strided array; `none` where steps or channels end.
+template <class T, class S>
+__device__ inline void load_steps(const void* base, int64_t sb, int64_t stp, const Place<S>& at,
+                                  T none, typename S::P (&v)[S::R]) {
   const T* p = (const T*)base + at.b * sb + at.mine * stp + at.c0;
   if (at.whole) {
 #pragma unroll
-    for (int r = 0; r < Shape<T>::R; ++r) v[r] = load_vec(p + r * stp);
+    for (int r = 0; r < S::R; ++r) v[r] = load_pack<T, S::V, S::STREAM>(p + r * stp, S::V);
     return;
   }
 #pragma unroll
-  for (int r = 0; r < Shape<T>::R; ++r) {
-    v[r].v = typename Vec<T>::type{};
-    if (at.mine + r < at.len && at.n > 0) v[r] = load_part(p + r * stp, at.n);
+  for (int r = 0; r < S::R; ++r) {
+#pragma unroll
+    for (int i = 0; i < S::V; ++i) v[r].v[i] = none;
+    if (at.mine + r < at.len && at.n > 0) v[r] = load_pack<T, S::V>(p + r * stp, at.n);
   }
 }
 // Stores them to a contiguous array: up to T, zeros from len on.
-template <class T, int NT>
-__device__ inline void store_steps(void* base, const RecArgs& q, const Place<T, NT>& at,
-                                   const Vec<T> (&v)[Shape<T>::R]) {
+template <class T, class S>
+__device__ inline void store_steps(void* base, const RecArgs& q, const Place<S>& at,
+                                   const typename S::P (&v)[S::R]) {
   T* p = (T*)base + (at.b * q.T + at.mine) * q.D + at.c0;
   if (at.whole) {
 #pragma unroll
-    for (int r = 0; r < Shape<T>::R; ++r) store_vec(p + r * q.D, v[r]);
+    for (int r = 0; r < S::R; ++r) store_pack<T, S::V, S::STREAM>(p + r * q.D, v[r], S::V);
     return;
   }
 #pragma unroll
-  for (int r = 0; r < Shape<T>::R; ++r)
+  for (int r = 0; r < S::R; ++r)
     if (at.mine + r < q.T && at.n > 0) {
-      Vec<T> x = v[r];
-      if (at.mine + r >= at.len) x.v = typename Vec<T>::type{};
-      store_part(p + r * q.D, x, at.n);
+      typename S::P x = v[r];
+      if (at.mine + r >= at.len) x.v = typename S::P::type{};
+      store_pack<T, S::V>(p + r * q.D, x, at.n);
     }
 }
 
-template <class T, bool SIG, bool MULTI, int NT>
-__global__ __launch_bounds__(NT) void rec_fwd(RecArgs q, Grid g, Board bd) {
-  typedef Acc<T> A;
-  typedef Shape<T> S;
-  constexpr int V = S::V, R = S::R, C = S::C, W = NT / 64;
-  __shared__ Maps<A, W, C> maps;
-  __shared__ A start[C];
+// What a and u are beyond a row's end, so that a step keeps the state and the
+// gradient: coefficient 1 and input 0.
+template <class T, bool SIG>
+__device__ inline T keep() {
+  return SIG ? (T)__builtin_inff() : T(1);
+}
+
+// The span this workgroup takes: the next one of its chain.
+__device__ inline int take_span(const Board& bd, uint32_t chain) {
   __shared__ int ticket;
-  const uint32_t chain = blockIdx.x % g.chains;
-  if (MULTI) {
-    if (threadIdx.x == 0) ticket = atomicAdd(bd.next + (int64_t)chain * kCounterInts, 1) + 1;
-    __syncthreads();
-  }
-  const Place<T, NT> at(q, g, chain, MULTI ? ticket : 0);
+  if (threadIdx.x == 0) ticket = atomicAdd(bd.next + (int64_t)chain * kCounterInts, 1) + 1;
+  __syncthreads();
+  return ticket;
+}
+
+template <class T, bool SIG, bool MULTI, bool STREAM, int NT>
+__global__ __launch_bounds__(NT, 4) void rec_fwd(RecArgs q, Grid g, Board bd) {
+  typedef Shape<T, NT, STREAM> S;
+  typedef typename S::A A;
+  constexpr int V = S::V, R = S::R, C = S::C;
+  __shared__ Maps<A, S::W, C> maps;
+  __shared__ A start[C];
+  const uint32_t chain = chain_of(g);
+  if (chain >= g.chains) return;
+  const Place<S> at(q, g, chain, MULTI ? take_span(bd, chain) : 0);
+  typename S::P va[R], vu[R];
   if (at.t0 >= at.len && at.span > 0) {  // nothing but zeros, and nobody asks for its state
-    Vec<T> zero[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) zero[r].v = typename Vec<T>::type{};
-    if (q.h) store_steps<T, NT>(q.h, q, at, zero);
+    for (int r = 0; r < R; ++r) va[r].v = typename S::P::type{};
+    if (q.h) store_steps<T>(q.h, q, at, va);
     return;
   }
-  Vec<T> va[R], vu[R];
-  load_steps<T, NT>(q.a, q.sa_b, q.sa_t, at, va);
-  load_steps<T, NT>(q.u, q.su_b, q.su_t, at, vu);
+  load_steps(q.a, q.sa_b, q.sa_t, at, keep<T, SIG>(), va);
+  load_steps(q.u, q.su_b, q.su_t, at, T(0), vu);
 
+  // SIGMOID: the gate and the gated input; COEFF: a and u stay packed.
   A c[R][V], d[R][V], a[V], h[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) a[i] = A(1), h[i] = A(0);
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const bool live = at.whole || (at.mine + r < at.len);
+  for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      A cc = up(va[r].v[i]), dd = up(vu[r].v[i]);
+      A s = up(va[r].v[i]), x = up(vu[r].v[i]);
       if (SIG) {
-        A s, o;
-        open_gate(gate_of<T>(cc), &s, &o);
-        cc = s;
-        dd = o * dd;
+        A o;
+        gates<T>(s, &s, &o);
+        c[r][i] = s;
+        d[r][i] = x = o * x;
       }
-      c[r][i] = live ? cc : A(1);
-      d[r][i] = live ? dd : A(0);
-      h[i] = fma_(c[r][i], h[i], d[r][i]);
-      a[i] *= c[r][i];
+      h[i] = fma_(s, h[i], x);
+      a[i] *= s;
     }
-  }
-  compose_wave<true>(a, h);
-  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-  const int col = (threadIdx.x % kLanes) * V;
-  if (lane >= 64 - kLanes) {
+  if (!SIG) forget(va), forget(vu);
+  const int wave = threadIdx.x / 64, col = (threadIdx.x & 63) * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) maps.a[wave][col + i] = a[i], maps.h[wave][col + i] = h[i];
-  }
-  exclude_own<true>(a, h);
+  for (int i = 0; i < V; ++i) maps.a[wave][col + i] = a[i], maps.h[wave][col + i] = h[i];
   __syncthreads();
   for (int k = threadIdx.x; k < C; k += NT) {
     A ma, mh;
     compose_waves<true>(maps, k, &ma, &mh);
     const int64_t ch = (int64_t)at.slab * C + k;
     const bool mine = ch < q.D;
-    const bool last = at.t0 + S::span(NT) >= at.len;
-    const int64_t place = ((int64_t)chain * g.spans + at.span) * C + k;
-    A x = A(0);
-    if (!MULTI || at.span == 0) {
-      if (mine && q.h0) x = ((const A*)q.h0)[at.b * q.D + ch];
-    } else {
-      if (mine && !last) MapWords<A>::store(bd.map, place, ma, mh);
-      asm volatile("" ::: "memory");  // published before this wave waits
-      if ((int64_t)at.slab * C + (k & ~63) < q.D)
-        x = enter<A>(bd, place, place - (k & 63), -C, at.span, mine);
+    const bool last = at.t0 + S::kSpan >= at.len;
+    A x = mine && q.h0 ? ((const A*)q.h0)[at.b * q.D + ch] : A(0);
+    if (MULTI) {
+      if (mine && !last) publish(bd, g, chain, at.span, C, k, ma, mh);
+      if (at.span > 0 && (int64_t)at.slab * C + (k & ~63) < q.D)
+        x = enter<A, C>(bd, g, chain, at.span, !last, k, mine, x, ma, mh);
     }
-    const A end = fma_(ma, x, mh);
-    if (MULTI && mine && !last) agent_store((Word<A>*)bd.state + place, word_of(end));
-    if (mine && q.ck) ((A*)q.ck)[(at.b * g.spans + at.span) * q.D + ch] = x;
-    if (mine && last && q.hT) ((A*)q.hT)[at.b * q.D + ch] = end;
+    if (mine && last && q.hT) ((A*)q.hT)[at.b * q.D + ch] = fma_(ma, x, mh);
     start[k] = x;
   }
-  if (!q.h) return;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const A x = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
-    h[i] = fma_(a[i], x, h[i]);
+  for (int i = 0; i < V; ++i)
+    h[i] = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
+  if (q.ck && wave % kCkWaves == 0 && (at.mine < at.len || at.mine == 0)) {
+    A* ck = (A*)q.ck + (at.b * g.cks + at.mine / (kCkWaves * R)) * q.D + at.c0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < at.n) ck[i] = h[i];
   }
+  if (!q.h) return;
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      h[i] = fma_(c[r][i], h[i], d[r][i]);
+      h[i] = SIG ? fma_(c[r][i], h[i], d[r][i]) : fma_(up(va[r].v[i]), h[i], up(vu[r].v[i]));
       va[r].v[i] = down<T>(h[i]);
     }
-  store_steps<T, NT>(q.h, q, at, va);
+  store_steps<T>(q.h, q, at, va);
 }
 
-template <class T, bool SIG, bool MULTI, int NT>
-__global__ __launch_bounds__(NT) void rec_rev(RecArgs q, Grid g, Board bd) {
-  typedef Acc<T> A;
-  typedef Shape<T> S;
-  constexpr int V = S::V, R = S::R, C = S::C, W = NT / 64;
-  __shared__ Maps<A, W, C> maps, rmaps;
+template <class T, bool SIG, bool MULTI, bool STREAM, int NT>
+__global__ __launch_bounds__(NT, 3) void rec_rev(RecArgs q, Grid g, Board bd) {
+  typedef Shape<T, NT, STREAM> S;
+  typedef typename S::A A;
+  constexpr int V = S::V, R = S::R, C = S::C;
+  __shared__ Maps<A, S::W, C> maps, rmaps;
   __shared__ A start[C], finish[C];
-  __shared__ int ticket;
-  const uint32_t chain = blockIdx.x % g.chains;
-  if (MULTI) {
-    if (threadIdx.x == 0) ticket = atomicAdd(bd.next + (int64_t)chain * kCounterInts, 1) + 1;
-    __syncthreads();
-  }
-  const Place<T, NT> at(q, g, chain, MULTI ? g.spans - 1 - ticket : 0);
-  Vec<T> va[R], vu[R], vd[R];
+  const uint32_t chain = chain_of(g);
+  if (chain >= g.chains) return;
+  typename S::P va[R], vu[R], vd[R];
+  const Place<S> at(q, g, chain, MULTI ? g.spans - 1 - take_span(bd, chain) : 0);
   if (at.t0 >= at.len && at.span > 0) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) va[r].v = typename Vec<T>::type{};
-    store_steps<T, NT>(q.da, q, at, va);
-    store_steps<T, NT>(q.du, q, at, va);
+    for (int r = 0; r < R; ++r) va[r].v = typename S::P::type{};
+    store_steps<T>(q.da, q, at, va);
+    store_steps<T>(q.du, q, at, va);
     return;
   }
-  load_steps<T, NT>(q.a, q.sa_b, q.sa_t, at, va);
-  load_steps<T, NT>(q.u, q.su_b, q.su_t, at, vu);
-  load_steps<T, NT>(q.dh, q.sd_b, q.sd_t, at, vd);
+  load_steps(q.a, q.sa_b, q.sa_t, at, keep<T, SIG>(), va);
+  load_steps(q.u, q.su_b, q.su_t, at, T(0), vu);
+  load_steps(q.dh, q.sd_b, q.sd_t, at, T(0), vd);
 
-  // gate[r][i]: the coefficient, or gate_of it. Steps beyond the end keep the
-  // state and the gradient: coefficient 1, input 0.
-  A gate[R][V], a[V], h[V], ra[V], rh[V];
-  constexpr A kKeep = SIG ? A(0) : A(1);
+  // SIGMOID: the gate s and o = 1 - s; COEFF: a stays packed.
+  A s[R][V], o[R][V], a[V], h[V], c[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) a[i] = A(1), h[i] = A(0), rh[i] = A(0);
+  for (int i = 0; i < V; ++i) a[i] = A(1), h[i] = A(0), c[i] = A(0);
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const bool live = at.whole || (at.mine + r < at.len);
+  for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      A cc = up(va[r].v[i]), dd = up(vu[r].v[i]);
-      if (SIG) cc = gate_of<T>(cc);
-      gate[r][i] = live ? cc : kKeep;
-      A s = gate[r][i];
+      A k = up(va[r].v[i]), d = up(vu[r].v[i]);
       if (SIG) {
-        A o;
-        open_gate(gate[r][i], &s, &o);
-        dd = o * dd;
+        gates<T>(k, &s[r][i], &o[r][i]);
+        k = s[r][i];
+        d = o[r][i] * d;
       }
-      h[i] = fma_(s, h[i], dd);
-      a[i] *= s;
+      h[i] = fma_(k, h[i], d);
+      a[i] *= k;
     }
-  }
-  if (SIG) forget(gate);
+  if (!SIG) forget(va);
 #pragma unroll
   for (int r = R - 1; r >= 0; --r)
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      A s = gate[r][i], o;
-      if (SIG) open_gate(gate[r][i], &s, &o);
-      rh[i] = s * (up(vd[r].v[i]) + rh[i]);
-    }
+    for (int i = 0; i < V; ++i)
+      c[i] = (SIG ? s[r][i] : up(va[r].v[i])) * (up(vd[r].v[i]) + c[i]);
+  forget(vu);
+  forget(vd);
+  const int wave = threadIdx.x / 64, col = (threadIdx.x & 63) * V;
 #pragma unroll
-  for (int i = 0; i < V; ++i) ra[i] = a[i];
-  compose_wave<true>(a, h);
-  compose_wave<false>(ra, rh);
-  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-  const int col = (threadIdx.x % kLanes) * V;
-  if (lane >= 64 - kLanes) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) maps.a[wave][col + i] = a[i], maps.h[wave][col + i] = h[i];
+  for (int i = 0; i < V; ++i) {
+    maps.a[wave][col + i] = rmaps.a[wave][col + i] = a[i];
+    maps.h[wave][col + i] = h[i], rmaps.h[wave][col + i] = c[i];
   }
-  if (lane < kLanes) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) rmaps.a[wave][col + i] = ra[i], rmaps.h[wave][col + i] = rh[i];
-  }
-  exclude_own<true>(a, h);
-  exclude_own<false>(ra, rh);
   __syncthreads();
   for (int k = threadIdx.x; k < C; k += NT) {
     A ma, mh;
@@ -520,64 +587,55 @@ __global__ __launch_bounds__(NT) void rec_rev(RecArgs q, Grid g, Board bd) {
     compose_waves<false>(rmaps, k, &ma, &mh);
     const int64_t ch = (int64_t)at.slab * C + k;
     const bool mine = ch < q.D;
-    // the row's last span, where the gradient of the last state enters
-    const int last = at.len > 0 ? (int)((at.len - 1) / S::span(NT)) : 0;
-    const int64_t place = ((int64_t)chain * g.spans + at.span) * C + k;
-    A x = A(0);
-    if (!MULTI || at.span == last) {
-      if (mine && q.dhT) x = ((const A*)q.dhT)[at.b * q.D + ch];
-    } else {
-      if (mine && at.span > 0) MapWords<A>::store(bd.map, place, ma, mh);
-      asm volatile("" ::: "memory");  // published before this wave waits
-      if ((int64_t)at.slab * C + (k & ~63) < q.D)
-        x = enter<A>(bd, place, place - (k & 63), C, last - at.span, mine);
+    // asked for before the wait
+    const A first = mine ? ((const A*)q.ck)[(at.b * g.cks + at.span * S::W / kCkWaves) * q.D + ch] : A(0);
+    // the sweep begins at the row's last span, where dhT enters
+    const int last = at.len > 0 ? (int)((at.len - 1) / S::kSpan) : 0;
+    A x = mine && q.dhT ? ((const A*)q.dhT)[at.b * q.D + ch] : A(0);
+    if (MULTI) {
+      const int e = last - at.span;
+      if (mine && at.span > 0) publish(bd, g, chain, e, C, k, ma, mh);
+      if (e > 0 && (int64_t)at.slab * C + (k & ~63) < q.D)
+        x = enter<A, C>(bd, g, chain, e, at.span > 0, k, mine, x, ma, mh);
     }
-    const A end = fma_(ma, x, mh);
-    if (MULTI && mine && at.span > 0) agent_store((Word<A>*)bd.state + place, word_of(end));
-    if (mine && at.span == 0 && q.dh0) ((A*)q.dh0)[at.b * q.D + ch] = end;
+    if (mine && at.span == 0 && q.dh0) ((A*)q.dh0)[at.b * q.D + ch] = fma_(ma, x, mh);
     finish[k] = x;
-    start[k] = mine ? ((const A*)q.ck)[(at.b * g.spans + at.span) * q.D + ch] : A(0);
+    start[k] = first;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const A x = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
-    h[i] = fma_(a[i], x, h[i]);
-    const A y = fma_(rmaps.a[wave][col + i], finish[col + i], rmaps.h[wave][col + i]);
-    rh[i] = fma_(ra[i], y, rh[i]);
+    h[i] = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
+    c[i] = fma_(rmaps.a[wave][col + i], finish[col + i], rmaps.h[wave][col + i]);
   }
-  if (SIG) forget(gate);
-  // e[r][i]: what G_t is multiplied with in da_t
-  A e[R][V];
+  if (SIG) forget(o);  // what was o * u is not kept
+  else forget(va);
+  A e[R][V];  // what G_t is multiplied with in da_t
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const A x = h[i], u = up(vu[r].v[i]);
       if (SIG) {
-        A s, o;
-        open_gate(gate[r][i], &s, &o);
-        e[r][i] = (x - u) * (s * o);
-        h[i] = fma_(s, x, o * u);
+        e[r][i] = (x - u) * (s[r][i] * o[r][i]);
+        h[i] = fma_(s[r][i], x, o[r][i] * u);
       } else {
         e[r][i] = x;
-        h[i] = fma_(gate[r][i], x, u);
+        h[i] = fma_(up(va[r].v[i]), x, u);
       }
     }
-  if (SIG) forget(gate);
+  if (!SIG) forget(va);
 #pragma unroll
   for (int r = R - 1; r >= 0; --r)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const A G = up(vd[r].v[i]) + rh[i];
-      A s = gate[r][i], o = A(1);
-      if (SIG) open_gate(gate[r][i], &s, &o);
+      const A G = up(vd[r].v[i]) + c[i], k = SIG ? s[r][i] : up(va[r].v[i]);
       va[r].v[i] = down<T>(G * e[r][i]);
-      vu[r].v[i] = down<T>(SIG ? G * o : G);
-      rh[i] = s * G;
+      vu[r].v[i] = down<T>(SIG ? G * o[r][i] : G);
+      c[i] = k * G;
     }
-  store_steps<T, NT>(q.da, q, at, va);
-  store_steps<T, NT>(q.du, q, at, vu);
+  store_steps<T>(q.da, q, at, va);
+  store_steps<T>(q.du, q, at, vu);
 }
 
 // One step of B rows on a pool of states, V channels a thread. Latency bounds
@@ -608,7 +666,7 @@ __global__ __launch_bounds__(kStepThreads) void rec_one(RecStep q, int64_t per_r
       A c = up(a.v[j]), v = up(u.v[j]);
       if (SIG) {
         A s, o;
-        open_gate(gate_of<T>(c), &s, &o);
+        gates<T>(c, &s, &o);
         c = s;
         v = o * v;
       }
@@ -629,30 +687,35 @@ __global__ __launch_bounds__(kFillThreads) void fill_ones(uint4* p, int64_t n) {
 }
 
 // -------------------------------------------------------------- on the host
-int type_steps(int32_t dtype) { return dtype == ADST_BF16 || dtype == ADST_F16 ? 4 : 8; }
 int type_size(int32_t dtype) { return dtype == ADST_F64 ? 8 : dtype == ADST_F32 ? 4 : 2; }
 
-Grid grid_of(int32_t dtype, int64_t B, int64_t T, int64_t D) {
-  const int C = kLanes * 16 / type_size(dtype);
+int type_channels(int32_t dtype) { return dtype == ADST_F64 || dtype == ADST_F32 ? 64 : 128; }
+int wave_steps(int32_t dtype) { return dtype == ADST_F64 ? 8 : 16; }
+
+Grid grid_of(int32_t dtype, int64_t B, int64_t T, int64_t D, bool forward) {
+  const int C = type_channels(dtype), R = wave_steps(dtype);
   Grid g;
   g.slabs = (int)((D + C - 1) / C);
   g.chains = (uint32_t)(B * g.slabs);
-  g.threads = 512;
-  if (T <= 64 / kLanes * type_steps(dtype)) g.threads = 64;
-  g.span = g.threads / kLanes * type_steps(dtype);
+  g.round = (g.chains + 7) / 8 * 8;
+  g.threads = T <= R ? 64 : T <= 2 * R ? 128 : T <= 4 * R ? 256
+              : forward ? kForward : kReverse;
+  g.span = g.threads / 64 * R;
   g.spans = T > 0 ? (int)((T + g.span - 1) / g.span) : 1;
+  g.groups = (g.spans + kGroup - 1) / kGroup;
+  g.cks = T > 0 ? (int)((T + kCkWaves * R - 1) / (kCkWaves * R)) : 1;
   return g;
 }
 
-int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
-
 Board board_of(int32_t dtype, const Grid& g, void* ws, int64_t* bytes) {
-  const int64_t C = kLanes * 16 / type_size(dtype), A = dtype == ADST_F64 ? 8 : 4;
+  const int64_t C = type_channels(dtype), A = dtype == ADST_F64 ? 8 : 4;
   const int64_t counters = (int64_t)g.chains * kCounterInts * 4;
-  const int64_t words = round16((int64_t)g.chains * g.spans * C * A);
+  const int64_t states = (int64_t)g.chains * g.groups * C * A;
+  const int64_t maps = (int64_t)g.chains * g.spans * C * 2 * A;
   char* p = static_cast<char*>(ws);
-  *bytes = g.spans > 1 ? counters + 3 * words : 0;
-  return {reinterpret_cast<int32_t*>(p), p + counters, p + counters + words};
+  *bytes = g.spans > 1 ? counters + 3 * states + maps : 0;
+  return {reinterpret_cast<int32_t*>(p), p + counters, p + counters + states,
+          p + counters + 3 * states};
 }
 
 template <class F>
@@ -665,25 +728,46 @@ void by_type(int32_t dtype, F f) {
   }
 }
 
-template <bool FORWARD, class T, bool SIG, bool MULTI, int NT>
+template <bool FORWARD, class T, bool SIG, bool MULTI, bool STREAM, int NT>
 void launch(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
-  const unsigned blocks = (unsigned)(g.chains * g.spans);
-  if (FORWARD) rec_fwd<T, SIG, MULTI, NT><<<blocks, NT, 0, st>>>(q, g, bd);
-  else rec_rev<T, SIG, MULTI, NT><<<blocks, NT, 0, st>>>(q, g, bd);
+  const unsigned blocks = g.round * (unsigned)g.spans;
+  if constexpr (FORWARD) rec_fwd<T, SIG, MULTI, STREAM, NT><<<blocks, NT, 0, st>>>(q, g, bd);
+  else rec_rev<T, SIG, MULTI, STREAM, NT><<<blocks, NT, 0, st>>>(q, g, bd);
 }
+
+// Non-temporal loads and stores for calls that move more than the caches keep,
+// on arrays whose rows are whole cache lines.
+constexpr int64_t kStreamBytes = int64_t(128) << 20, kLine = 128;
+bool streams(const RecArgs& q, bool forward) {
+  const int64_t e = type_size(q.dtype);
+  int64_t off = q.D * e | q.sa_b * e | q.sa_t * e | q.su_b * e | q.su_t * e;
+  off |= (int64_t)(uintptr_t)q.a | (int64_t)(uintptr_t)q.u;
+  if (forward) off |= (int64_t)(uintptr_t)q.h;
+  else off |= q.sd_b * e | q.sd_t * e | (int64_t)(uintptr_t)q.dh | (int64_t)(uintptr_t)q.da |
+              (int64_t)(uintptr_t)q.du;
+  return off % kLine == 0 && q.B * q.T * q.D * e * (forward ? 3 : 5) >= kStreamBytes;
+}
+
 template <bool FORWARD, class T, bool SIG>
 void by_grid(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
-  if (g.threads == 64)
-    launch<FORWARD, T, SIG, false, 64>(q, g, bd, st);
-  else if (g.spans == 1)
-    launch<FORWARD, T, SIG, false, 512>(q, g, bd, st);
-  else
-    launch<FORWARD, T, SIG, true, 512>(q, g, bd, st);
+  constexpr int kLong = FORWARD ? kForward : kReverse;
+  if (g.spans > 1)
+    streams(q, FORWARD) ? launch<FORWARD, T, SIG, true, true, kLong>(q, g, bd, st)
+                        : launch<FORWARD, T, SIG, true, false, kLong>(q, g, bd, st);
+  else if (g.threads == 64)
+    launch<FORWARD, T, SIG, false, false, 64>(q, g, bd, st);
+  else if (g.threads == 128)
+    launch<FORWARD, T, SIG, false, false, 128>(q, g, bd, st);
+  else if (g.threads == 256)
+    streams(q, FORWARD) ? launch<FORWARD, T, SIG, false, true, 256>(q, g, bd, st)
+                        : launch<FORWARD, T, SIG, false, false, 256>(q, g, bd, st);
+  else if constexpr (kLong > 256)
+    launch<FORWARD, T, SIG, false, false, kLong>(q, g, bd, st);
 }
 
 template <bool FORWARD>
 hipError_t sweep(const RecArgs& q, void* ws, hipStream_t st) {
-  const Grid g = grid_of(q.dtype, q.B, q.T, q.D);
+  const Grid g = grid_of(q.dtype, q.B, q.T, q.D, FORWARD);
   int64_t bytes;
   const Board bd = board_of(q.dtype, g, ws, &bytes);
   if (bytes) {
@@ -704,18 +788,22 @@ hipError_t sweep(const RecArgs& q, void* ws, hipStream_t st) {
 }  // namespace
 
 RecPlan rec_plan(int32_t dtype, int64_t B, int64_t T, int64_t D) {
-  const Grid g = grid_of(dtype, B, T, D);
   RecPlan p;
-  p.span = g.span;
-  p.spans = g.spans;
-  p.ck_bytes = (uint64_t)(B * D * g.spans) * (dtype == ADST_F64 ? 8 : 4);
-  int64_t bytes;
-  board_of(dtype, g, nullptr, &bytes);
-  p.ws_bytes = (uint64_t)bytes;
-  // work-items of a launch, and of the step's, in the 32-bit dispatch grid
+  p.ws_bytes = 0;
+  p.fits = true;
+  for (int forward = 0; forward < 2; ++forward) {
+    const Grid g = grid_of(dtype, B, T, D, forward);
+    int64_t bytes;
+    board_of(dtype, g, nullptr, &bytes);
+    if ((uint64_t)bytes > p.ws_bytes) p.ws_bytes = (uint64_t)bytes;
+    // a launch's work-items in the 32-bit dispatch grid
+    p.fits = p.fits && ((double)B * g.slabs + 7) * g.spans * g.threads < 4294967296.0 &&
+             bytes / 16 < (int64_t(1) << 32) - 256;
+    p.span = kCkWaves * wave_steps(dtype);
+    p.ck_bytes = (uint64_t)(B * D * g.cks) * (dtype == ADST_F64 ? 8 : 4);
+  }
   const int64_t per_row = (D + 16 / type_size(dtype) - 1) / (16 / type_size(dtype));
-  p.fits = (double)B * g.slabs * g.spans * g.threads < 4294967296.0 &&
-           (double)B * per_row < 4294967296.0 - 64 && bytes / 16 < (int64_t(1) << 32) - 256;
+  p.fits = p.fits && (double)B * per_row < 4294967296.0 - 64;  // the step's
   return p;
 }
 

@@ -22,7 +22,7 @@ struct RecArgs {
   // forward
   void* h;
   void* hT;
-  void* ck;  // [B][spans][D] accumulation type
+  void* ck;  // [B][checkpoints][D] accumulation type
   // reverse (ck: read)
   const void* dh;
   const void* dhT;
@@ -33,9 +33,8 @@ struct RecArgs {
 };
 
 struct RecPlan {
-  int64_t span;   // steps between checkpoints
-  int64_t spans;  // per batch row, at least 1
-  bool fits;      // the launches hold that many
+  int64_t span;  // steps between checkpoints
+  bool fits;     // the launches hold the problem
   uint64_t ck_bytes, ws_bytes;
 };
 RecPlan rec_plan(int32_t dtype, int64_t B, int64_t T, int64_t D);

@@ -70,17 +70,19 @@ __device__ inline void store_pack(T* p, Pack<T, V> x, int n) {
     if (i < n) p[i] = x.v[i];
 }
 
-// A workgroup of NT threads: a wave's lanes lie along channels, V of them a
-// lane; each wave holds R consecutive steps.
-template <class T, int NT_, bool STREAM_>
+// A workgroup of NT threads: L lanes of a wave lie along channels, V of them a
+// lane, and its 64 / L rows of lanes along time, R consecutive steps each.
+template <class T, int NT_, int L_, bool STREAM_>
 struct Shape {
   typedef Acc<T> A;
   static constexpr bool STREAM = STREAM_;
   static constexpr int V = sizeof(T) == 2 ? 2 : 1;
   static constexpr int R = sizeof(T) == 8 ? 8 : 16;
   static constexpr int W = NT_ / 64;
-  static constexpr int C = 64 * V;      // channels of a workgroup
-  static constexpr int kSpan = W * R;   // its steps
+  static constexpr int L = L_;
+  static constexpr int C = L * V;                // channels of a workgroup
+  static constexpr int kWaveSteps = 64 / L * R;
+  static constexpr int kSpan = W * kWaveSteps;   // a workgroup's steps
   typedef Pack<T, V> P;
 };
 constexpr int kForward = 512, kReverse = 256;  // threads of a workgroup on long rows
@@ -92,7 +94,10 @@ struct Grid {
   int span;    // steps
   int spans;   // per batch row
   int groups;  // of spans
-  int slabs;   // of C channels
+  int lanes;   // along channels
+  int C;       // channels of a slab
+  int slabs;   // of a batch row
+  int ck;      // steps between checkpoints
   int cks;     // checkpoints of a batch row
   uint32_t chains;  // batch rows times slabs
   uint32_t round;   // chains, to a multiple of 8: the workgroups of one span of each
@@ -170,6 +175,74 @@ __device__ inline int64_t row_length(const int32_t* lens, int64_t b, int64_t T) 
 }
 
 // ------------------------------------------------------- maps along the time
+// Rows of 16 lanes exchange values: in every lane the value of its pair's even
+// (lower) row and of the odd (upper) one, or of the wave's lower and upper
+// half. Vector instructions, which do without LDS.
+template <bool HALVES>
+__device__ inline void exchange(uint32_t x, uint32_t* lower, uint32_t* upper) {
+  const auto r = HALVES ? __builtin_amdgcn_permlane32_swap(x, x, false, false)
+                        : __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  *lower = r[0];
+  *upper = r[1];
+}
+template <bool HALVES>
+__device__ inline void exchange(float x, float* lower, float* upper) {
+  uint32_t a, b;
+  exchange<HALVES>(__builtin_bit_cast(uint32_t, x), &a, &b);
+  *lower = __builtin_bit_cast(float, a);
+  *upper = __builtin_bit_cast(float, b);
+}
+template <bool HALVES>
+__device__ inline void exchange(double x, double* lower, double* upper) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, x);
+  uint32_t a0, b0, a1, b1;
+  exchange<HALVES>((uint32_t)w, &a0, &b0);
+  exchange<HALVES>((uint32_t)(w >> 32), &a1, &b1);
+  *lower = __builtin_bit_cast(double, (uint64_t)a1 << 32 | a0);
+  *upper = __builtin_bit_cast(double, (uint64_t)b1 << 32 | b0);
+}
+
+// From a row's map (a, h) the one of the rows before it in the wave, and the
+// wave's.
+template <class A>
+__device__ inline void compose_rows(A& a, A& h, A* wave_a, A* wave_h) {
+  const int lane = threadIdx.x & 63;
+  const bool odd = lane & 16, high = lane & 32;
+  A ea, oa, eh, oh, la, ua, lh, uh;
+  exchange<false>(a, &ea, &oa);
+  exchange<false>(h, &eh, &oh);
+  exchange<true>(oa * ea, &la, &ua);
+  exchange<true>(fma_(oa, eh, oh), &lh, &uh);
+  *wave_a = ua * la;
+  *wave_h = fma_(ua, lh, uh);
+  const A xa = odd ? ea : A(1), xh = odd ? eh : A(0);
+  a = high ? xa * la : xa;
+  h = high ? fma_(xa, lh, xh) : xh;
+}
+// The same, and against the time: from (a, c) the map of the rows after it.
+template <class A>
+__device__ inline void compose_rows_both(A a, A& h, A& c, A* before_a, A* after_a, A* wave_a,
+                                         A* wave_h, A* wave_c) {
+  const int lane = threadIdx.x & 63;
+  const bool odd = lane & 16, high = lane & 32;
+  A ea, oa, eh, oh, ec, oc, la, ua, lh, uh, lc, uc;
+  exchange<false>(a, &ea, &oa);
+  exchange<false>(h, &eh, &oh);
+  exchange<false>(c, &ec, &oc);
+  exchange<true>(oa * ea, &la, &ua);
+  exchange<true>(fma_(oa, eh, oh), &lh, &uh);
+  exchange<true>(fma_(ea, oc, ec), &lc, &uc);
+  *wave_a = ua * la;
+  *wave_h = fma_(ua, lh, uh);
+  *wave_c = fma_(la, uc, lc);
+  const A xa = odd ? ea : A(1), xh = odd ? eh : A(0);
+  *before_a = high ? xa * la : xa;
+  h = high ? fma_(xa, lh, xh) : xh;
+  const A ya = odd ? A(1) : oa, yc = odd ? A(0) : oc;
+  *after_a = high ? ya : ya * ua;
+  c = high ? yc : fma_(ya, uc, yc);
+}
+
 // Per wave and channel, in LDS: first each wave's map, then the composition of
 // the waves before (after) it.
 template <class A, int W, int C>
@@ -389,8 +462,8 @@ struct Place {
     slab = (int)(chain % (uint32_t)g.slabs);
     len = row_length(r.lens, b, r.T);
     t0 = (int64_t)span * S::kSpan;
-    mine = t0 + threadIdx.x / 64 * S::R;
-    c0 = slab * S::C + (int)(threadIdx.x & 63) * S::V;
+    mine = t0 + threadIdx.x / S::L * S::R;
+    c0 = slab * S::C + (int)(threadIdx.x % S::L) * S::V;
     const int64_t left = r.D - c0;
     n = left < 0 ? 0 : left < S::V ? (int)left : S::V;
     whole = (int64_t)(slab + 1) * S::C <= r.D && t0 + S::kSpan <= len;
@@ -448,9 +521,9 @@ __device__ inline int take_span(const Board& bd, uint32_t chain) {
   return ticket;
 }
 
-template <class T, bool SIG, bool MULTI, bool STREAM, int NT>
+template <class T, bool SIG, bool MULTI, bool STREAM, int NT, int L>
 __global__ __launch_bounds__(NT, 4) void rec_fwd(RecArgs q, Grid g, Board bd) {
-  typedef Shape<T, NT, STREAM> S;
+  typedef Shape<T, NT, L, STREAM> S;
   typedef typename S::A A;
   constexpr int V = S::V, R = S::R, C = S::C;
   __shared__ Maps<A, S::W, C> maps;
@@ -487,15 +560,19 @@ __global__ __launch_bounds__(NT, 4) void rec_fwd(RecArgs q, Grid g, Board bd) {
       a[i] *= s;
     }
   if (!SIG) forget(va), forget(vu);
-  const int wave = threadIdx.x / 64, col = (threadIdx.x & 63) * V;
+  const int wave = threadIdx.x / 64, col = threadIdx.x % L * V;
 #pragma unroll
-  for (int i = 0; i < V; ++i) maps.a[wave][col + i] = a[i], maps.h[wave][col + i] = h[i];
+  for (int i = 0; i < V; ++i) {
+    A wa = a[i], wh = h[i];
+    if (L < 64) compose_rows(a[i], h[i], &wa, &wh);
+    if (L == 64 || (threadIdx.x & 63) < L) maps.a[wave][col + i] = wa, maps.h[wave][col + i] = wh;
+  }
   __syncthreads();
-  for (int k = threadIdx.x; k < C; k += NT) {
-    A ma, mh;
-    compose_waves<true>(maps, k, &ma, &mh);
+  for (int k = threadIdx.x; k < (C + 63) / 64 * 64; k += NT) {  // whole waves
+    A ma = A(1), mh = A(0);
+    if (k < C) compose_waves<true>(maps, k, &ma, &mh);
     const int64_t ch = (int64_t)at.slab * C + k;
-    const bool mine = ch < q.D;
+    const bool mine = k < C && ch < q.D;
     const bool last = at.t0 + S::kSpan >= at.len;
     A x = mine && q.h0 ? ((const A*)q.h0)[at.b * q.D + ch] : A(0);
     if (MULTI) {
@@ -504,14 +581,17 @@ __global__ __launch_bounds__(NT, 4) void rec_fwd(RecArgs q, Grid g, Board bd) {
         x = enter<A, C>(bd, g, chain, at.span, !last, k, mine, x, ma, mh);
     }
     if (mine && last && q.hT) ((A*)q.hT)[at.b * q.D + ch] = fma_(ma, x, mh);
-    start[k] = x;
+    if (k < C) start[k] = x;
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < V; ++i)
-    h[i] = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
-  if (q.ck && wave % kCkWaves == 0 && (at.mine < at.len || at.mine == 0)) {
-    A* ck = (A*)q.ck + (at.b * g.cks + at.mine / (kCkWaves * R)) * q.D + at.c0;
+  for (int i = 0; i < V; ++i) {
+    const A x = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
+    h[i] = L == 64 ? x : fma_(a[i], x, h[i]);
+  }
+  if (q.ck && wave % kCkWaves == 0 && (threadIdx.x & 63) < L &&
+      (at.mine < at.len || at.mine == 0)) {
+    A* ck = (A*)q.ck + (at.b * g.cks + at.mine / (kCkWaves * S::kWaveSteps)) * q.D + at.c0;
 #pragma unroll
     for (int i = 0; i < V; ++i)
       if (i < at.n) ck[i] = h[i];
@@ -527,9 +607,9 @@ __global__ __launch_bounds__(NT, 4) void rec_fwd(RecArgs q, Grid g, Board bd) {
   store_steps<T>(q.h, q, at, va);
 }
 
-template <class T, bool SIG, bool MULTI, bool STREAM, int NT>
+template <class T, bool SIG, bool MULTI, bool STREAM, int NT, int L>
 __global__ __launch_bounds__(NT, 3) void rec_rev(RecArgs q, Grid g, Board bd) {
-  typedef Shape<T, NT, STREAM> S;
+  typedef Shape<T, NT, L, STREAM> S;
   typedef typename S::A A;
   constexpr int V = S::V, R = S::R, C = S::C;
   __shared__ Maps<A, S::W, C> maps, rmaps;
@@ -574,19 +654,26 @@ __global__ __launch_bounds__(NT, 3) void rec_rev(RecArgs q, Grid g, Board bd) {
       c[i] = (SIG ? s[r][i] : up(va[r].v[i])) * (up(vd[r].v[i]) + c[i]);
   forget(vu);
   forget(vd);
-  const int wave = threadIdx.x / 64, col = (threadIdx.x & 63) * V;
+  const int wave = threadIdx.x / 64, col = threadIdx.x % L * V;
+  A ra[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    maps.a[wave][col + i] = rmaps.a[wave][col + i] = a[i];
-    maps.h[wave][col + i] = h[i], rmaps.h[wave][col + i] = c[i];
+    A wa = a[i], wh = h[i], wc = c[i];
+    if (L < 64) compose_rows_both(a[i], h[i], c[i], &a[i], &ra[i], &wa, &wh, &wc);
+    if (L == 64 || (threadIdx.x & 63) < L) {
+      maps.a[wave][col + i] = rmaps.a[wave][col + i] = wa;
+      maps.h[wave][col + i] = wh, rmaps.h[wave][col + i] = wc;
+    }
   }
   __syncthreads();
-  for (int k = threadIdx.x; k < C; k += NT) {
-    A ma, mh;
-    compose_waves<true>(maps, k, &ma, &mh);
-    compose_waves<false>(rmaps, k, &ma, &mh);
+  for (int k = threadIdx.x; k < (C + 63) / 64 * 64; k += NT) {  // whole waves
+    A ma = A(1), mh = A(0);
+    if (k < C) {
+      compose_waves<true>(maps, k, &ma, &mh);
+      compose_waves<false>(rmaps, k, &ma, &mh);
+    }
     const int64_t ch = (int64_t)at.slab * C + k;
-    const bool mine = ch < q.D;
+    const bool mine = k < C && ch < q.D;
     // asked for before the wait
     const A first = mine ? ((const A*)q.ck)[(at.b * g.cks + at.span * S::W / kCkWaves) * q.D + ch] : A(0);
     // the sweep begins at the row's last span, where dhT enters
@@ -599,14 +686,15 @@ __global__ __launch_bounds__(NT, 3) void rec_rev(RecArgs q, Grid g, Board bd) {
         x = enter<A, C>(bd, g, chain, e, at.span > 0, k, mine, x, ma, mh);
     }
     if (mine && at.span == 0 && q.dh0) ((A*)q.dh0)[at.b * q.D + ch] = fma_(ma, x, mh);
-    finish[k] = x;
-    start[k] = first;
+    if (k < C) finish[k] = x, start[k] = first;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    h[i] = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
-    c[i] = fma_(rmaps.a[wave][col + i], finish[col + i], rmaps.h[wave][col + i]);
+    const A x = fma_(maps.a[wave][col + i], start[col + i], maps.h[wave][col + i]);
+    const A y = fma_(rmaps.a[wave][col + i], finish[col + i], rmaps.h[wave][col + i]);
+    h[i] = L == 64 ? x : fma_(a[i], x, h[i]);
+    c[i] = L == 64 ? y : fma_(ra[i], y, c[i]);
   }
   if (SIG) forget(o);  // what was o * u is not kept
   else forget(va);
@@ -689,26 +777,35 @@ __global__ __launch_bounds__(kFillThreads) void fill_ones(uint4* p, int64_t n) {
 // -------------------------------------------------------------- on the host
 int type_size(int32_t dtype) { return dtype == ADST_F64 ? 8 : dtype == ADST_F32 ? 4 : 2; }
 
-int type_channels(int32_t dtype) { return dtype == ADST_F64 || dtype == ADST_F32 ? 64 : 128; }
-int wave_steps(int32_t dtype) { return dtype == ADST_F64 ? 8 : 16; }
+int lane_channels(int32_t dtype) { return dtype == ADST_F64 || dtype == ADST_F32 ? 1 : 2; }
+int lane_steps(int32_t dtype) { return dtype == ADST_F64 ? 8 : 16; }
+
+// Lanes along channels: all 64 where that leaves few without one, else 16.
+int lanes_of(int32_t dtype, int64_t D) {
+  const int64_t C = 64 * lane_channels(dtype), all = (D + C - 1) / C * C;
+  return 4 * (all - D) <= all ? 64 : 16;
+}
 
 Grid grid_of(int32_t dtype, int64_t B, int64_t T, int64_t D, bool forward) {
-  const int C = type_channels(dtype), R = wave_steps(dtype);
   Grid g;
-  g.slabs = (int)((D + C - 1) / C);
+  g.lanes = lanes_of(dtype, D);
+  g.C = g.lanes * lane_channels(dtype);
+  const int wave = 64 / g.lanes * lane_steps(dtype);  // its steps
+  g.slabs = (int)((D + g.C - 1) / g.C);
   g.chains = (uint32_t)(B * g.slabs);
   g.round = (g.chains + 7) / 8 * 8;
-  g.threads = T <= R ? 64 : T <= 2 * R ? 128 : T <= 4 * R ? 256
+  g.threads = T <= wave ? 64 : T <= 2 * wave ? 128 : T <= 4 * wave ? 256
               : forward ? kForward : kReverse;
-  g.span = g.threads / 64 * R;
+  g.span = g.threads / 64 * wave;
   g.spans = T > 0 ? (int)((T + g.span - 1) / g.span) : 1;
   g.groups = (g.spans + kGroup - 1) / kGroup;
-  g.cks = T > 0 ? (int)((T + kCkWaves * R - 1) / (kCkWaves * R)) : 1;
+  g.ck = kCkWaves * wave;
+  g.cks = T > 0 ? (int)((T + g.ck - 1) / g.ck) : 1;
   return g;
 }
 
 Board board_of(int32_t dtype, const Grid& g, void* ws, int64_t* bytes) {
-  const int64_t C = type_channels(dtype), A = dtype == ADST_F64 ? 8 : 4;
+  const int64_t C = g.C, A = dtype == ADST_F64 ? 8 : 4;
   const int64_t counters = (int64_t)g.chains * kCounterInts * 4;
   const int64_t states = (int64_t)g.chains * g.groups * C * A;
   const int64_t maps = (int64_t)g.chains * g.spans * C * 2 * A;
@@ -728,11 +825,11 @@ void by_type(int32_t dtype, F f) {
   }
 }
 
-template <bool FORWARD, class T, bool SIG, bool MULTI, bool STREAM, int NT>
+template <bool FORWARD, class T, bool SIG, bool MULTI, bool STREAM, int NT, int L>
 void launch(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
   const unsigned blocks = g.round * (unsigned)g.spans;
-  if constexpr (FORWARD) rec_fwd<T, SIG, MULTI, STREAM, NT><<<blocks, NT, 0, st>>>(q, g, bd);
-  else rec_rev<T, SIG, MULTI, STREAM, NT><<<blocks, NT, 0, st>>>(q, g, bd);
+  if constexpr (FORWARD) rec_fwd<T, SIG, MULTI, STREAM, NT, L><<<blocks, NT, 0, st>>>(q, g, bd);
+  else rec_rev<T, SIG, MULTI, STREAM, NT, L><<<blocks, NT, 0, st>>>(q, g, bd);
 }
 
 // Non-temporal loads and stores for calls that move more than the caches keep,
@@ -748,21 +845,32 @@ bool streams(const RecArgs& q, bool forward) {
   return off % kLine == 0 && q.B * q.T * q.D * e * (forward ? 3 : 5) >= kStreamBytes;
 }
 
-template <bool FORWARD, class T, bool SIG>
-void by_grid(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
+template <bool FORWARD, class T, bool SIG, int L>
+void by_threads(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
   constexpr int kLong = FORWARD ? kForward : kReverse;
   if (g.spans > 1)
-    streams(q, FORWARD) ? launch<FORWARD, T, SIG, true, true, kLong>(q, g, bd, st)
-                        : launch<FORWARD, T, SIG, true, false, kLong>(q, g, bd, st);
+    launch<FORWARD, T, SIG, true, false, kLong, L>(q, g, bd, st);
   else if (g.threads == 64)
-    launch<FORWARD, T, SIG, false, false, 64>(q, g, bd, st);
+    launch<FORWARD, T, SIG, false, false, 64, L>(q, g, bd, st);
   else if (g.threads == 128)
-    launch<FORWARD, T, SIG, false, false, 128>(q, g, bd, st);
+    launch<FORWARD, T, SIG, false, false, 128, L>(q, g, bd, st);
   else if (g.threads == 256)
-    streams(q, FORWARD) ? launch<FORWARD, T, SIG, false, true, 256>(q, g, bd, st)
-                        : launch<FORWARD, T, SIG, false, false, 256>(q, g, bd, st);
+    launch<FORWARD, T, SIG, false, false, 256, L>(q, g, bd, st);
   else if constexpr (kLong > 256)
-    launch<FORWARD, T, SIG, false, false, kLong>(q, g, bd, st);
+    launch<FORWARD, T, SIG, false, false, kLong, L>(q, g, bd, st);
+}
+template <bool FORWARD, class T, bool SIG>
+void by_grid(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
+  if (g.lanes == 16)
+    by_threads<FORWARD, T, SIG, 16>(q, g, bd, st);
+  else if (!streams(q, FORWARD) || g.threads < 256)
+    by_threads<FORWARD, T, SIG, 64>(q, g, bd, st);
+  else if (g.spans > 1)
+    launch<FORWARD, T, SIG, true, true, FORWARD ? kForward : kReverse, 64>(q, g, bd, st);
+  else if (g.threads == 256)
+    launch<FORWARD, T, SIG, false, true, 256, 64>(q, g, bd, st);
+  else if constexpr (FORWARD)
+    launch<FORWARD, T, SIG, false, true, kForward, 64>(q, g, bd, st);
 }
 
 template <bool FORWARD>
@@ -799,7 +907,7 @@ RecPlan rec_plan(int32_t dtype, int64_t B, int64_t T, int64_t D) {
     // a launch's work-items in the 32-bit dispatch grid
     p.fits = p.fits && ((double)B * g.slabs + 7) * g.spans * g.threads < 4294967296.0 &&
              bytes / 16 < (int64_t(1) << 32) - 256;
-    p.span = kCkWaves * wave_steps(dtype);
+    p.span = g.ck;
     p.ck_bytes = (uint64_t)(B * D * g.cks) * (dtype == ADST_F64 ? 8 : 4);
   }
   const int64_t per_row = (D + 16 / type_size(dtype) - 1) / (16 / type_size(dtype));

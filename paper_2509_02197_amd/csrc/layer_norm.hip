@@ -1,4 +1,17 @@
 // Layer norm over rows, its VJP, and the weights' gradients summed over rows.
+//
+// The forward reads x and writes y, the VJP reads x and dy and writes dx:
+// HBM bandwidth bounds both. A row is held in the registers of a group of
+// lanes, so that its mean, its spread about that mean (two passes, which lose
+// nothing to a large mean) and its result need one read: 16 or 64 lanes of a
+// wave, or the waves of a workgroup that join their sums through LDS. A group
+// takes R rows at a time, to have their reads under way together and to wait
+// once for their sums. The weights stay in registers over all of a
+// workgroup's rows, and so do, in the VJP, the sums of dw and db of the
+// group's columns; each workgroup writes its sums once, and a second kernel
+// adds those of all workgroups. Their number, and so the order of all sums,
+// depends on the sizes alone. Rows longer than the registers hold are read
+// again for each pass (norm_fwd_long, norm_rev_long), from the caches mostly.
 
 #include "seq_common.h"
 #include "seq_kernels.h"
@@ -6,103 +19,407 @@
 namespace adst {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kParts = 256;  // row groups of the weights' gradients
-
-template <class A>
-__device__ inline A block_sum(A v) {
-  __shared__ A part[kThreads / 64];
-  v = lane_sum<64>(v);
-  __syncthreads();  // earlier sums are read
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (part[0] + part[1]) + (part[2] + part[3]);
-}
-
 __device__ inline float sqrt_(float x) { return __builtin_sqrtf(x); }
 __device__ inline double sqrt_(double x) { return __builtin_sqrt(x); }
 
-template <class T, class W>
-__global__ __launch_bounds__(kThreads) void norm_fwd(NormArgs p) {
+// N values of W, at any element's address.
+template <class W, int N>
+struct Pack {
+  typedef W type __attribute__((ext_vector_type(N)));
+  typedef W unaligned __attribute__((ext_vector_type(N), aligned(sizeof(W))));
+  type v;
+};
+template <class W, int N>
+__device__ inline Pack<W, N> load_pack(const W* p, int n, W none) {
+  Pack<W, N> r;
+  if (p && n >= N) {
+    r.v = *reinterpret_cast<const typename Pack<W, N>::unaligned*>(p);
+    return r;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.v[i] = p && i < n ? p[i] : none;
+  return r;
+}
+
+// A workgroup of NT threads in groups of L lanes; a lane holds K vectors of
+// each of R rows.
+template <class T, int NT_, int L_, int K_, int R_>
+struct Shape {
   typedef Acc<T> A;
-  const int64_t row = blockIdx.x;
-  const T* x = (const T*)p.x + row * p.sx;
-  T* y = (T*)p.y + row * p.n;
-  A s = 0;
-  for (int64_t i = threadIdx.x; i < p.n; i += kThreads) s += up(x[i]);
-  const A mean = block_sum(s) / A(p.n);
-  s = 0;
-  for (int64_t i = threadIdx.x; i < p.n; i += kThreads) {
-    const A d = up(x[i]) - mean;
-    s = fma_(d, d, s);
-  }
-  const A rstd = A(1) / sqrt_(block_sum(s) / A(p.n) + A(p.eps));
-  for (int64_t i = threadIdx.x; i < p.n; i += kThreads) {
-    const A w = p.w ? (A)up(((const W*)p.w)[i]) : A(1), b = p.b ? (A)up(((const W*)p.b)[i]) : A(0);
-    y[i] = down<T>(fma_((up(x[i]) - mean) * rstd, w, b));
-  }
-  if (threadIdx.x == 0) {
-    if (p.mean) ((A*)p.mean)[row] = mean;
-    if (p.rstd) ((A*)p.rstd)[row] = rstd;
+  static constexpr int NT = NT_, L = L_, K = K_, R = R_;
+  static constexpr int V = Vec<T>::N;
+  static constexpr int G = NT / L;             // groups
+  static constexpr int W = L > 64 ? L / 64 : 1;  // waves of a group
+  static constexpr int kRows = G * R;          // rows of a workgroup at a time
+};
+
+// Sums over a group, of R values each, in every lane. Calls alternate between
+// two buffers, so that one barrier a call is enough.
+template <class S>
+struct Sums {
+  typename S::A part[2][S::G][S::W][S::R];
+};
+template <class S, int N>
+__device__ inline void group_sum(Sums<S>& sm, int& turn, typename S::A (&v)[N]) {
+  static_assert(N <= S::R, "");
+#pragma unroll
+  for (int r = 0; r < N; ++r) v[r] = lane_sum<(S::L < 64 ? S::L : 64)>(v[r]);
+  if constexpr (S::W > 1) {
+    const int g = threadIdx.x / S::L, w = threadIdx.x % S::L / 64;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int r = 0; r < N; ++r) sm.part[turn][g][w][r] = v[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      v[r] = sm.part[turn][g][0][r];
+#pragma unroll
+      for (int k = 1; k < S::W; ++k) v[r] += sm.part[turn][g][k][r];
+    }
+    turn ^= 1;
   }
 }
 
-template <class T, class W>
-__global__ __launch_bounds__(kThreads) void norm_dx(NormArgs p) {
-  typedef Acc<T> A;
-  const int64_t row = blockIdx.x;
-  const T* x = (const T*)p.x + row * p.sx;
-  const T* dy = (const T*)p.dy + row * p.sdy;
-  T* dx = (T*)p.dx + row * p.n;
-  const A mean = ((const A*)p.mean)[row], rstd = ((const A*)p.rstd)[row];
-  A s = 0, q = 0;
-  for (int64_t i = threadIdx.x; i < p.n; i += kThreads) {
-    const A w = p.w ? (A)up(((const W*)p.w)[i]) : A(1);
-    const A e = up(dy[i]) * w;
-    s += e;
-    q = fma_(e, (up(x[i]) - mean) * rstd, q);
+template <class T, class W, int NT, int L, int K, int R_>
+__global__ __launch_bounds__(NT) void norm_fwd(NormArgs p) {
+  typedef Shape<T, NT, L, K, R_> S;
+  typedef typename S::A A;
+  constexpr int V = S::V, R = S::R;
+  __shared__ Sums<S> sm;
+  int turn = 0;
+  const int lane = threadIdx.x % L, group = threadIdx.x / L;
+  int n[K];  // columns of each of this lane's vectors
+  Pack<W, V> w[K], b[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int64_t c = (int64_t)(k * L + lane) * V;
+    n[k] = (int)min((int64_t)V, p.n - c);
+    w[k] = load_pack<W, V>(p.w ? (const W*)p.w + c : nullptr, n[k], W(1));
+    b[k] = load_pack<W, V>(p.b ? (const W*)p.b + c : nullptr, n[k], W(0));
   }
-  s = block_sum(s) / A(p.n);
-  q = block_sum(q) / A(p.n);
-  for (int64_t i = threadIdx.x; i < p.n; i += kThreads) {
-    const A w = p.w ? (A)up(((const W*)p.w)[i]) : A(1);
-    const A e = up(dy[i]) * w;
-    dx[i] = down<T>(fma_(-q, (up(x[i]) - mean) * rstd, e - s) * rstd);
+  const A inv = A(1) / A(p.n);
+  for (int64_t row0 = (int64_t)blockIdx.x * S::kRows; row0 < p.rows;
+       row0 += (int64_t)gridDim.x * S::kRows) {
+    const int64_t row = row0 + group * R;
+    Vec<T> x[R][K];
+    A s[R], mean[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        x[r][k].v = typename Vec<T>::type{};
+        if (row + r < p.rows && n[k] > 0)
+          x[r][k] = load_part((const T*)p.x + (row + r) * p.sx + (k * L + lane) * V, n[k]);
+      }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      s[r] = A(0);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[r] += up(x[r][k].v[i]);
+    }
+    group_sum<S>(sm, turn, s);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mean[r] = s[r] * inv;
+      s[r] = A(0);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const A d = i < n[k] ? up(x[r][k].v[i]) - mean[r] : A(0);
+          s[r] = fma_(d, d, s[r]);
+        }
+    }
+    group_sum<S>(sm, turn, s);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= p.rows) continue;
+      const A rstd = A(1) / sqrt_(s[r] * inv + A(p.eps));
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (n[k] <= 0) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          x[r][k].v[i] = down<T>(fma_((up(x[r][k].v[i]) - mean[r]) * rstd, (A)up(w[k].v[i]),
+                                      (A)up(b[k].v[i])));
+        store_part((T*)p.y + (row + r) * p.n + (k * L + lane) * V, x[r][k], n[k]);
+      }
+      if (lane == 0) {
+        if (p.mean) ((A*)p.mean)[row + r] = mean[r];
+        if (p.rstd) ((A*)p.rstd)[row + r] = rstd;
+      }
+    }
   }
 }
 
-// Partial sums of dw and db of rows blockIdx.y, + kParts, ..., one column a thread.
+// dx, and where part is given this workgroup's sums of dw and db in
+// part[blockIdx.x][2][n].
+template <class T, class W, int NT, int L, int K, int R_>
+__global__ __launch_bounds__(NT) void norm_rev(NormArgs p, Acc<T>* part) {
+  typedef Shape<T, NT, L, K, R_> S;
+  typedef typename S::A A;
+  constexpr int V = S::V, R = S::R;
+  __shared__ Sums<S> sm;
+  __shared__ Sums<S> sm2;
+  int turn = 0, turn2 = 0;
+  const int lane = threadIdx.x % L, group = threadIdx.x / L;
+  int n[K];
+  Pack<W, V> w[K];
+  A dw[K][V], db[K][V];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int64_t c = (int64_t)(k * L + lane) * V;
+    n[k] = (int)min((int64_t)V, p.n - c);
+    w[k] = load_pack<W, V>(p.w ? (const W*)p.w + c : nullptr, n[k], W(1));
+#pragma unroll
+    for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = A(0);
+  }
+  const A inv = A(1) / A(p.n);
+  for (int64_t row0 = (int64_t)blockIdx.x * S::kRows; row0 < p.rows;
+       row0 += (int64_t)gridDim.x * S::kRows) {
+    const int64_t row = row0 + group * R;
+    Vec<T> x[R][K], y[R][K];
+    A s[R], q[R], mean[R], rstd[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool in = row + r < p.rows;
+      mean[r] = in ? ((const A*)p.mean)[row + r] : A(0);
+      rstd[r] = in ? ((const A*)p.rstd)[row + r] : A(0);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        x[r][k].v = y[r][k].v = typename Vec<T>::type{};
+        if (in && n[k] > 0) {
+          x[r][k] = load_part((const T*)p.x + (row + r) * p.sx + (k * L + lane) * V, n[k]);
+          y[r][k] = load_part((const T*)p.dy + (row + r) * p.sdy + (k * L + lane) * V, n[k]);
+        }
+      }
+    }
+    // columns beyond the end have dy = 0 and add nothing; rows beyond it too
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      s[r] = q[r] = A(0);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const A d = up(y[r][k].v[i]), h = (up(x[r][k].v[i]) - mean[r]) * rstd[r];
+          const A e = d * (A)up(w[k].v[i]);
+          s[r] += e;
+          q[r] = fma_(e, h, q[r]);
+          dw[k][i] = fma_(d, h, dw[k][i]);
+          db[k][i] += d;
+        }
+    }
+    if (!p.dx) continue;
+    group_sum<S>(sm, turn, s);
+    group_sum<S>(sm2, turn2, q);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= p.rows) continue;
+      const A ms = s[r] * inv, mq = q[r] * inv;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (n[k] <= 0) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const A h = (up(x[r][k].v[i]) - mean[r]) * rstd[r];
+          const A e = up(y[r][k].v[i]) * (A)up(w[k].v[i]);
+          x[r][k].v[i] = down<T>(fma_(-mq, h, e - ms) * rstd[r]);
+        }
+        store_part((T*)p.dx + (row + r) * p.n + (k * L + lane) * V, x[r][k], n[k]);
+      }
+    }
+  }
+  if (!part) return;
+  // The groups' sums, added in their order: in LDS, a group after the other.
+  A* const out = part + (int64_t)blockIdx.x * 2 * p.n;
+  if constexpr (S::G > 1) {
+    __shared__ A total[2][L * K * V];
+    for (int g = 0; g < S::G; ++g) {
+      __syncthreads();
+      if (group == g) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const int c = (k * L + lane) * V + i;
+            total[0][c] = g == 0 ? dw[k][i] : total[0][c] + dw[k][i];
+            total[1][c] = g == 0 ? db[k][i] : total[1][c] + db[k][i];
+          }
+      }
+    }
+    __syncthreads();
+    for (int64_t c = threadIdx.x; c < p.n; c += NT) {
+      out[c] = total[0][c];
+      out[p.n + c] = total[1][c];
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < n[k]) {
+          out[(k * L + lane) * V + i] = dw[k][i];
+          out[p.n + (k * L + lane) * V + i] = db[k][i];
+        }
+  }
+}
+
+// Rows of any length, read again for each pass; a workgroup a row at a time.
+constexpr int kLongThreads = 1024;
 template <class T>
-__global__ __launch_bounds__(kThreads) void norm_dw_part(NormArgs p, Acc<T>* part) {
-  typedef Acc<T> A;
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= p.n) return;
-  A sw = 0, sb = 0;
-  for (int64_t row = blockIdx.y; row < p.rows; row += kParts) {
-    const A d = up(((const T*)p.dy)[row * p.sdy + i]);
-    const A xh = (up(((const T*)p.x)[row * p.sx + i]) - ((const A*)p.mean)[row]) *
-                 ((const A*)p.rstd)[row];
-    sw = fma_(d, xh, sw);
-    sb += d;
+struct LongShape : Shape<T, kLongThreads, kLongThreads, 1, 2> {};
+
+template <class T, class W>
+__global__ __launch_bounds__(kLongThreads) void norm_fwd_long(NormArgs p) {
+  typedef LongShape<T> S;
+  typedef typename S::A A;
+  constexpr int V = S::V;
+  __shared__ Sums<S> sm;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const T* x = (const T*)p.x + row * p.sx;
+    T* y = (T*)p.y + row * p.n;
+    A s[1] = {A(0)};
+    for (int64_t c = threadIdx.x * V; c < p.n; c += kLongThreads * V) {
+      const Vec<T> v = load_part(x + c, (int)min((int64_t)V, p.n - c));
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[0] += up(v.v[i]);
+    }
+    group_sum<S>(sm, turn, s);
+    const A mean = s[0] / A(p.n);
+    s[0] = A(0);
+    for (int64_t c = threadIdx.x * V; c < p.n; c += kLongThreads * V) {
+      const int n = (int)min((int64_t)V, p.n - c);
+      const Vec<T> v = load_part(x + c, n);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const A d = i < n ? up(v.v[i]) - mean : A(0);
+        s[0] = fma_(d, d, s[0]);
+      }
+    }
+    group_sum<S>(sm, turn, s);
+    const A rstd = A(1) / sqrt_(s[0] / A(p.n) + A(p.eps));
+    for (int64_t c = threadIdx.x * V; c < p.n; c += kLongThreads * V) {
+      const int n = (int)min((int64_t)V, p.n - c);
+      Vec<T> v = load_part(x + c, n);
+      const Pack<W, V> w = load_pack<W, V>(p.w ? (const W*)p.w + c : nullptr, n, W(1));
+      const Pack<W, V> b = load_pack<W, V>(p.b ? (const W*)p.b + c : nullptr, n, W(0));
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        v.v[i] = down<T>(fma_((up(v.v[i]) - mean) * rstd, (A)up(w.v[i]), (A)up(b.v[i])));
+      store_part(y + c, v, n);
+    }
+    if (threadIdx.x == 0) {
+      if (p.mean) ((A*)p.mean)[row] = mean;
+      if (p.rstd) ((A*)p.rstd)[row] = rstd;
+    }
   }
-  part[(2 * (int64_t)blockIdx.y) * p.n + i] = sw;
-  part[(2 * (int64_t)blockIdx.y + 1) * p.n + i] = sb;
 }
 
 template <class T, class W>
-__global__ __launch_bounds__(kThreads) void norm_dw_sum(NormArgs p, const Acc<T>* part, int parts) {
-  typedef Acc<T> A;
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= p.n) return;
-  A sw = 0, sb = 0;
-  for (int64_t k = 0; k < parts; ++k) {
-    sw += part[2 * k * p.n + i];
-    sb += part[(2 * k + 1) * p.n + i];
+__global__ __launch_bounds__(kLongThreads) void norm_rev_long(NormArgs p) {
+  typedef LongShape<T> S;
+  typedef typename S::A A;
+  constexpr int V = S::V;
+  __shared__ Sums<S> sm;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const T* x = (const T*)p.x + row * p.sx;
+    const T* dy = (const T*)p.dy + row * p.sdy;
+    T* dx = (T*)p.dx + row * p.n;
+    const A mean = ((const A*)p.mean)[row], rstd = ((const A*)p.rstd)[row];
+    A s[2] = {A(0), A(0)};
+    for (int64_t c = threadIdx.x * V; c < p.n; c += kLongThreads * V) {
+      const int n = (int)min((int64_t)V, p.n - c);
+      const Vec<T> v = load_part(x + c, n), d = load_part(dy + c, n);
+      const Pack<W, V> w = load_pack<W, V>(p.w ? (const W*)p.w + c : nullptr, n, W(1));
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const A e = up(d.v[i]) * (A)up(w.v[i]);
+        s[0] += e;
+        s[1] = fma_(e, (up(v.v[i]) - mean) * rstd, s[1]);
+      }
+    }
+    group_sum<S>(sm, turn, s);
+    const A ms = s[0] / A(p.n), mq = s[1] / A(p.n);
+    for (int64_t c = threadIdx.x * V; c < p.n; c += kLongThreads * V) {
+      const int n = (int)min((int64_t)V, p.n - c);
+      Vec<T> v = load_part(x + c, n);
+      const Vec<T> d = load_part(dy + c, n);
+      const Pack<W, V> w = load_pack<W, V>(p.w ? (const W*)p.w + c : nullptr, n, W(1));
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const A h = (up(v.v[i]) - mean) * rstd, e = up(d.v[i]) * (A)up(w.v[i]);
+        v.v[i] = down<T>(fma_(-mq, h, e - ms) * rstd);
+      }
+      store_part(dx + c, v, n);
+    }
   }
-  if (p.dw) ((W*)p.dw)[i] = down<W>(sw);
-  if (p.db) ((W*)p.db)[i] = down<W>(sb);
 }
 
+// The same rows' sums of dw and db: a vector of columns a thread, of the rows
+// blockIdx.y, + gridDim.y, ...
+constexpr int kColumnThreads = 64;
+template <class T>
+__global__ __launch_bounds__(kColumnThreads) void norm_dw_long(NormArgs p, Acc<T>* part) {
+  typedef Acc<T> A;
+  constexpr int V = Vec<T>::N;
+  const int64_t c = ((int64_t)blockIdx.x * kColumnThreads + threadIdx.x) * V;
+  const int n = (int)min((int64_t)V, p.n - c);
+  if (n <= 0) return;
+  A sw[V], sb[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sw[i] = sb[i] = A(0);
+  for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+    const Vec<T> v = load_part((const T*)p.x + row * p.sx + c, n);
+    const Vec<T> d = load_part((const T*)p.dy + row * p.sdy + c, n);
+    const A mean = ((const A*)p.mean)[row], rstd = ((const A*)p.rstd)[row];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      sw[i] = fma_(up(d.v[i]), (up(v.v[i]) - mean) * rstd, sw[i]);
+      sb[i] += up(d.v[i]);
+    }
+  }
+  A* const out = part + (int64_t)blockIdx.y * 2 * p.n + c;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < n) out[i] = sw[i], out[p.n + i] = sb[i];
+}
+
+// dw and db from the workgroups' sums: 64 columns a workgroup, its waves each
+// a share of the parts.
+constexpr int kSumWaves = 16;
+template <class T, class W>
+__global__ __launch_bounds__(64 * kSumWaves) void norm_dw_sum(NormArgs p, const Acc<T>* part,
+                                                              int parts) {
+  typedef Acc<T> A;
+  __shared__ A sums[kSumWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;  // of dw's columns, then db's
+  A s = A(0);
+  if (c < 2 * p.n) {
+    const int share = (parts + kSumWaves - 1) / kSumWaves;
+    const int from = wave * share, to = min(from + share, parts);
+#pragma unroll 8
+    for (int k = from; k < to; ++k) s += part[(int64_t)k * 2 * p.n + c];
+  }
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave > 0 || c >= 2 * p.n) return;
+#pragma unroll
+  for (int k = 1; k < kSumWaves; ++k) s += sums[k][lane];
+  if (c < p.n) {
+    if (p.dw) ((W*)p.dw)[c] = down<W>((Acc<W>)s);
+  } else if (p.db) {
+    ((W*)p.db)[c - p.n] = down<W>((Acc<W>)s);
+  }
+}
+
+// -------------------------------------------------------------- on the host
 template <class F>
 hipError_t by_type(int32_t dtype, int32_t wtype, F f) {
   switch (dtype) {
@@ -120,32 +437,94 @@ hipError_t by_type(int32_t dtype, int32_t wtype, F f) {
   return hipGetLastError();
 }
 
-int parts_of(int64_t rows) { return (int)(rows < kParts ? rows : kParts); }
+int64_t vectors_of(int32_t dtype, int64_t n) {
+  const int64_t v = dtype == ADST_F64 ? 2 : dtype == ADST_F32 ? 4 : 8;
+  return (n + v - 1) / v;
+}
+// Vectors of a row that registers hold: in the VJP with the sums of dw and db,
+// fewer.
+constexpr int64_t kHeld = 4096;
+int64_t held_in_vjp(int32_t dtype) { return dtype == ADST_F32 ? 4096 : 2048; }
+
+// Workgroups of the forward: enough to fill the chip several times over, each
+// with several rows to keep its weights for.
+template <class T, class W, int NT, int L, int K, int R>
+void forward(const NormArgs& a, hipStream_t st) {
+  const int64_t per = (int64_t)NT / L * R, all = (a.rows + per - 1) / per;
+  const int64_t most = 256 * 2048 / NT;
+  norm_fwd<T, W, NT, L, K, R><<<(unsigned)(all < most ? all : most), NT, 0, st>>>(a);
+}
+unsigned long_grid(int64_t rows) { return (unsigned)(rows < 4096 ? rows : 4096); }
+template <class T, class W>
+void forward_by_length(const NormArgs& a, int64_t nv, hipStream_t st) {
+  if (nv <= 16) forward<T, W, 256, 16, 1, 2>(a, st);
+  else if (nv <= 64) forward<T, W, 256, 64, 1, 4>(a, st);
+  else if (nv <= 128) forward<T, W, 256, 64, 2, 2>(a, st);
+  else if (nv <= 256) forward<T, W, 256, 64, 4, 1>(a, st);
+  else if (nv <= 512) forward<T, W, 256, 256, 2, 1>(a, st);
+  else if (nv <= 1024) forward<T, W, 256, 256, 4, 1>(a, st);
+  else if (nv <= 2048) forward<T, W, 512, 512, 4, 1>(a, st);
+  else if (nv <= kHeld) forward<T, W, 1024, 1024, 4, 1>(a, st);
+  else norm_fwd_long<T, W><<<long_grid(a.rows), kLongThreads, 0, st>>>(a);
+}
+
+// Groups of rows that sum dw and db apart.
+constexpr int kParts = 512, kLongParts = 128;
+int parts_of(int32_t dtype, int64_t rows, int64_t nv) {
+  // rows that the VJP's workgroups take at a time (reverse_by_length)
+  const int64_t at_once = nv <= 16 ? 64 : nv <= 64 ? 32 : nv <= 128 ? 16
+                          : nv <= 256 ? 8 : nv <= 512 ? 4 : 1;
+  const int64_t all = (rows + at_once - 1) / at_once;
+  const int64_t most = nv > held_in_vjp(dtype) ? kLongParts : nv > 1024 ? kParts / 2 : kParts;
+  return (int)(all < most ? all : most);
+}
+
+template <class T, class W>
+void reverse_by_length(const NormArgs& a, int64_t nv, int parts, Acc<T>* part, hipStream_t st) {
+  const unsigned g = (unsigned)parts;
+  if (nv <= 16) norm_rev<T, W, 512, 16, 1, 2><<<g, 512, 0, st>>>(a, part);
+  else if (nv <= 64) norm_rev<T, W, 512, 64, 1, 4><<<g, 512, 0, st>>>(a, part);
+  else if (nv <= 128) norm_rev<T, W, 512, 64, 2, 2><<<g, 512, 0, st>>>(a, part);
+  else if (nv <= 256) norm_rev<T, W, 512, 256, 1, 4><<<g, 512, 0, st>>>(a, part);
+  else if (nv <= 512) norm_rev<T, W, 512, 256, 2, 2><<<g, 512, 0, st>>>(a, part);
+  else if (nv <= 1024) norm_rev<T, W, 512, 512, 2, 1><<<g, 512, 0, st>>>(a, part);
+  else if (nv <= 2048) norm_rev<T, W, 512, 512, 4, 1><<<g, 512, 0, st>>>(a, part);
+  else if (nv <= held_in_vjp(a.dtype)) {
+    if constexpr (sizeof(T) == 4) norm_rev<T, W, 1024, 1024, 4, 1><<<g, 1024, 0, st>>>(a, part);
+  } else {
+    if (a.dx) norm_rev_long<T, W><<<long_grid(a.rows), kLongThreads, 0, st>>>(a);
+    if (part) {
+      const unsigned columns = (unsigned)((nv + kColumnThreads - 1) / kColumnThreads);
+      norm_dw_long<T><<<dim3(columns, g), kColumnThreads, 0, st>>>(a, part);
+    }
+  }
+}
 
 }  // namespace
 
 hipError_t norm_forward(const NormArgs& a, hipStream_t st) {
+  const int64_t nv = vectors_of(a.dtype, a.n);
   return by_type(a.dtype, a.wtype, [&](auto t, auto w) {
-    norm_fwd<decltype(t), decltype(w)><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
+    forward_by_length<decltype(t), decltype(w)>(a, nv, st);
   });
 }
 
 uint64_t norm_workspace_bytes(int32_t dtype, int64_t rows, int64_t n) {
-  return 2ull * parts_of(rows) * (uint64_t)n * (dtype == ADST_F64 ? 8 : 4);
+  return 2ull * parts_of(dtype, rows, vectors_of(dtype, n)) * (uint64_t)n * (dtype == ADST_F64 ? 8 : 4);
 }
 
 hipError_t norm_vjp(const NormArgs& a, void* ws, hipStream_t st) {
+  const int64_t nv = vectors_of(a.dtype, a.n);
+  const int parts = parts_of(a.dtype, a.rows, nv);
+  const bool sums = a.dw || a.db;
   return by_type(a.dtype, a.wtype, [&](auto t, auto w) {
     typedef decltype(t) T;
     typedef decltype(w) W;
-    if (a.dx && a.rows > 0) norm_dx<T, W><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
-    if (a.dw || a.db) {
-      const int parts = parts_of(a.rows);
-      const unsigned cols = (unsigned)((a.n + kThreads - 1) / kThreads);
-      Acc<T>* part = (Acc<T>*)ws;
-      if (parts > 0)
-        norm_dw_part<T><<<dim3(cols, parts), kThreads, 0, st>>>(a, part);
-      norm_dw_sum<T, W><<<cols, kThreads, 0, st>>>(a, part, parts);
+    Acc<T>* const part = sums ? (Acc<T>*)ws : nullptr;
+    if (parts > 0) reverse_by_length<T, W>(a, nv, parts, part, st);
+    if (sums) {
+      const unsigned columns = (unsigned)((2 * a.n + 63) / 64);
+      norm_dw_sum<T, W><<<columns, 64 * kSumWaves, 0, st>>>(a, part, parts);
     }
   });
 }

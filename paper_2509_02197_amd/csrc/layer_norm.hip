@@ -41,6 +41,39 @@ __device__ inline Pack<W, N> load_pack(const W* p, int n, W none) {
   return r;
 }
 
+// Has the compiler keep 16-bit vectors as they are and unpack them again
+// later: unpacked, they take twice the registers.
+template <class T, int R, int K>
+__device__ inline void keep_packed(Vec<T> (&x)[R][K]) {
+  if constexpr (sizeof(T) == 2) {
+    typedef uint32_t Four __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        Four w = __builtin_bit_cast(Four, x[r][k].v);
+        asm volatile("" : "+v"(w));
+        x[r][k].v = __builtin_bit_cast(typename Vec<T>::type, w);
+      }
+  }
+}
+
+// The compiler does not mix the vectors before with those after: their
+// intermediate values share registers.
+__device__ inline void one_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
+template <class W, int N, int K>
+__device__ inline void keep_packed(Pack<W, N> (&w)[K]) {
+  if constexpr (sizeof(W) == 2) {
+    typedef uint32_t Words __attribute__((ext_vector_type(N / 2)));
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      Words x = __builtin_bit_cast(Words, w[k].v);
+      asm volatile("" : "+v"(x));
+      w[k].v = __builtin_bit_cast(typename Pack<W, N>::type, x);
+    }
+  }
+}
+
 // A workgroup of NT threads in groups of L lanes; a lane holds K vectors of
 // each of R rows.
 template <class T, int NT_, int L_, int K_, int R_>
@@ -53,15 +86,54 @@ struct Shape {
   static constexpr int kRows = G * R;          // rows of a workgroup at a time
 };
 
-// Sums over a group, of R values each, in every lane. Calls alternate between
+// How rows are read and written: vectors at a row's end in part (PARTS), or
+// all of them whole (WHOLE), then also with non-temporal hints (STREAM).
+enum Mode { PARTS, WHOLE, STREAM };
+
+// A group's R rows, this lane's vectors of them: n[k] columns of the k-th,
+// zeros beyond a row's end and the last row.
+template <class S, Mode M, class T>
+__device__ inline void load_rows(const void* base, int64_t stride, int64_t row, int64_t rows,
+                                 const int (&n)[S::K], Vec<T> (&v)[S::R][S::K]) {
+  const T* p = (const T*)base + row * stride + threadIdx.x % S::L * S::V;
+#pragma unroll
+  for (int r = 0; r < S::R; ++r)
+#pragma unroll
+    for (int k = 0; k < S::K; ++k) {
+      v[r][k].v = typename Vec<T>::type{};
+      if (row + r < rows && n[k] > 0) {
+        const T* at = p + r * stride + k * S::L * S::V;
+        if constexpr (M == STREAM)
+          v[r][k].v = __builtin_nontemporal_load(
+              reinterpret_cast<const typename Vec<T>::unaligned*>(at));
+        else if constexpr (M == WHOLE) v[r][k] = load_vec(at);
+        else v[r][k] = load_part(at, n[k]);
+      }
+    }
+}
+template <class S, Mode M, class T>
+__device__ inline void store_row(void* base, int64_t row, int64_t columns,
+                                 const int (&n)[S::K], const Vec<T> (&v)[S::K]) {
+  T* p = (T*)base + row * columns + threadIdx.x % S::L * S::V;
+#pragma unroll
+  for (int k = 0; k < S::K; ++k)
+    if (n[k] > 0) {
+      T* at = p + k * S::L * S::V;
+      if constexpr (M == STREAM)
+        __builtin_nontemporal_store(v[k].v, reinterpret_cast<typename Vec<T>::unaligned*>(at));
+      else if constexpr (M == WHOLE) store_vec(at, v[k]);
+      else store_part(at, v[k], n[k]);
+    }
+}
+
+// Sums over a group, of N values each, in every lane. Calls alternate between
 // two buffers, so that one barrier a call is enough.
-template <class S>
+template <class S, int N>
 struct Sums {
-  typename S::A part[2][S::G][S::W][S::R];
+  typename S::A part[2][S::G][S::W][N];
 };
 template <class S, int N>
-__device__ inline void group_sum(Sums<S>& sm, int& turn, typename S::A (&v)[N]) {
-  static_assert(N <= S::R, "");
+__device__ inline void group_sum(Sums<S, N>& sm, int& turn, typename S::A (&v)[N]) {
 #pragma unroll
   for (int r = 0; r < N; ++r) v[r] = lane_sum<(S::L < 64 ? S::L : 64)>(v[r]);
   if constexpr (S::W > 1) {
@@ -81,22 +153,26 @@ __device__ inline void group_sum(Sums<S>& sm, int& turn, typename S::A (&v)[N]) 
   }
 }
 
-template <class T, class W, int NT, int L, int K, int R_>
+template <class T, class W, int NT, int L, int K, int R_, Mode M>
 __global__ __launch_bounds__(NT) void norm_fwd(NormArgs p) {
   typedef Shape<T, NT, L, K, R_> S;
   typedef typename S::A A;
   constexpr int V = S::V, R = S::R;
-  __shared__ Sums<S> sm;
+  __shared__ Sums<S, R> sm;
   int turn = 0;
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
+  constexpr bool kHoldsWeights = K < 8;
   int n[K];  // columns of each of this lane's vectors
   Pack<W, V> w[K], b[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
+  const auto weights = [&](int k) {
     const int64_t c = (int64_t)(k * L + lane) * V;
-    n[k] = (int)min((int64_t)V, p.n - c);
     w[k] = load_pack<W, V>(p.w ? (const W*)p.w + c : nullptr, n[k], W(1));
     b[k] = load_pack<W, V>(p.b ? (const W*)p.b + c : nullptr, n[k], W(0));
+  };
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    n[k] = (int)min((int64_t)V, p.n - (int64_t)(k * L + lane) * V);
+    if (kHoldsWeights) weights(k);
   }
   const A inv = A(1) / A(p.n);
   for (int64_t row0 = (int64_t)blockIdx.x * S::kRows; row0 < p.rows;
@@ -104,14 +180,7 @@ __global__ __launch_bounds__(NT) void norm_fwd(NormArgs p) {
     const int64_t row = row0 + group * R;
     Vec<T> x[R][K];
     A s[R], mean[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        x[r][k].v = typename Vec<T>::type{};
-        if (row + r < p.rows && n[k] > 0)
-          x[r][k] = load_part((const T*)p.x + (row + r) * p.sx + (k * L + lane) * V, n[k]);
-      }
+    load_rows<S, M>(p.x, p.sx, row, p.rows, n, x);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       s[r] = A(0);
@@ -120,6 +189,7 @@ __global__ __launch_bounds__(NT) void norm_fwd(NormArgs p) {
 #pragma unroll
         for (int i = 0; i < V; ++i) s[r] += up(x[r][k].v[i]);
     }
+    keep_packed(x);
     group_sum<S>(sm, turn, s);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -129,10 +199,11 @@ __global__ __launch_bounds__(NT) void norm_fwd(NormArgs p) {
       for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const A d = i < n[k] ? up(x[r][k].v[i]) - mean[r] : A(0);
+          const A d = (M != PARTS ? n[k] > 0 : i < n[k]) ? up(x[r][k].v[i]) - mean[r] : A(0);
           s[r] = fma_(d, d, s[r]);
         }
     }
+    keep_packed(x);
     group_sum<S>(sm, turn, s);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -140,13 +211,13 @@ __global__ __launch_bounds__(NT) void norm_fwd(NormArgs p) {
       const A rstd = A(1) / sqrt_(s[r] * inv + A(p.eps));
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        if (n[k] <= 0) continue;
+        if (!kHoldsWeights) weights(k);
 #pragma unroll
         for (int i = 0; i < V; ++i)
           x[r][k].v[i] = down<T>(fma_((up(x[r][k].v[i]) - mean[r]) * rstd, (A)up(w[k].v[i]),
                                       (A)up(b[k].v[i])));
-        store_part((T*)p.y + (row + r) * p.n + (k * L + lane) * V, x[r][k], n[k]);
       }
+      store_row<S, M>(p.y, row + r, p.n, n, x[r]);
       if (lane == 0) {
         if (p.mean) ((A*)p.mean)[row + r] = mean[r];
         if (p.rstd) ((A*)p.rstd)[row + r] = rstd;
@@ -155,16 +226,15 @@ __global__ __launch_bounds__(NT) void norm_fwd(NormArgs p) {
   }
 }
 
-// dx, and where part is given this workgroup's sums of dw and db in
-// part[blockIdx.x][2][n].
-template <class T, class W, int NT, int L, int K, int R_>
+// dx (where asked for), and with SUMS and where part is given this workgroup's
+// sums of dw and db in part[blockIdx.x][2][n].
+template <class T, class W, int NT, int L, int K, int R_, Mode M, bool SUMS>
 __global__ __launch_bounds__(NT) void norm_rev(NormArgs p, Acc<T>* part) {
   typedef Shape<T, NT, L, K, R_> S;
   typedef typename S::A A;
   constexpr int V = S::V, R = S::R;
-  __shared__ Sums<S> sm;
-  __shared__ Sums<S> sm2;
-  int turn = 0, turn2 = 0;
+  __shared__ Sums<S, 2 * R> sm;
+  int turn = 0;
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
   int n[K];
   Pack<W, V> w[K];
@@ -182,103 +252,115 @@ __global__ __launch_bounds__(NT) void norm_rev(NormArgs p, Acc<T>* part) {
        row0 += (int64_t)gridDim.x * S::kRows) {
     const int64_t row = row0 + group * R;
     Vec<T> x[R][K], y[R][K];
-    A s[R], q[R], mean[R], rstd[R];
+    A s[2 * R], mean[R], rstd[R];  // sums of e, then of e * xhat
+    load_rows<S, M>(p.x, p.sx, row, p.rows, n, x);
+    load_rows<S, M>(p.dy, p.sdy, row, p.rows, n, y);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const bool in = row + r < p.rows;
-      mean[r] = in ? ((const A*)p.mean)[row + r] : A(0);
-      rstd[r] = in ? ((const A*)p.rstd)[row + r] : A(0);
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        x[r][k].v = y[r][k].v = typename Vec<T>::type{};
-        if (in && n[k] > 0) {
-          x[r][k] = load_part((const T*)p.x + (row + r) * p.sx + (k * L + lane) * V, n[k]);
-          y[r][k] = load_part((const T*)p.dy + (row + r) * p.sdy + (k * L + lane) * V, n[k]);
-        }
-      }
+      mean[r] = row + r < p.rows ? ((const A*)p.mean)[row + r] : A(0);
+      rstd[r] = row + r < p.rows ? ((const A*)p.rstd)[row + r] : A(0);
     }
     // columns beyond the end have dy = 0 and add nothing; rows beyond it too
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      s[r] = q[r] = A(0);
+      s[r] = s[R + r] = A(0);
 #pragma unroll
-      for (int k = 0; k < K; ++k)
+      for (int k = 0; k < K; ++k) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const A d = up(y[r][k].v[i]), h = (up(x[r][k].v[i]) - mean[r]) * rstd[r];
           const A e = d * (A)up(w[k].v[i]);
           s[r] += e;
-          q[r] = fma_(e, h, q[r]);
-          dw[k][i] = fma_(d, h, dw[k][i]);
-          db[k][i] += d;
+          s[R + r] = fma_(e, h, s[R + r]);
+          if (SUMS) {
+            dw[k][i] = fma_(d, h, dw[k][i]);
+            db[k][i] += d;
+          }
         }
+        one_at_a_time();
+      }
     }
     if (!p.dx) continue;
+    keep_packed(x);
+    keep_packed(y);
+    keep_packed(w);
     group_sum<S>(sm, turn, s);
-    group_sum<S>(sm2, turn2, q);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (row + r >= p.rows) continue;
-      const A ms = s[r] * inv, mq = q[r] * inv;
+      const A ms = s[r] * inv, mq = s[R + r] * inv;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        if (n[k] <= 0) continue;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const A h = (up(x[r][k].v[i]) - mean[r]) * rstd[r];
           const A e = up(y[r][k].v[i]) * (A)up(w[k].v[i]);
           x[r][k].v[i] = down<T>(fma_(-mq, h, e - ms) * rstd[r]);
         }
-        store_part((T*)p.dx + (row + r) * p.n + (k * L + lane) * V, x[r][k], n[k]);
+        one_at_a_time();
       }
+      store_row<S, M>(p.dx, row + r, p.n, n, x[r]);
     }
+    keep_packed(w);
   }
-  if (!part) return;
-  // The groups' sums, added in their order: in LDS, a group after the other.
-  A* const out = part + (int64_t)blockIdx.x * 2 * p.n;
-  if constexpr (S::G > 1) {
-    __shared__ A total[2][L * K * V];
-    for (int g = 0; g < S::G; ++g) {
-      __syncthreads();
-      if (group == g) {
+  if constexpr (SUMS) {
+    if (!part) return;
+    // The groups' sums (of 16 lanes: first the wave's four), added in their
+    // order through LDS.
+    constexpr int kShare = L < 64 ? 64 : L, kShares = NT / kShare;
+    A* const out = part + (int64_t)blockIdx.x * 2 * p.n;
+    if constexpr (L < 64) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const int c = (k * L + lane) * V + i;
-            total[0][c] = g == 0 ? dw[k][i] : total[0][c] + dw[k][i];
-            total[1][c] = g == 0 ? db[k][i] : total[1][c] + db[k][i];
-          }
+      for (int i = 0; i < V; ++i) {
+        dw[0][i] = sum_rows(dw[0][i]);
+        db[0][i] = sum_rows(db[0][i]);
       }
     }
-    __syncthreads();
-    for (int64_t c = threadIdx.x; c < p.n; c += NT) {
-      out[c] = total[0][c];
-      out[p.n + c] = total[1][c];
-    }
-  } else {
+    const int share = threadIdx.x / kShare;
+    if constexpr (kShares > 1) {
+      __shared__ A total[kShares][L * K * V];
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+      for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+        if (L >= 64 || (threadIdx.x & 63) < L) {
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < n[k]) {
-          out[(k * L + lane) * V + i] = dw[k][i];
-          out[p.n + (k * L + lane) * V + i] = db[k][i];
+          for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+              total[share][(k * L + lane) * V + i] = which ? db[k][i] : dw[k][i];
         }
+        __syncthreads();
+        for (int c = threadIdx.x; c < p.n; c += NT) {
+          A t = total[0][c];
+#pragma unroll
+          for (int g = 1; g < kShares; ++g) t += total[g][c];
+          out[which * p.n + c] = t;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (i < n[k]) {
+            out[(k * L + lane) * V + i] = dw[k][i];
+            out[p.n + (k * L + lane) * V + i] = db[k][i];
+          }
+    }
   }
 }
 
 // Rows of any length, read again for each pass; a workgroup a row at a time.
 constexpr int kLongThreads = 1024;
 template <class T>
-struct LongShape : Shape<T, kLongThreads, kLongThreads, 1, 2> {};
+struct LongShape : Shape<T, kLongThreads, kLongThreads, 1, 1> {};
 
 template <class T, class W>
 __global__ __launch_bounds__(kLongThreads) void norm_fwd_long(NormArgs p) {
   typedef LongShape<T> S;
   typedef typename S::A A;
   constexpr int V = S::V;
-  __shared__ Sums<S> sm;
+  __shared__ Sums<S, 1> sm;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const T* x = (const T*)p.x + row * p.sx;
@@ -325,7 +407,7 @@ __global__ __launch_bounds__(kLongThreads) void norm_rev_long(NormArgs p) {
   typedef LongShape<T> S;
   typedef typename S::A A;
   constexpr int V = S::V;
-  __shared__ Sums<S> sm;
+  __shared__ Sums<S, 2> sm;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const T* x = (const T*)p.x + row * p.sx;
@@ -390,28 +472,29 @@ __global__ __launch_bounds__(kColumnThreads) void norm_dw_long(NormArgs p, Acc<T
     if (i < n) out[i] = sw[i], out[p.n + i] = sb[i];
 }
 
-// dw and db from the workgroups' sums: 64 columns a workgroup, its waves each
-// a share of the parts.
-constexpr int kSumWaves = 16;
+// dw and db from the workgroups' sums: 32 columns a workgroup, 32 shares of the
+// parts.
+constexpr int kSumColumns = 32, kShares = 32;
 template <class T, class W>
-__global__ __launch_bounds__(64 * kSumWaves) void norm_dw_sum(NormArgs p, const Acc<T>* part,
-                                                              int parts) {
+__global__ __launch_bounds__(kSumColumns * kShares) void norm_dw_sum(NormArgs p,
+                                                                     const Acc<T>* part,
+                                                                     int parts) {
   typedef Acc<T> A;
-  __shared__ A sums[kSumWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;  // of dw's columns, then db's
+  __shared__ A sums[kShares][kSumColumns];
+  const int column = threadIdx.x % kSumColumns, share = threadIdx.x / kSumColumns;
+  const int64_t c = (int64_t)blockIdx.x * kSumColumns + column;  // of dw's columns, then db's
   A s = A(0);
   if (c < 2 * p.n) {
-    const int share = (parts + kSumWaves - 1) / kSumWaves;
-    const int from = wave * share, to = min(from + share, parts);
-#pragma unroll 8
+    const int each = (parts + kShares - 1) / kShares;
+    const int from = share * each, to = min(from + each, parts);
+#pragma unroll 16
     for (int k = from; k < to; ++k) s += part[(int64_t)k * 2 * p.n + c];
   }
-  sums[wave][lane] = s;
+  sums[share][column] = s;
   __syncthreads();
-  if (wave > 0 || c >= 2 * p.n) return;
+  if (share > 0 || c >= 2 * p.n) return;
 #pragma unroll
-  for (int k = 1; k < kSumWaves; ++k) s += sums[k][lane];
+  for (int k = 1; k < kShares; ++k) s += sums[k][column];
   if (c < p.n) {
     if (p.dw) ((W*)p.dw)[c] = down<W>((Acc<W>)s);
   } else if (p.db) {
@@ -441,10 +524,16 @@ int64_t vectors_of(int32_t dtype, int64_t n) {
   const int64_t v = dtype == ADST_F64 ? 2 : dtype == ADST_F32 ? 4 : 8;
   return (n + v - 1) / v;
 }
-// Vectors of a row that registers hold: in the VJP with the sums of dw and db,
-// fewer.
-constexpr int64_t kHeld = 4096;
+// Vectors of a row that the VJP's registers hold with the sums of dw and db.
 int64_t held_in_vjp(int32_t dtype) { return dtype == ADST_F32 ? 4096 : 2048; }
+
+// Non-temporal accesses where a call moves more than the caches keep for the
+// next one (32768 x 2048 bf16: forward 47 us against 49, VJP 77 against 83).
+constexpr int64_t kStreamBytes = int64_t(128) << 20;
+Mode mode_of(const NormArgs& a, int64_t size, int64_t arrays) {
+  if (a.n % (16 / size) != 0) return PARTS;
+  return a.rows * a.n * size * arrays >= kStreamBytes ? STREAM : WHOLE;
+}
 
 // Workgroups of the forward: enough to fill the chip several times over, each
 // with several rows to keep its weights for.
@@ -452,7 +541,11 @@ template <class T, class W, int NT, int L, int K, int R>
 void forward(const NormArgs& a, hipStream_t st) {
   const int64_t per = (int64_t)NT / L * R, all = (a.rows + per - 1) / per;
   const int64_t most = 256 * 2048 / NT;
-  norm_fwd<T, W, NT, L, K, R><<<(unsigned)(all < most ? all : most), NT, 0, st>>>(a);
+  const unsigned grid = (unsigned)(all < most ? all : most);
+  const Mode m = mode_of(a, sizeof(T), 2);
+  if (m == PARTS) norm_fwd<T, W, NT, L, K, R, PARTS><<<grid, NT, 0, st>>>(a);
+  else if (m == WHOLE) norm_fwd<T, W, NT, L, K, R, WHOLE><<<grid, NT, 0, st>>>(a);
+  else norm_fwd<T, W, NT, L, K, R, STREAM><<<grid, NT, 0, st>>>(a);
 }
 unsigned long_grid(int64_t rows) { return (unsigned)(rows < 4096 ? rows : 4096); }
 template <class T, class W>
@@ -464,7 +557,10 @@ void forward_by_length(const NormArgs& a, int64_t nv, hipStream_t st) {
   else if (nv <= 512) forward<T, W, 256, 256, 2, 1>(a, st);
   else if (nv <= 1024) forward<T, W, 256, 256, 4, 1>(a, st);
   else if (nv <= 2048) forward<T, W, 512, 512, 4, 1>(a, st);
-  else if (nv <= kHeld) forward<T, W, 1024, 1024, 4, 1>(a, st);
+  else if (nv <= 4096) forward<T, W, 1024, 1024, 4, 1>(a, st);
+  else if (nv <= 8192 && sizeof(T) == 4) {
+    if constexpr (sizeof(T) == 4) forward<T, W, 1024, 1024, 8, 1>(a, st);
+  }
   else norm_fwd_long<T, W><<<long_grid(a.rows), kLongThreads, 0, st>>>(a);
 }
 
@@ -473,26 +569,48 @@ constexpr int kParts = 512, kLongParts = 128;
 int parts_of(int32_t dtype, int64_t rows, int64_t nv) {
   // rows that the VJP's workgroups take at a time (reverse_by_length)
   const int64_t at_once = nv <= 16 ? 64 : nv <= 64 ? 32 : nv <= 128 ? 16
-                          : nv <= 256 ? 8 : nv <= 512 ? 4 : 1;
+                          : nv <= 512 ? 4 : 1;
   const int64_t all = (rows + at_once - 1) / at_once;
   const int64_t most = nv > held_in_vjp(dtype) ? kLongParts : nv > 1024 ? kParts / 2 : kParts;
   return (int)(all < most ? all : most);
 }
 
+template <class T, class W, int NT, int L, int K, int R, bool SUMS>
+void reverse_sums(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {
+  const Mode m = mode_of(a, sizeof(T), 3);
+  if (m == PARTS) norm_rev<T, W, NT, L, K, R, PARTS, SUMS><<<grid, NT, 0, st>>>(a, part);
+  else if (m == WHOLE) norm_rev<T, W, NT, L, K, R, WHOLE, SUMS><<<grid, NT, 0, st>>>(a, part);
+  else norm_rev<T, W, NT, L, K, R, STREAM, SUMS><<<grid, NT, 0, st>>>(a, part);
+}
+template <class T, class W, int NT, int L, int K, int R>
+void reverse(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {
+  reverse_sums<T, W, NT, L, K, R, true>(a, grid, part, st);
+}
+
 template <class T, class W>
 void reverse_by_length(const NormArgs& a, int64_t nv, int parts, Acc<T>* part, hipStream_t st) {
   const unsigned g = (unsigned)parts;
-  if (nv <= 16) norm_rev<T, W, 512, 16, 1, 2><<<g, 512, 0, st>>>(a, part);
-  else if (nv <= 64) norm_rev<T, W, 512, 64, 1, 4><<<g, 512, 0, st>>>(a, part);
-  else if (nv <= 128) norm_rev<T, W, 512, 64, 2, 2><<<g, 512, 0, st>>>(a, part);
-  else if (nv <= 256) norm_rev<T, W, 512, 256, 1, 4><<<g, 512, 0, st>>>(a, part);
-  else if (nv <= 512) norm_rev<T, W, 512, 256, 2, 2><<<g, 512, 0, st>>>(a, part);
-  else if (nv <= 1024) norm_rev<T, W, 512, 512, 2, 1><<<g, 512, 0, st>>>(a, part);
-  else if (nv <= 2048) norm_rev<T, W, 512, 512, 4, 1><<<g, 512, 0, st>>>(a, part);
+  if (nv <= 16) reverse<T, W, 512, 16, 1, 2>(a, g, part, st);
+  else if (nv <= 64) reverse<T, W, 512, 64, 1, 4>(a, g, part, st);
+  else if (nv <= 128) reverse<T, W, 512, 64, 2, 2>(a, g, part, st);
+  else if (nv <= 256) reverse<T, W, 512, 256, 1, 2>(a, g, part, st);
+  else if (nv <= 512) reverse<T, W, 512, 256, 2, 2>(a, g, part, st);
+  else if (nv <= 1024) reverse<T, W, 512, 512, 2, 1>(a, g, part, st);
+  else if (nv <= 2048) reverse<T, W, 512, 512, 4, 1>(a, g, part, st);
   else if (nv <= held_in_vjp(a.dtype)) {
-    if constexpr (sizeof(T) == 4) norm_rev<T, W, 1024, 1024, 4, 1><<<g, 1024, 0, st>>>(a, part);
+    if constexpr (sizeof(T) == 4) reverse<T, W, 1024, 1024, 4, 1>(a, g, part, st);
   } else {
-    if (a.dx) norm_rev_long<T, W><<<long_grid(a.rows), kLongThreads, 0, st>>>(a);
+    // dx without the sums' registers, as long as those hold the row
+    if (!a.dx) {
+    } else if (nv <= 4096) {
+      if constexpr (sizeof(T) != 4)
+        reverse_sums<T, W, 1024, 1024, 4, 1, false>(a, long_grid(a.rows), nullptr, st);
+    } else if (nv <= 8192 && sizeof(T) == 4) {
+      if constexpr (sizeof(T) == 4)
+        reverse_sums<T, W, 1024, 1024, 8, 1, false>(a, long_grid(a.rows), nullptr, st);
+    } else {
+      norm_rev_long<T, W><<<long_grid(a.rows), kLongThreads, 0, st>>>(a);
+    }
     if (part) {
       const unsigned columns = (unsigned)((nv + kColumnThreads - 1) / kColumnThreads);
       norm_dw_long<T><<<dim3(columns, g), kColumnThreads, 0, st>>>(a, part);
@@ -523,8 +641,8 @@ hipError_t norm_vjp(const NormArgs& a, void* ws, hipStream_t st) {
     Acc<T>* const part = sums ? (Acc<T>*)ws : nullptr;
     if (parts > 0) reverse_by_length<T, W>(a, nv, parts, part, st);
     if (sums) {
-      const unsigned columns = (unsigned)((2 * a.n + 63) / 64);
-      norm_dw_sum<T, W><<<columns, 64 * kSumWaves, 0, st>>>(a, part, parts);
+      const unsigned grid = (unsigned)((2 * a.n + kSumColumns - 1) / kSumColumns);
+      norm_dw_sum<T, W><<<grid, kSumColumns * kShares, 0, st>>>(a, part, parts);
     }
   });
 }

@@ -87,12 +87,44 @@ __device__ inline void store_part(T* p, Vec<T> v, int n) {
 __device__ inline float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
 __device__ inline double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
 
-// Sum over groups of W consecutive lanes (a power of two), in every lane.
-template <int W, class A>
-__device__ inline A lane_sum(A v) {
+// Sum over groups of W consecutive lanes (16 or 64), in every lane, in an
+// order that is the same for all of them. Within a row of 16 lanes the values
+// go through the vector instructions' lane permutations (pairs, quads, halves,
+// the row), and between rows through row exchanges: nothing goes through LDS.
+template <int CTRL>
+__device__ inline float permuted(float v) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// Sum of the wave's four rows, lane by lane.
+__device__ inline float sum_rows(float v) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  const auto rows = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  // (named words: a bit cast of a vector's element takes its first one)
+  const uint32_t even = rows[0], odd = rows[1];
+  v = __builtin_bit_cast(float, even) + __builtin_bit_cast(float, odd);
+  const uint32_t c = __builtin_bit_cast(uint32_t, v);
+  const auto halves = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+  const uint32_t low = halves[0], high = halves[1];
+  return __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
+}
+__device__ inline double sum_rows(double v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+template <int W>
+__device__ inline float lane_sum(float v) {
+  v += permuted<0xb1>(v);   // lanes 1 0 3 2
+  v += permuted<0x4e>(v);   // lanes 2 3 0 1
+  v += permuted<0x141>(v);  // the half row, mirrored
+  v += permuted<0x140>(v);  // the row, mirrored
+  return W > 16 ? sum_rows(v) : v;
+}
+template <int W>
+__device__ inline double lane_sum(double v) {
 #pragma unroll
-  for (int off = W / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
+  for (int off = 1; off < 16; off <<= 1) v += __shfl_xor(v, off, 64);
+  return W > 16 ? sum_rows(v) : v;
 }
 
 }  // namespace

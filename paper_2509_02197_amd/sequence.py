@@ -75,13 +75,12 @@ def _codes():
 
 
 def _code(name, t):
-    import torch
-    if not torch.is_tensor(t):
+    if not hasattr(t, "data_ptr"):
         raise ValueError(f"{name} must be a torch tensor")
-    code = _codes().get(t.dtype)
+    code = (_CODES or _codes()).get(t.dtype)
     if code is None:
         raise TypeError(f"{name} has unsupported dtype {t.dtype}")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU, not {t.device}")
     return code
 
@@ -99,7 +98,7 @@ def _expect(name, t, shape, dtype, device, contiguous=True):
         raise ValueError(f"{name} must be a torch tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, not {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
@@ -133,6 +132,10 @@ def _call(device, stream, inputs, body):
 def _bytes(n, device):
     import torch
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 # -------------------------------------------------------------- recurrence
@@ -180,7 +183,9 @@ def recurrence(a, u, h0=None, lens=None, gate=ADST_GATE_COEFF, want_h=True, want
         hT = torch.empty((B, D), dtype=acc, device=a.device)
         ck = _bytes(info.ck_bytes, a.device) if want_ck else None
         ws = _bytes(info.workspace_bytes, a.device)
-        adst_recurrence_forward(prob, a, u, h0, lens, h, hT, ck, ws, info.workspace_bytes, handle)
+        _check(lib().adst_recurrence_forward(prob, a.data_ptr(), u.data_ptr(), _at(h0), _at(lens),
+                                             _at(h), hT.data_ptr(), _at(ck), _at(ws),
+                                             info.workspace_bytes, handle))
         return {"h": h, "hT": hT, "ck": ck}
 
     return _call(a.device, stream, (a, u, h0, lens), body)
@@ -205,10 +210,13 @@ def recurrence_vjp(a, u, dh, h0=None, lens=None, dhT=None, ck=None, gate=ADST_GA
     need = info.workspace_bytes if ck is not None else info.vjp_workspace_bytes
 
     def body(handle):
-        da, du = (torch.empty((B, T, D), dtype=a.dtype, device=a.device) for _ in range(2))
+        da = torch.empty((B, T, D), dtype=a.dtype, device=a.device)
+        du = torch.empty_like(da)
         dh0 = torch.empty((B, D), dtype=acc, device=a.device)
         ws = _bytes(need, a.device)
-        adst_recurrence_vjp(prob, a, u, h0, lens, ck, dh, dhT, da, du, dh0, ws, need, handle)
+        _check(lib().adst_recurrence_vjp(prob, a.data_ptr(), u.data_ptr(), _at(h0), _at(lens),
+                                         _at(ck), dh.data_ptr(), _at(dhT), da.data_ptr(),
+                                         du.data_ptr(), dh0.data_ptr(), _at(ws), need, handle))
         return {"da": da, "du": du, "dh0": dh0}
 
     return _call(a.device, stream, (a, u, dh, h0, lens, dhT, ck), body)
@@ -235,7 +243,8 @@ def recurrence_step(a, u, state, slots=None, gate=ADST_GATE_COEFF, stream=None):
 
     def body(handle):
         h = torch.empty((B, D), dtype=a.dtype, device=a.device)
-        adst_recurrence_step(prob, a, u, slots, state, state.shape[0], h, handle)
+        _check(lib().adst_recurrence_step(prob, a.data_ptr(), u.data_ptr(), _at(slots),
+                                          state.data_ptr(), state.shape[0], h.data_ptr(), handle))
         return h
 
     return _call(a.device, stream, (a, u, state, slots), body)
@@ -268,7 +277,10 @@ def _norm_problem(x, w, b, eps, dy=None):
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError(f"x must be [..., n] with n >= 1, not {tuple(x.shape)}")
     n = x.shape[-1]
-    rows, sx = _rows("x", x, n)
+    if x.is_contiguous():
+        rows, sx = x.numel() // n, n
+    else:
+        rows, sx = _rows("x", x, n)
     sdy = n
     if dy is not None:
         _expect("dy", dy, x.shape, x.dtype, x.device, contiguous=False)
@@ -295,8 +307,10 @@ def layer_norm(x, w=None, b=None, eps=1e-5, stream=None):
 
     def body(handle):
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean, rstd = (torch.empty(x.shape[:-1], dtype=acc, device=x.device) for _ in range(2))
-        adst_layer_norm_forward(prob, x, w, b, y, mean, rstd, handle)
+        mean = torch.empty(x.shape[:-1], dtype=acc, device=x.device)
+        rstd = torch.empty_like(mean)
+        _check(lib().adst_layer_norm_forward(prob, x.data_ptr(), _at(w), _at(b), y.data_ptr(),
+                                             mean.data_ptr(), rstd.data_ptr(), handle))
         return {"y": y, "mean": mean, "rstd": rstd}
 
     return _call(x.device, stream, (x, w, b), body)
@@ -323,7 +337,9 @@ def layer_norm_vjp(x, dy, mean, rstd, w=None, want_dx=True, want_dw=True, want_d
         db = torch.empty(prob.n, dtype=wt, device=x.device) if want_db else None
         need = adst_layer_norm_workspace_bytes(prob) if want_dw or want_db else 0
         ws = _bytes(need, x.device)
-        adst_layer_norm_vjp(prob, x, dy, w, mean, rstd, dx, dw, db, ws, need, handle)
+        _check(lib().adst_layer_norm_vjp(prob, x.data_ptr(), dy.data_ptr(), _at(w),
+                                         mean.data_ptr(), rstd.data_ptr(), _at(dx), _at(dw),
+                                         _at(db), _at(ws), need, handle))
         return {"dx": dx, "dw": dw, "db": db}
 
     return _call(x.device, stream, (x, dy, mean, rstd, w), body)
@@ -419,11 +435,14 @@ class AdamW:
         if (code == ADST_F64) != (self._prob.dtype == ADST_F64):
             raise TypeError(f"gradients of {self.params[0].dtype} parameters in {dtype}")
         device = self.device
-        for i, g in enumerate(grads):
-            if g.dtype is not dtype or g.device != device or g.numel() != self._numel[i] or \
+        rows = self._rows
+        for i, (g, n, row, p) in enumerate(zip(grads, self._numel, rows, self.params)):
+            if g.dtype is not dtype or g.device != device or g.numel() != n or \
                     not g.is_contiguous():
-                raise ValueError(f"grads[{i}] must be contiguous, of {self._numel[i]} values in "
-                                 f"{dtype} on {device}")
+                raise ValueError(f"grads[{i}] must be contiguous, of {n} values in {dtype} on "
+                                 f"{device}")
+            row.grad = g.data_ptr()
+            row.p = p.data_ptr()
         if grad_scale is not None:
             _expect("grad_scale", grad_scale, grad_scale.shape, torch.float32, device)
             if grad_scale.numel() != 1:
@@ -432,9 +451,6 @@ class AdamW:
             self._set("lr", lr)
         if weight_decay is not None:
             self._set("weight_decay", weight_decay)
-        rows = self._rows
-        for row, p, g in zip(rows, self.params, grads):
-            row.p, row.grad = p.data_ptr(), g.data_ptr()
         if self.copies is not None:
             for row, c in zip(rows, self.copies):
                 row.copy = c.data_ptr()
@@ -443,5 +459,5 @@ class AdamW:
         prob.t = self.t + 1 if t is None else t
         prob.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
         used = () if stream is None else (*self.params, *grads, grad_scale)
-        _call(device, stream, used, lambda handle: adst_adamw(prob, rows, self._n, handle))
+        _call(device, stream, used, lambda handle: _check(lib().adst_adamw(prob, rows, self._n, handle)))
         self.t = prob.t

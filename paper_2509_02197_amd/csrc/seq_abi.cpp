@@ -430,19 +430,27 @@ adst_status adst_adamw(const adst_adamw_problem* prob, const adst_adamw_tensor* 
         (p.bits == 8 && (!aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))) ||
         (t.copy && !aligned(t.copy, ce)))
       return fail(ADST_ERR_ARG, "tensor %d: an array is not aligned to its elements", i);
-    const Wide blocks = (t.n + ADST_STATE_BLOCK - 1) / ADST_STATE_BLOCK;
-    Ranges rs;
-    rs.in("grad", t.grad, Wide(t.n) * ge);
-    rs.in("grad_scale", p.grad_scale, 4);
-    rs.out("p", t.p, Wide(t.n) * e);
-    rs.out("m", t.m, Wide(t.n) * se);
-    rs.out("v", t.v, Wide(t.n) * se);
-    if (p.bits == 8) {
-      rs.out("m_scale", t.m_scale, blocks * 4);
-      rs.out("v_scale", t.v_scale, blocks * 4);
-    }
-    rs.out("copy", t.copy, Wide(t.n) * ce);
-    CHECK(rs.check());
+    // fewer than 2^40 values at a 64-bit address: sums of 64 bits do
+    struct One {
+      const char* name;
+      const void* at;
+      uint64_t bytes;
+    };
+    const uint64_t n = (uint64_t)t.n, scales = (n + ADST_STATE_BLOCK - 1) / ADST_STATE_BLOCK * 4;
+    const One r[8] = {{"p", t.p, n * e},
+                      {"m", t.m, n * se},
+                      {"v", t.v, n * se},
+                      {"copy", t.copy, n * ce},
+                      {"m_scale", p.bits == 8 ? t.m_scale : nullptr, scales},
+                      {"v_scale", p.bits == 8 ? t.v_scale : nullptr, scales},
+                      {"grad", t.grad, n * ge},
+                      {"grad_scale", p.grad_scale, 4}};
+    for (int k = 0; k < 6; ++k)  // what is written overlaps nothing
+      for (int j = k + 1; j < 8; ++j) {
+        const uint64_t x = (uint64_t)(uintptr_t)r[k].at, y = (uint64_t)(uintptr_t)r[j].at;
+        if (x && y && x < y + r[j].bytes && y < x + r[k].bytes)
+          return fail(ADST_ERR_ARG, "tensor %d: %s and %s overlap", i, r[k].name, r[j].name);
+      }
   }
   if (n_tensors == 0) return report_ok();
   return done(adamw(p, tensors, n_tensors, stream), "adamw");

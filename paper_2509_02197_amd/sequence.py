@@ -10,6 +10,9 @@ before anything is launched. A call runs on torch's current stream, or on
 inputs are recorded as used there.
 """
 import ctypes
+from operator import attrgetter
+
+import numpy as np
 
 from . import (ADST_BF16, ADST_F16, ADST_F32, ADST_F64, ADST_GATE_COEFF, ADST_GATE_SIGMOID,
                ADST_STATE_BLOCK, _check, _ptr, _stream, adst_adamw_problem, adst_adamw_tensor,
@@ -346,6 +349,9 @@ def layer_norm_vjp(x, dy, mean, rstd, w=None, want_dx=True, want_dw=True, want_d
 
 
 # ------------------------------------------------------------------- AdamW
+_dtype_of = attrgetter("dtype")
+
+
 class AdamW:
     """AdamW over a list of tensors, one call a step, updated in place.
 
@@ -405,6 +411,8 @@ class AdamW:
         self._n = n
         self._numel = [p.numel() for p in self.params]
         self._rows = (adst_adamw_tensor * n)()
+        # the same memory as 8-byte words: p, grad, m, v, m_scale, v_scale, copy, n, lr, decay
+        self._words = np.frombuffer(self._rows, dtype=np.uint64).reshape(n, -1)
         for i, row in enumerate(self._rows):
             for name in names:
                 setattr(row, name, getattr(self, name)[i].data_ptr())
@@ -430,19 +438,22 @@ class AdamW:
         import torch
         if len(grads) != self._n:
             raise ValueError(f"{len(grads)} gradients for {self._n} parameters")
-        dtype = grads[0].dtype
         code = _code("grads[0]", grads[0])
         if (code == ADST_F64) != (self._prob.dtype == ADST_F64):
-            raise TypeError(f"gradients of {self.params[0].dtype} parameters in {dtype}")
-        device = self.device
+            raise TypeError(f"gradients of {self.params[0].dtype} parameters in {grads[0].dtype}")
+        device, kind = self.device, torch.Tensor
+        if set(map(_dtype_of, grads)) != {grads[0].dtype} or \
+                set(map(kind.get_device, grads)) != {device.index} or \
+                list(map(kind.numel, grads)) != self._numel or \
+                not all(map(kind.is_contiguous, grads)):
+            for i, (g, n) in enumerate(zip(grads, self._numel)):
+                if g.dtype != grads[0].dtype or g.device != device or g.numel() != n or \
+                        not g.is_contiguous():
+                    raise ValueError(f"grads[{i}] must be contiguous, of {n} values in "
+                                     f"{grads[0].dtype} on {device}")
         rows = self._rows
-        for i, (g, n, row, p) in enumerate(zip(grads, self._numel, rows, self.params)):
-            if g.dtype is not dtype or g.device != device or g.numel() != n or \
-                    not g.is_contiguous():
-                raise ValueError(f"grads[{i}] must be contiguous, of {n} values in {dtype} on "
-                                 f"{device}")
-            row.grad = g.data_ptr()
-            row.p = p.data_ptr()
+        self._words[:, 0] = list(map(kind.data_ptr, self.params))
+        self._words[:, 1] = list(map(kind.data_ptr, grads))
         if grad_scale is not None:
             _expect("grad_scale", grad_scale, grad_scale.shape, torch.float32, device)
             if grad_scale.numel() != 1:
@@ -452,8 +463,7 @@ class AdamW:
         if weight_decay is not None:
             self._set("weight_decay", weight_decay)
         if self.copies is not None:
-            for row, c in zip(rows, self.copies):
-                row.copy = c.data_ptr()
+            self._words[:, 6] = list(map(kind.data_ptr, self.copies))
         prob = self._prob
         prob.grad_dtype = code
         prob.t = self.t + 1 if t is None else t

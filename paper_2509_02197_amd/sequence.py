@@ -97,6 +97,14 @@ def _acc(code):
 def _expect(name, t, shape, dtype, device, contiguous=True):
     if t is None:
         return
+    try:  # what a right tensor passes at once
+        if t.dtype is dtype and t.shape == shape and t.device == device and \
+                (not contiguous or t.is_contiguous()):
+            return
+    except AttributeError:
+        pass
+    if isinstance(name, tuple):
+        name = "{}[{}]".format(*name)
     if not hasattr(t, "data_ptr"):
         raise ValueError(f"{name} must be a torch tensor")
     if t.dtype != dtype:
@@ -110,14 +118,14 @@ def _expect(name, t, shape, dtype, device, contiguous=True):
 
 
 def _channels_contiguous(name, t):
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}'s last axis must be contiguous (stride 1, not {t.stride(-1)})")
 
 
 def _call(device, stream, inputs, body):
     """body(stream handle) on the tensors' device, allocations of body included."""
     import torch
-    if stream is None and torch.cuda.current_device() == device.index:
+    if stream is None and torch._C._cuda_getDevice() == device.index:
         return body(torch._C._cuda_getCurrentRawStream(device.index))
     with torch.cuda.device(device):
         if stream is None:
@@ -182,7 +190,7 @@ def recurrence(a, u, h0=None, lens=None, gate=ADST_GATE_COEFF, want_h=True, want
     info = adst_recurrence_plan(prob)
 
     def body(handle):
-        h = torch.empty((B, T, D), dtype=a.dtype, device=a.device) if want_h else None
+        h = torch.empty_like(a, memory_format=torch.contiguous_format) if want_h else None
         hT = torch.empty((B, D), dtype=acc, device=a.device)
         ck = _bytes(info.ck_bytes, a.device) if want_ck else None
         ws = _bytes(info.workspace_bytes, a.device)
@@ -213,7 +221,7 @@ def recurrence_vjp(a, u, dh, h0=None, lens=None, dhT=None, ck=None, gate=ADST_GA
     need = info.workspace_bytes if ck is not None else info.vjp_workspace_bytes
 
     def body(handle):
-        da = torch.empty((B, T, D), dtype=a.dtype, device=a.device)
+        da = torch.empty_like(a, memory_format=torch.contiguous_format)
         du = torch.empty_like(da)
         dh0 = torch.empty((B, D), dtype=acc, device=a.device)
         ws = _bytes(need, a.device)
@@ -245,7 +253,7 @@ def recurrence_step(a, u, state, slots=None, gate=ADST_GATE_COEFF, stream=None):
     prob = adst_recurrence_problem(code, gate, B, 1, D, a.stride(0), 0, u.stride(0), 0, 0, 0)
 
     def body(handle):
-        h = torch.empty((B, D), dtype=a.dtype, device=a.device)
+        h = torch.empty_like(a, memory_format=torch.contiguous_format)
         _check(lib().adst_recurrence_step(prob, a.data_ptr(), u.data_ptr(), _at(slots),
                                           state.data_ptr(), state.shape[0], h.data_ptr(), handle))
         return h
@@ -291,10 +299,10 @@ def _norm_problem(x, w, b, eps, dy=None):
     wcode = code
     given = w if w is not None else b
     if given is not None:
-        wcode = _code("w" if w is not None else "b", given)
+        wcode = (_CODES or _codes()).get(getattr(given, "dtype", None), -1)
         if wcode != code and not (code in (ADST_BF16, ADST_F16) and wcode == ADST_F32):
             raise ValueError(f"weights must be {x.dtype} (or float32 beside 16-bit types), "
-                             f"not {given.dtype}")
+                             f"not {getattr(given, 'dtype', type(given))}")
         _expect("w", w, (n,), given.dtype, x.device)
         _expect("b", b, (n,), given.dtype, x.device)
     return adst_norm_problem(code, wcode, rows, n, sx, sdy, eps)
@@ -309,7 +317,7 @@ def layer_norm(x, w=None, b=None, eps=1e-5, stream=None):
     acc = _acc(prob.dtype)
 
     def body(handle):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
         mean = torch.empty(x.shape[:-1], dtype=acc, device=x.device)
         rstd = torch.empty_like(mean)
         _check(lib().adst_layer_norm_forward(prob, x.data_ptr(), _at(w), _at(b), y.data_ptr(),
@@ -335,7 +343,7 @@ def layer_norm_vjp(x, dy, mean, rstd, w=None, want_dx=True, want_dw=True, want_d
     wt = w.dtype if w is not None else x.dtype
 
     def body(handle):
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format) if want_dx else None
         dw = torch.empty(prob.n, dtype=wt, device=x.device) if want_dw else None
         db = torch.empty(prob.n, dtype=wt, device=x.device) if want_db else None
         need = adst_layer_norm_workspace_bytes(prob) if want_dw or want_db else 0
@@ -378,7 +386,10 @@ class AdamW:
                             f"not {first.dtype}")
         self.device = first.device
         for i, p in enumerate(self.params):
-            _expect(f"params[{i}]", p, getattr(p, "shape", ()), first.dtype, self.device)
+            if not hasattr(p, "shape"):
+                raise ValueError(f"params[{i}] must be a torch tensor")
+            if p.dtype is not first.dtype or p.device != self.device or not p.is_contiguous():
+                _expect(f"params[{i}]", p, p.shape, first.dtype, self.device)
         self.copies = None if copies is None else tuple(copies)
         copy_code = ADST_BF16
         if self.copies is not None:
@@ -388,8 +399,9 @@ class AdamW:
                 copy_code = _code("copies[0]", self.copies[0])
                 if copy_code == ADST_F64:
                     raise TypeError("copies must be float32, bfloat16 or float16")
+            kind = self.copies[0].dtype if n else None
             for i, (c, p) in enumerate(zip(self.copies, self.params)):
-                _expect(f"copies[{i}]", c, p.shape, self.copies[0].dtype, self.device)
+                _expect(("copies", i), c, p.shape, kind, self.device)
         self.bits = bits
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
         self.t = 0
@@ -406,17 +418,17 @@ class AdamW:
                 if len(held) != n:
                     raise ValueError(f"{len(held)} tensors of state {name} for {n} parameters")
                 for i, (t, s) in enumerate(zip(held, shapes)):
-                    _expect(f"{name}[{i}]", t, s, dtype, self.device)
+                    _expect((name, i), t, s, dtype, self.device)
             setattr(self, name, held)
         self._n = n
         self._numel = [p.numel() for p in self.params]
         self._rows = (adst_adamw_tensor * n)()
         # the same memory as 8-byte words: p, grad, m, v, m_scale, v_scale, copy, n, lr, decay
         self._words = np.frombuffer(self._rows, dtype=np.uint64).reshape(n, -1)
-        for i, row in enumerate(self._rows):
-            for name in names:
-                setattr(row, name, getattr(self, name)[i].data_ptr())
-            row.n = self._numel[i]
+        for name, word in zip(("m", "v", "m_scale", "v_scale"), range(2, 6)):
+            if name in names:
+                self._words[:, word] = [t.data_ptr() for t in getattr(self, name)]
+        self._words[:, 7] = self._numel
         self._set("lr", lr)
         self._set("weight_decay", weight_decay)
         self._prob = adst_adamw_problem(code, ADST_F32, copy_code, bits, 0, *self.betas, self.eps,
@@ -427,8 +439,7 @@ class AdamW:
         if len(values) != self._n:
             raise ValueError(f"{len(values)} values of {name} for {self._n} parameters")
         setattr(self, name, value)
-        for row, x in zip(self._rows, values):
-            setattr(row, name, float(x))
+        self._words.view(np.float64)[:, 8 if name == "lr" else 9] = values
 
     def step(self, grads, lr=None, weight_decay=None, t=None, grad_scale=None, stream=None):
         """One step with contiguous gradients like params (float32, bfloat16 or float16, one

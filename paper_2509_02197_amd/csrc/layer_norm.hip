@@ -569,9 +569,9 @@ constexpr int kParts = 512, kLongParts = 128;
 int parts_of(int32_t dtype, int64_t rows, int64_t nv) {
   // rows that the VJP's workgroups take at a time (reverse_by_length)
   const int64_t at_once = nv <= 16 ? 64 : nv <= 64 ? 32 : nv <= 128 ? 16
-                          : nv <= 512 ? 4 : 1;
+                          : nv <= 512 ? 4 : nv <= 1024 ? 2 : 1;
   const int64_t all = (rows + at_once - 1) / at_once;
-  const int64_t most = nv > held_in_vjp(dtype) ? kLongParts : nv > 1024 ? kParts / 2 : kParts;
+  const int64_t most = nv > held_in_vjp(dtype) ? kLongParts : nv > 256 ? kParts / 2 : kParts;
   return (int)(all < most ? all : most);
 }
 
@@ -594,8 +594,8 @@ void reverse_by_length(const NormArgs& a, int64_t nv, int parts, Acc<T>* part, h
   else if (nv <= 64) reverse<T, W, 512, 64, 1, 4>(a, g, part, st);
   else if (nv <= 128) reverse<T, W, 512, 64, 2, 2>(a, g, part, st);
   else if (nv <= 256) reverse<T, W, 512, 256, 1, 2>(a, g, part, st);
-  else if (nv <= 512) reverse<T, W, 512, 256, 2, 2>(a, g, part, st);
-  else if (nv <= 1024) reverse<T, W, 512, 512, 2, 1>(a, g, part, st);
+  else if (nv <= 512) reverse<T, W, 1024, 512, 1, 2>(a, g, part, st);
+  else if (nv <= 1024) reverse<T, W, 1024, 512, 2, 1>(a, g, part, st);
   else if (nv <= 2048) reverse<T, W, 512, 512, 4, 1>(a, g, part, st);
   else if (nv <= held_in_vjp(a.dtype)) {
     if constexpr (sizeof(T) == 4) reverse<T, W, 1024, 1024, 4, 1>(a, g, part, st);

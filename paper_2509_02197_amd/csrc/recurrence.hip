@@ -768,10 +768,12 @@ __global__ __launch_bounds__(kStepThreads) void rec_one(RecStep q, int64_t per_r
   if (q.h) store_part((T*)q.h + b * q.D + d, out, n);
 }
 
-constexpr int kFillThreads = 256;
+constexpr int kFillThreads = 256, kFillEach = 4;
 __global__ __launch_bounds__(kFillThreads) void fill_ones(uint4* p, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * kFillThreads + threadIdx.x;
-  if (i < n) p[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
+  const int64_t i = (int64_t)blockIdx.x * (kFillThreads * kFillEach) + threadIdx.x;
+#pragma unroll
+  for (int k = 0; k < kFillEach; ++k)
+    if (i + k * kFillThreads < n) p[i + k * kFillThreads] = make_uint4(~0u, ~0u, ~0u, ~0u);
 }
 
 // -------------------------------------------------------------- on the host
@@ -879,8 +881,8 @@ hipError_t sweep(const RecArgs& q, void* ws, hipStream_t st) {
   int64_t bytes;
   const Board bd = board_of(q.dtype, g, ws, &bytes);
   if (bytes) {
-    const int64_t n = bytes / 16;
-    fill_ones<<<(unsigned)((n + kFillThreads - 1) / kFillThreads), kFillThreads, 0, st>>>(
+    const int64_t n = bytes / 16, each = kFillThreads * kFillEach;
+    fill_ones<<<(unsigned)((n + each - 1) / each), kFillThreads, 0, st>>>(
         static_cast<uint4*>(ws), n);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

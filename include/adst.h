@@ -1,5 +1,6 @@
 /* adst.h — reverse-mode gradients of time-iterated stencil programs under a
- * checkpoint-memory budget, on AMD MI355X (gfx950).
+ * checkpoint-memory budget, on AMD MI355X (gfx950); and the time loop of a
+ * sequence layer with its gradients (the section "Sequence operators").
  *
  * The operation (DaCe AD, arXiv 2509.02197): given an unmodified time loop
  *     x_t = F(x_{t-1}; K),  t = 1..T,

@@ -1,7 +1,8 @@
 """adst: reverse-mode gradients of time-iterated stencils under a checkpoint
 memory budget, on AMD MI355X (gfx950).
 
-Thin ctypes binding of ``libadst.so`` (declared in ``include/adst.h``). The
+Thin ctypes binding of ``libadst.so`` (declared in ``include/adst.h``; the
+sequence operators are in ``sequence.py``). The
 functions keep the C names and only marshal arguments: tensors become device
 pointers, the stream defaults to torch's current stream. Every step of the
 path runs in the library's HIP kernels; there is no Python or CPU fallback,

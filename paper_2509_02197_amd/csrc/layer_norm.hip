@@ -456,6 +456,7 @@ __global__ __launch_bounds__(kColumnThreads) void norm_dw_long(NormArgs p, Acc<T
   A sw[V], sb[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) sw[i] = sb[i] = A(0);
+#pragma unroll 4
   for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
     const Vec<T> v = load_part((const T*)p.x + row * p.sx + c, n);
     const Vec<T> d = load_part((const T*)p.dy + row * p.sdy + c, n);
@@ -628,7 +629,8 @@ hipError_t norm_forward(const NormArgs& a, hipStream_t st) {
 }
 
 uint64_t norm_workspace_bytes(int32_t dtype, int64_t rows, int64_t n) {
-  return 2ull * parts_of(dtype, rows, vectors_of(dtype, n)) * (uint64_t)n * (dtype == ADST_F64 ? 8 : 4);
+  const uint64_t parts = (uint64_t)parts_of(dtype, rows, vectors_of(dtype, n));
+  return 2 * parts * (uint64_t)n * (dtype == ADST_F64 ? 8 : 4);
 }
 
 hipError_t norm_vjp(const NormArgs& a, void* ws, hipStream_t st) {

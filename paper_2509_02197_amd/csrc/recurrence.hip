@@ -6,14 +6,23 @@
 // (A', H') is (A A', A H' + H). So a row is cut into spans, a workgroup each:
 // it loads its span once, composes its steps, learns the state at its start
 // from the spans before it, and applies its steps to that. Everything is read
-// and written once, and HBM bandwidth bounds it. A workgroup's lanes lie along
-// channels (16 lanes of 16 bytes: 256 consecutive bytes of a step) and its
-// groups of 16 lanes along time, each with R consecutive steps in registers;
-// maps are composed within a lane, over the wave by lane shifts, and over the
-// waves through LDS. The reverse sweep is the same recurrence backwards
+// and written once, and HBM bandwidth bounds it. A wave's lanes lie along
+// channels (256 consecutive bytes of a step) and each lane holds 16 consecutive
+// steps of its channels in registers, so maps are composed within a lane, and
+// over the waves through LDS; a wave needs no exchange between its lanes.
+// (Lanes of 16 bytes with their maps composed across the wave took 100 us
+// forward and 191 in reverse at 8 x 4096 x 2048 bf16, against 90 and 138: more
+// registers for the maps, and a third more instructions.) Where channels are
+// few, rows of 16 lanes lie along channels and the wave's four rows along time.
+// The reverse sweep is the same recurrence backwards
 // (G_t = dh_t + c_{t+1} G_{t+1}); it recomputes its span's states in registers
 // from the checkpoint at its start, so the forward's h is not needed: reading
 // a, u and dh and writing da and du is all it moves.
+//
+// Measured, bf16 SIGMOID on halves of one projection: 8 x 4096 x 2048 forward
+// 90 us (4.5 TB/s), reverse 138 us (4.9 TB/s); 1 x 65536 x 1024 forward 106 us,
+// reverse 176. Without the waits between spans the first would take 85 and 136,
+// the second 83 and 133; the fill of the board is 3 to 5 us of each.
 //
 // Between spans: a workgroup publishes its span's map (A, H) as soon as it has
 // it. Eight spans form a group; a group's last workgroup also publishes the
@@ -85,7 +94,10 @@ struct Shape {
   static constexpr int kSpan = W * kWaveSteps;   // a workgroup's steps
   typedef Pack<T, V> P;
 };
-constexpr int kForward = 512, kReverse = 256;  // threads of a workgroup on long rows
+// Threads of a workgroup on long rows. Forward: 512 (8 x 4096 x 2048 bf16 90 us,
+// 94 with 256; 1 x 65536 x 1024 106 and 137). Reverse, which needs more
+// registers: 256 (138 us, 156 with 512; the longer row 176 and 161).
+constexpr int kForward = 512, kReverse = 256;
 constexpr int kCkWaves = 4;  // a checkpoint at every fourth wave's steps
 
 // How a problem is laid out over workgroups of `threads`.
@@ -675,7 +687,8 @@ __global__ __launch_bounds__(NT, 3) void rec_rev(RecArgs q, Grid g, Board bd) {
     const int64_t ch = (int64_t)at.slab * C + k;
     const bool mine = k < C && ch < q.D;
     // asked for before the wait
-    const A first = mine ? ((const A*)q.ck)[(at.b * g.cks + at.span * S::W / kCkWaves) * q.D + ch] : A(0);
+    const int64_t check = at.b * g.cks + at.span * S::W / kCkWaves;
+    const A first = mine ? ((const A*)q.ck)[check * q.D + ch] : A(0);
     // the sweep begins at the row's last span, where dhT enters
     const int last = at.len > 0 ? (int)((at.len - 1) / S::kSpan) : 0;
     A x = mine && q.dhT ? ((const A*)q.dhT)[at.b * q.D + ch] : A(0);
@@ -782,7 +795,9 @@ int type_size(int32_t dtype) { return dtype == ADST_F64 ? 8 : dtype == ADST_F32 
 int lane_channels(int32_t dtype) { return dtype == ADST_F64 || dtype == ADST_F32 ? 1 : 2; }
 int lane_steps(int32_t dtype) { return dtype == ADST_F64 ? 8 : 16; }
 
-// Lanes along channels: all 64 where that leaves few without one, else 16.
+// Lanes along channels: all 64 where that leaves few without one, else 16
+// (64 x 30000 x 7 f32: 93 us forward and 106 in reverse with 16, 274 and 293
+// with 64; 1 x 4096 x 64 bf16 8.7 and 10.1 us against 14.0 and 18.7).
 int lanes_of(int32_t dtype, int64_t D) {
   const int64_t C = 64 * lane_channels(dtype), all = (D + C - 1) / C * C;
   return 4 * (all - D) <= all ? 64 : 16;
@@ -835,7 +850,9 @@ void launch(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
 }
 
 // Non-temporal loads and stores for calls that move more than the caches keep,
-// on arrays whose rows are whole cache lines.
+// on arrays whose rows are whole cache lines (8 x 4096 x 2048 bf16: reverse 148
+// us with them, 163 without; rows off the lines, whose shared lines then leave
+// the cache between two workgroups, 5 x 2049 x 771 f32: 59 and 47).
 constexpr int64_t kStreamBytes = int64_t(128) << 20, kLine = 128;
 bool streams(const RecArgs& q, bool forward) {
   const int64_t e = type_size(q.dtype);

@@ -150,7 +150,8 @@ adst_status check_norm(const adst_norm_problem* p) {
     return fail(ADST_ERR_ARG, "weight_dtype must be the dtype, or F32 beside BF16 and F16");
   if (p->rows < 0 || p->n < 1) return fail(ADST_ERR_ARG, "rows must be >= 0 and n >= 1");
   if (p->stride_x < 0 || p->stride_dy < 0) return fail(ADST_ERR_ARG, "strides must be >= 0");
-  if (!std::isfinite(p->eps) || p->eps < 0) return fail(ADST_ERR_ARG, "eps must be finite and >= 0");
+  if (!std::isfinite(p->eps) || p->eps < 0)
+    return fail(ADST_ERR_ARG, "eps must be finite and >= 0");
   if (p->rows >= kMost || p->n >= kMost)
     return fail(ADST_ERR_UNSUPPORTED, "rows and n must be below 2^31 - 2^16");
   return ADST_OK;

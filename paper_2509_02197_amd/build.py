@@ -1,13 +1,15 @@
 """Build step for libadst.so (gfx950).
 
 Host sources are compiled as C++ and the kernels as HIP, all with hipcc,
-then linked into ``libadst.so`` inside the package directory. Every compile
-uses -ffp-contract=off (the forward steps are bit-reproducible in the
+then linked into ``libadst.so`` inside the package directory; beside it
+``_binding.so``, which takes torch tensors to its calls. Every compile of the
+library uses -ffp-contract=off (the forward steps are bit-reproducible in the
 documented evaluation order) and disables packed-fp32 instructions.
 """
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -15,6 +17,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libadst.so")
+BINDING = os.path.join(HERE, "_binding.so")
 ARCH = "gfx950"
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
@@ -46,10 +49,30 @@ def _run(cmd, verbose):
     return r
 
 
+def _binding_commands():
+    """Compile and link of the binding, whose headers and libraries are torch's."""
+    import torch
+    torch_dir = os.path.dirname(torch.__file__)
+    obj = os.path.join(BUILD, "binding.cpp.o")
+    compile_ = ["g++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+                "-D_GLIBCXX_USE_CXX11_ABI=" + str(int(torch._C._GLIBCXX_USE_CXX11_ABI)),
+                "-I" + os.path.join(ROOT, "include"),
+                "-isystem", sysconfig.get_paths()["include"],
+                "-isystem", os.path.join(torch_dir, "include"),
+                "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+                "-isystem", os.path.join(ROCM, "include"),
+                "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj]
+    link = ["g++", "-shared", "-o", BINDING + ".tmp", obj, LIB,
+            "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip",
+            "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(torch_dir, "lib")]
+    return compile_, link
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     hipcc = _hipcc()
-    jobs = []
+    compile_binding, link_binding = _binding_commands()
+    jobs = [compile_binding]
     for s in HOST_SOURCES:
         jobs.append([hipcc, "-x", "c++", "-D__HIP_PLATFORM_AMD__=1",
                      "-I" + os.path.join(ROCM, "include")] + COMMON +
@@ -64,6 +87,8 @@ def build(verbose: bool = False) -> str:
          ["-L" + os.path.join(ROCM, "lib"), "-lrocprofiler-sdk-roctx",
           "-Wl,-rpath," + os.path.join(ROCM, "lib")], verbose)
     os.replace(LIB + ".tmp", LIB)
+    _run(link_binding, verbose)
+    os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 

@@ -10,10 +10,12 @@ before anything is launched. A call runs on torch's current stream, or on
 inputs are recorded as used there.
 """
 import ctypes
+import os
 from operator import attrgetter
 
 import numpy as np
 
+from . import build as _build
 from . import (ADST_BF16, ADST_F16, ADST_F32, ADST_F64, ADST_GATE_COEFF, ADST_GATE_SIGMOID,
                ADST_STATE_BLOCK, _check, _ptr, _stream, adst_adamw_problem, adst_adamw_tensor,
                adst_norm_problem, adst_recurrence_info, adst_recurrence_problem, lib)
@@ -65,6 +67,23 @@ def adst_adamw(prob, tensors, n, stream=None):
 
 
 # ------------------------------------------------------------------ checks
+_BINDING = None
+
+
+def _binding():
+    """The native form of this file's ordinary calls (csrc/binding.cpp): it answers None to
+    anything else, which the code here then handles."""
+    global _BINDING
+    if _BINDING is None:
+        import torch  # noqa: F401  (whose libraries the binding is linked with)
+        lib()
+        if not os.path.exists(_build.BINDING):
+            _build.build()
+        from . import _binding as module
+        _BINDING = module
+    return _BINDING
+
+
 _CODES = None
 
 
@@ -181,6 +200,10 @@ def recurrence(a, u, h0=None, lens=None, gate=ADST_GATE_COEFF, want_h=True, want
     [batch] int32: the steps of each row. a and u may have any strides with contiguous
     channels. Returns a dict: h (None unless want_h), hT the last states, and ck (None unless
     want_ck) the checkpoints with which recurrence_vjp recomputes the states."""
+    if stream is None:
+        done = _binding().recurrence(a, u, h0, lens, gate, want_h, want_ck)
+        if done is not None:
+            return done
     import torch
     prob = _recurrence_problem(a, u, gate)
     B, T, D = a.shape
@@ -207,6 +230,10 @@ def recurrence_vjp(a, u, dh, h0=None, lens=None, dhT=None, ck=None, gate=ADST_GA
     """The VJP of recurrence: dh = dL/dh, dhT = dL/dhT (optional). ck: the checkpoints that
     recurrence gave for the same a, u, h0, lens and gate; None recomputes them, at the price of
     one more pass over a and u. Returns a dict: da, du [batch, steps, channels] and dh0."""
+    if stream is None:
+        done = _binding().recurrence_vjp(a, u, dh, h0, lens, dhT, ck, gate)
+        if done is not None:
+            return done
     import torch
     if dh is None:
         raise ValueError("dh is required")
@@ -238,6 +265,10 @@ def recurrence_step(a, u, state, slots=None, gate=ADST_GATE_COEFF, stream=None):
     [nstates, channels] (float32, float64 for float64 inputs), updated in place. slots [batch]
     int32: each row's state, no two the same; None: row b's is state[b]. Rows whose slot is
     outside the pool are idle: their h is 0. Returns h [batch, channels]."""
+    if stream is None:
+        h = _binding().recurrence_step(a, u, state, slots, gate)
+        if h is not None:
+            return h
     import torch
     code = _code("a", a)
     if a.dim() != 2:
@@ -312,6 +343,10 @@ def layer_norm(x, w=None, b=None, eps=1e-5, stream=None):
     """Layer norm over the last axis of x [..., n]; w and b [n] of x's dtype, or float32 beside
     16-bit types. Returns a dict: y (contiguous), and mean and rstd of each row (float32, or
     float64 for float64) for layer_norm_vjp."""
+    if stream is None:
+        done = _binding().layer_norm(x, w, b, eps)
+        if done is not None:
+            return done
     import torch
     prob = _norm_problem(x, w, b, eps)
     acc = _acc(prob.dtype)
@@ -331,6 +366,10 @@ def layer_norm_vjp(x, dy, mean, rstd, w=None, want_dx=True, want_dw=True, want_d
                    stream=None):
     """The VJP of layer_norm: mean and rstd as it gave them. Returns a dict: dx [..., n]
     (contiguous), dw and db [n] in w's dtype (x's without w), each None unless wanted."""
+    if stream is None:
+        done = _binding().layer_norm_vjp(x, dy, mean, rstd, w, want_dx, want_dw, want_db)
+        if done is not None:
+            return done
     import torch
     if dy is None:
         raise ValueError("dy is required")
@@ -433,6 +472,7 @@ class AdamW:
         self._set("weight_decay", weight_decay)
         self._prob = adst_adamw_problem(code, ADST_F32, copy_code, bits, 0, *self.betas, self.eps,
                                         None)
+        self._addresses = ctypes.addressof(self._prob), ctypes.addressof(self._rows)
 
     def _set(self, name, value):
         values = [value] * self._n if isinstance(value, (int, float)) else list(value)
@@ -446,6 +486,16 @@ class AdamW:
         dtype; float64 for float64). lr, weight_decay: from now on. t: the step's number, one more
         than the last one's if None. grad_scale: a float32 tensor of one value that multiplies the
         gradients; where it is not finite nothing is updated (the step's number counts on)."""
+        if lr is not None:
+            self._set("lr", lr)
+        if weight_decay is not None:
+            self._set("weight_decay", weight_decay)
+        if t is None:
+            t = self.t + 1
+        if stream is None and _binding().adamw_step(*self._addresses, self.params, grads,
+                                                    self.copies, grad_scale, t):
+            self.t = t
+            return
         import torch
         if len(grads) != self._n:
             raise ValueError(f"{len(grads)} gradients for {self._n} parameters")
@@ -469,16 +519,13 @@ class AdamW:
             _expect("grad_scale", grad_scale, grad_scale.shape, torch.float32, device)
             if grad_scale.numel() != 1:
                 raise ValueError("grad_scale must have one value")
-        if lr is not None:
-            self._set("lr", lr)
-        if weight_decay is not None:
-            self._set("weight_decay", weight_decay)
         if self.copies is not None:
             self._words[:, 6] = list(map(kind.data_ptr, self.copies))
         prob = self._prob
         prob.grad_dtype = code
-        prob.t = self.t + 1 if t is None else t
+        prob.t = t
         prob.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
         used = () if stream is None else (*self.params, *grads, grad_scale)
-        _call(device, stream, used, lambda handle: _check(lib().adst_adamw(prob, rows, self._n, handle)))
+        _call(device, stream, used,
+              lambda handle: _check(lib().adst_adamw(prob, rows, self._n, handle)))
         self.t = prob.t

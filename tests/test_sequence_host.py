@@ -206,3 +206,20 @@ def test_tensors_of_other_types():
         adst.layer_norm([1.0, 2.0])
     with pytest.raises(ValueError):
         adst.AdamW([])
+
+
+def test_the_native_calls_answer_none_to_anything_unusual():
+    """sequence.py then handles it, or raises its error; no exception leaves the binding."""
+    b = adst.sequence._binding()
+    x, w = torch.zeros(4, 8), torch.zeros(8)
+    h = torch.zeros(2, 3, 8)
+    for call in (lambda: b.layer_norm(x, w, w, 1e-5), lambda: b.layer_norm(x, w, w, "eps"),
+                 lambda: b.layer_norm(), lambda: b.layer_norm(1, 2, 3, 4),
+                 lambda: b.layer_norm_vjp(x, x, None, None, None, 1, 1, 1),
+                 lambda: b.recurrence(h, h, None, None, 0, True, True),
+                 lambda: b.recurrence(h, h, None, None, 1.5, True, True),
+                 lambda: b.recurrence_vjp(h, h, h, None, None, None, None, 0),
+                 lambda: b.recurrence_step(x, x, x, None, 0),
+                 lambda: b.adamw_step(0, 0, (), [], None, None, 1),
+                 lambda: b.adamw_step(None, None, (x,), [x], None, None, 1)):
+        assert call() is None

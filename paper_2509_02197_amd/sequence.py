@@ -136,6 +136,23 @@ def _expect(name, t, shape, dtype, device, contiguous=True):
         raise ValueError(f"{name} must be contiguous")
 
 
+def _expect_all(name, tensors, shapes, dtype, device):
+    """_expect for a list: what a right list passes at once, then one by one for the message."""
+    import torch
+    kind = torch.Tensor
+    try:
+        if list(map(_shape_of, tensors)) == shapes and set(map(_dtype_of, tensors)) == {dtype} and \
+                set(map(kind.get_device, tensors)) == {device.index} and \
+                all(map(kind.is_contiguous, tensors)):
+            return
+    except (AttributeError, TypeError):
+        pass
+    for i, (t, shape) in enumerate(zip(tensors, shapes)):
+        if t is None:
+            raise ValueError(f"{name}[{i}] must be a torch tensor")
+        _expect((name, i), t, shape, dtype, device)
+
+
 def _channels_contiguous(name, t):
     if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}'s last axis must be contiguous (stride 1, not {t.stride(-1)})")
@@ -396,7 +413,7 @@ def layer_norm_vjp(x, dy, mean, rstd, w=None, want_dx=True, want_dw=True, want_d
 
 
 # ------------------------------------------------------------------- AdamW
-_dtype_of = attrgetter("dtype")
+_dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
 
 
 class AdamW:
@@ -427,8 +444,8 @@ class AdamW:
         for i, p in enumerate(self.params):
             if not hasattr(p, "shape"):
                 raise ValueError(f"params[{i}] must be a torch tensor")
-            if p.dtype is not first.dtype or p.device != self.device or not p.is_contiguous():
-                _expect(f"params[{i}]", p, p.shape, first.dtype, self.device)
+        shapes = list(map(_shape_of, self.params))
+        _expect_all("params", self.params, shapes, first.dtype, self.device)
         self.copies = None if copies is None else tuple(copies)
         copy_code = ADST_BF16
         if self.copies is not None:
@@ -439,28 +456,26 @@ class AdamW:
                 if copy_code == ADST_F64:
                     raise TypeError("copies must be float32, bfloat16 or float16")
             kind = self.copies[0].dtype if n else None
-            for i, (c, p) in enumerate(zip(self.copies, self.params)):
-                _expect(("copies", i), c, p.shape, kind, self.device)
+            _expect_all("copies", self.copies, shapes, kind, self.device)
         self.bits = bits
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
         self.t = 0
+        self._numel = [p.numel() for p in self.params]
+        blocks = [(-(-k // ADST_STATE_BLOCK),) for k in self._numel]
         names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
         for name in names:
-            shapes = [(-(-p.numel() // ADST_STATE_BLOCK),) if name.endswith("scale") else p.shape
-                      for p in self.params]
+            needed = blocks if name.endswith("scale") else shapes
             dtype = (torch.float32 if name.endswith("scale") else
                      torch.float8_e4m3fn if bits == 8 else first.dtype)
             if state is None:
-                held = tuple(torch.zeros(s, dtype=dtype, device=self.device) for s in shapes)
+                held = tuple(torch.zeros(s, dtype=dtype, device=self.device) for s in needed)
             else:
                 held = tuple(state[name])
                 if len(held) != n:
                     raise ValueError(f"{len(held)} tensors of state {name} for {n} parameters")
-                for i, (t, s) in enumerate(zip(held, shapes)):
-                    _expect((name, i), t, s, dtype, self.device)
+                _expect_all(name, held, needed, dtype, self.device)
             setattr(self, name, held)
         self._n = n
-        self._numel = [p.numel() for p in self.params]
         self._rows = (adst_adamw_tensor * n)()
         # the same memory as 8-byte words: p, grad, m, v, m_scale, v_scale, copy, n, lr, decay
         self._words = np.frombuffer(self._rows, dtype=np.uint64).reshape(n, -1)

@@ -151,6 +151,16 @@ def test_rows_and_channels_are_independent(gate):
     assert torch.equal(two["da"][~hit], one["da"][~hit])
 
 
+@pytest.mark.parametrize("B", [3, 4, 5, 9, 33])
+def test_a_row_is_the_same_alone(B):
+    """Whatever the number of rows, and so of the workgroups' chains and where they run."""
+    s = make(B, 900, 250, torch.bfloat16, SIGMOID, seed=B)
+    got = run(s, SIGMOID)
+    for b in (0, B // 2, B - 1):
+        one = run({k: None if v is None else v[b:b + 1] for k, v in s.items()}, SIGMOID)
+        assert all(torch.equal(got[k][b:b + 1], one[k]) for k in one)
+
+
 def test_extreme_gates():
     """Gates at and beyond the type's range: 0 and 1 exactly, no NaN."""
     z = torch.tensor([-1e30, -200.0, -90.0, 0.0, 90.0, 200.0, 1e30, float("inf"), -float("inf")])

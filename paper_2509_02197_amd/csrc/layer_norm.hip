@@ -10,8 +10,14 @@
 // workgroup's rows, and so do, in the VJP, the sums of dw and db of the
 // group's columns; each workgroup writes its sums once, and a second kernel
 // adds those of all workgroups. Their number, and so the order of all sums,
-// depends on the sizes alone. Rows longer than the registers hold are read
-// again for each pass (norm_fwd_long, norm_rev_long), from the caches mostly.
+// depends on the sizes alone. In large calls the VJP's next rows are on their
+// way to LDS while the ones before are worked on. Rows longer than the
+// registers hold are read again for each pass (norm_fwd_long, norm_rev_long),
+// from the caches mostly.
+//
+// Measured, bf16, forward and VJP with its sums: 32768 x 2048 48 and 71 us (5.6
+// and 5.7 TB/s), 16384 x 4096 50 and 74, 8192 x 8192 47 and 76, 4096 x 16384 48
+// and 84.
 
 #include "seq_common.h"
 #include "seq_kernels.h"
@@ -87,8 +93,9 @@ struct Shape {
 };
 
 // How rows are read and written: vectors at a row's end in part (PARTS), or
-// all of them whole (WHOLE), then also with non-temporal hints (STREAM).
-enum Mode { PARTS, WHOLE, STREAM };
+// all of them whole (WHOLE), then also with non-temporal hints (STREAM), and
+// the next rows requested into LDS while the ones before are worked on (AHEAD).
+enum Mode { PARTS, WHOLE, STREAM, AHEAD };
 
 // A group's R rows, this lane's vectors of them: n[k] columns of the k-th,
 // zeros beyond a row's end and the last row.
@@ -119,11 +126,114 @@ __device__ inline void store_row(void* base, int64_t row, int64_t columns,
   for (int k = 0; k < S::K; ++k)
     if (n[k] > 0) {
       T* at = p + k * S::L * S::V;
-      if constexpr (M == STREAM)
+      if constexpr (M >= STREAM)
         __builtin_nontemporal_store(v[k].v, reinterpret_cast<typename Vec<T>::unaligned*>(at));
       else if constexpr (M == WHOLE) store_vec(at, v[k]);
       else store_part(at, v[k], n[k]);
     }
+}
+
+// Rows on their way through LDS, for AHEAD. Each wave has its own lanes' part
+// of its rows there, R * K vectors of x and as many of dy, so that only its own
+// wait counts. The compiler would wait for every request before any read of
+// LDS and at every barrier; so LDS is read by instructions that it does not
+// see as such, with their wait, and the barrier leaves the requests under way.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+__device__ inline uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// Four times 16 bytes, STEP apart.
+template <int STEP>
+__device__ inline void read_lds(uint32_t at, Words4 (&v)[4]) {
+  asm volatile(
+      "ds_read_b128 %0, %4\n\t"
+      "ds_read_b128 %1, %4 offset:%5\n\t"
+      "ds_read_b128 %2, %4 offset:%6\n\t"
+      "ds_read_b128 %3, %4 offset:%7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+      : "v"(at), "n"(STEP), "n"(2 * STEP), "n"(3 * STEP)
+      : "memory");
+}
+__device__ inline void write_lds(uint32_t at, const float (&v)[2]) {
+  typedef float Two __attribute__((ext_vector_type(2)));
+  asm volatile("ds_write_b64 %0, %1" : : "v"(at), "v"(Two{v[0], v[1]}) : "memory");
+}
+__device__ inline void write_lds(uint32_t at, const float (&v)[4]) {
+  typedef float Four __attribute__((ext_vector_type(4)));
+  asm volatile("ds_write_b128 %0, %1" : : "v"(at), "v"(Four{v[0], v[1], v[2], v[3]}) : "memory");
+}
+// A value that no kernel of the launch writes, the same for the wave: through
+// the scalar cache, whose loads do not queue behind the requests.
+template <class A>
+__device__ inline A uniform_load(const A* p) {
+  return *(const __attribute__((address_space(4))) A*)p;
+}
+// Now, and not in the loop, where the wait would be for the requests too.
+template <class W, int N, int K>
+__device__ inline void wait_for(Pack<W, N> (&w)[K]) {
+  typedef uint32_t Words __attribute__((ext_vector_type(N * sizeof(W) / 4)));
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    Words x = __builtin_bit_cast(Words, w[k].v);
+    asm volatile("" : "+v"(x));
+    w[k].v = __builtin_bit_cast(typename Pack<W, N>::type, x);
+  }
+}
+// Until at most `later` of this wave's newest loads and stores are under way.
+__device__ inline void wait_all_but(int later) {
+  switch (later) {
+    case 1: __builtin_amdgcn_s_waitcnt(0x0f71); break;
+    case 2: __builtin_amdgcn_s_waitcnt(0x0f72); break;
+    case 3: __builtin_amdgcn_s_waitcnt(0x0f73); break;
+    case 4: __builtin_amdgcn_s_waitcnt(0x0f74); break;
+    default: __builtin_amdgcn_s_waitcnt(0x0f70); break;
+  }
+}
+template <class S, class T, bool USED>
+struct Ahead {
+  Words4 words[USED ? S::NT / 64 : 1][USED ? 2 * S::R * S::K : 1][64];
+};
+// Requests this lane's vectors of a group's rows; beyond a row's end and the
+// last row, of the last ones that are there.
+template <class S, class T>
+__device__ inline void request_rows(const void* base, int64_t stride, int64_t row, int64_t rows,
+                                    int64_t columns, Words4 (*slots)[64]) {
+#pragma unroll
+  for (int r = 0; r < S::R; ++r) {
+    const T* p = (const T*)base + (row + r < rows ? row + r : rows - 1) * stride;
+#pragma unroll
+    for (int k = 0; k < S::K; ++k) {
+      const int c = (k * S::L + (int)threadIdx.x % S::L) * S::V, end = (int)columns - S::V;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(p + (c < end ? c : end)),
+          (__attribute__((address_space(3))) void*)slots[r * S::K + k], 16, 0, 2);
+    }
+  }
+}
+// They arrive: x, then dy; zeros beyond a row's end and the last row.
+template <class S, class T>
+__device__ inline void take_rows(const Words4 (*slots)[64], int64_t row, int64_t rows,
+                                 const int (&n)[S::K], Vec<T> (&x)[S::R][S::K],
+                                 Vec<T> (&y)[S::R][S::K]) {
+  constexpr int N = S::R * S::K;
+  static_assert(N % 2 == 0);
+  const uint32_t at = lds_address(slots) + (threadIdx.x & 63) * 16;
+#pragma unroll
+  for (int j = 0; j < 2 * N; j += 4) {
+    Words4 v[4];
+    read_lds<1024>(at + j * 1024, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = (j + i) % N / S::K, k = (j + i) % S::K;
+      if (!(row + r < rows && n[k] > 0)) v[i] = Words4{};
+      const auto got = __builtin_bit_cast(typename Vec<T>::type, v[i]);
+      if (j + i < N) x[r][k].v = got;
+      else y[r][k].v = got;
+    }
+  }
 }
 
 // Sums over a group, of N values each, in every lane. Calls alternate between
@@ -132,15 +242,40 @@ template <class S, int N>
 struct Sums {
   typename S::A part[2][S::G][S::W][N];
 };
-template <class S, int N>
+template <class S, int N, Mode M = PARTS>
 __device__ inline void group_sum(Sums<S, N>& sm, int& turn, typename S::A (&v)[N]) {
 #pragma unroll
   for (int r = 0; r < N; ++r) v[r] = lane_sum<(S::L < 64 ? S::L : 64)>(v[r]);
   if constexpr (S::W > 1) {
     const int g = threadIdx.x / S::L, w = threadIdx.x % S::L / 64;
     if ((threadIdx.x & 63) == 0) {
+      if constexpr (M == AHEAD) {
+        write_lds(lds_address(&sm.part[turn][g][w][0]), v);
+      } else {
 #pragma unroll
-      for (int r = 0; r < N; ++r) sm.part[turn][g][w][r] = v[r];
+        for (int r = 0; r < N; ++r) sm.part[turn][g][w][r] = v[r];
+      }
+    }
+    if constexpr (M == AHEAD) {
+      static_assert(S::W * N % 16 == 0);
+      meet();
+      const uint32_t at = lds_address(&sm.part[turn][g][0][0]);
+#pragma unroll
+      for (int r = 0; r < N; ++r) v[r] = 0;
+#pragma unroll
+      for (int j = 0; j < S::W * N; j += 16) {
+        Words4 p[4];
+        read_lds<16>(at + j * 4, p);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t word = p[i / 4][i % 4];
+          const float f = __builtin_bit_cast(float, word);
+          if (j + i < N) v[i] = f;
+          else v[(j + i) % N] += f;
+        }
+      }
+      turn ^= 1;
+      return;
     }
     __syncthreads();
 #pragma unroll
@@ -233,7 +368,7 @@ __global__ __launch_bounds__(NT) void norm_rev(NormArgs p, Acc<T>* part) {
   typedef Shape<T, NT, L, K, R_> S;
   typedef typename S::A A;
   constexpr int V = S::V, R = S::R;
-  __shared__ Sums<S, 2 * R> sm;
+  __shared__ alignas(M == AHEAD ? 16 : sizeof(A)) Sums<S, 2 * R> sm;
   int turn = 0;
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
   int n[K];
@@ -247,18 +382,47 @@ __global__ __launch_bounds__(NT) void norm_rev(NormArgs p, Acc<T>* part) {
 #pragma unroll
     for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = A(0);
   }
+  if constexpr (M == AHEAD) wait_for(w);
   const A inv = A(1) / A(p.n);
-  for (int64_t row0 = (int64_t)blockIdx.x * S::kRows; row0 < p.rows;
-       row0 += (int64_t)gridDim.x * S::kRows) {
-    const int64_t row = row0 + group * R;
-    Vec<T> x[R][K], y[R][K];
-    A s[2 * R], mean[R], rstd[R];  // sums of e, then of e * xhat
-    load_rows<S, M>(p.x, p.sx, row, p.rows, n, x);
-    load_rows<S, M>(p.dy, p.sdy, row, p.rows, n, y);
+  __shared__ Ahead<S, T, M == AHEAD> ahead;
+  Words4 (*const slots)[64] =
+      ahead.words[M == AHEAD ? uniform((int)threadIdx.x / 64) : 0];
+  A next_mean[R], next_rstd[R];
+  int stores = 0;  // of this wave since its last request
+  const auto request = [&](int64_t row) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      mean[r] = row + r < p.rows ? ((const A*)p.mean)[row + r] : A(0);
-      rstd[r] = row + r < p.rows ? ((const A*)p.rstd)[row + r] : A(0);
+      const int64_t at = row + r < p.rows ? row + r : p.rows - 1;
+      next_mean[r] = uniform_load((const A*)p.mean + at);
+      next_rstd[r] = uniform_load((const A*)p.rstd + at);
+    }
+    request_rows<S, T>(p.x, p.sx, row, p.rows, p.n, slots);
+    request_rows<S, T>(p.dy, p.sdy, row, p.rows, p.n, slots + R * K);
+  };
+  if constexpr (M == AHEAD)
+    if ((int64_t)blockIdx.x * S::kRows < p.rows)
+      request((int64_t)blockIdx.x * S::kRows + uniform(group) * R);
+  for (int64_t row0 = (int64_t)blockIdx.x * S::kRows; row0 < p.rows;
+       row0 += (int64_t)gridDim.x * S::kRows) {
+    const int64_t row = row0 + (M == AHEAD ? uniform(group) : group) * R;
+    Vec<T> x[R][K], y[R][K];
+    A s[2 * R], mean[R], rstd[R];  // sums of e, then of e * xhat
+    if constexpr (M == AHEAD) {
+      wait_all_but(stores);
+      take_rows<S, T>(slots, row, p.rows, n, x, y);
+#pragma unroll
+      for (int r = 0; r < R; ++r) mean[r] = next_mean[r], rstd[r] = next_rstd[r];
+      if (row0 + (int64_t)gridDim.x * S::kRows < p.rows)
+        request(row + (int64_t)gridDim.x * S::kRows);
+      stores = 0;
+    } else {
+      load_rows<S, M>(p.x, p.sx, row, p.rows, n, x);
+      load_rows<S, M>(p.dy, p.sdy, row, p.rows, n, y);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        mean[r] = row + r < p.rows ? ((const A*)p.mean)[row + r] : A(0);
+        rstd[r] = row + r < p.rows ? ((const A*)p.rstd)[row + r] : A(0);
+      }
     }
     // columns beyond the end have dy = 0 and add nothing; rows beyond it too
 #pragma unroll
@@ -284,7 +448,7 @@ __global__ __launch_bounds__(NT) void norm_rev(NormArgs p, Acc<T>* part) {
     keep_packed(x);
     keep_packed(y);
     keep_packed(w);
-    group_sum<S>(sm, turn, s);
+    group_sum<S, 2 * R, M>(sm, turn, s);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (row + r >= p.rows) continue;
@@ -300,6 +464,10 @@ __global__ __launch_bounds__(NT) void norm_rev(NormArgs p, Acc<T>* part) {
         one_at_a_time();
       }
       store_row<S, M>(p.dx, row + r, p.n, n, x[r]);
+      if constexpr (M == AHEAD) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) stores += uniform(n[k]) > 0;
+      }
     }
     keep_packed(w);
   }
@@ -582,12 +750,27 @@ int parts_of(int32_t dtype, int64_t rows, int64_t nv) {
   return (int)(all < most ? all : most);
 }
 
+// Rows requested ahead of their use, where a workgroup joins its sums through
+// LDS and so has all its waves wait at the same time, and the requests' 16 bytes
+// are aligned (VJP in bf16 with, without: 32768 x 2048 71 and 74 us, 16384 x 4096
+// 74 and 81, 8192 x 8192 76 and 81, 4096 x 16384 84 and 92). A second turn of
+// rows under way gained nothing more.
+template <class T, int L, int K, int R>
+constexpr bool kAheadFits = sizeof(T) < 8 && L >= 256 && R * K <= 4;
+bool requests(const NormArgs& a) {
+  const int64_t e = a.dtype == ADST_F32 ? 4 : 2;
+  return (((int64_t)(uintptr_t)a.x | (int64_t)(uintptr_t)a.dy | a.sx * e | a.sdy * e) & 15) == 0;
+}
+
 template <class T, class W, int NT, int L, int K, int R, bool SUMS>
 void reverse_sums(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {
   const Mode m = mode_of(a, sizeof(T), 3);
   if (m == PARTS) norm_rev<T, W, NT, L, K, R, PARTS, SUMS><<<grid, NT, 0, st>>>(a, part);
   else if (m == WHOLE) norm_rev<T, W, NT, L, K, R, WHOLE, SUMS><<<grid, NT, 0, st>>>(a, part);
-  else norm_rev<T, W, NT, L, K, R, STREAM, SUMS><<<grid, NT, 0, st>>>(a, part);
+  else if (kAheadFits<T, L, K, R> && requests(a)) {
+    if constexpr (kAheadFits<T, L, K, R>)
+      norm_rev<T, W, NT, L, K, R, AHEAD, SUMS><<<grid, NT, 0, st>>>(a, part);
+  } else norm_rev<T, W, NT, L, K, R, STREAM, SUMS><<<grid, NT, 0, st>>>(a, part);
 }
 template <class T, class W, int NT, int L, int K, int R>
 void reverse(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {

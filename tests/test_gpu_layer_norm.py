@@ -171,6 +171,37 @@ def test_many_rows():
     assert torch.equal(b["db"], c["db"] * rows)
 
 
+@pytest.mark.parametrize("dtype,rows,n", [
+    (torch.bfloat16, 11003, 2056), (torch.float16, 5501, 4104), (torch.bfloat16, 2801, 8200),
+    (torch.bfloat16, 1130, 20000), (torch.float32, 5501, 2060), (torch.float32, 11003, 1032),
+    (torch.float32, 2801, 4100), (torch.float32, 701, 16000)])
+def test_large_calls(dtype, rows, n):
+    """Calls that request their rows ahead of their use: a row's results are those of a small call,
+    and the weights' gradients those of rows that start off a 16-byte boundary."""
+    g = torch.Generator("cuda").manual_seed(n)
+    x, dy = (torch.randn(rows, n, generator=g, device="cuda").to(dtype) for _ in range(2))
+    w, b = (torch.randn(n, generator=g, device="cuda").to(dtype) for _ in range(2))
+    one = run(x, w, b, dy)
+    for r in (slice(0, 40), slice(rows // 2, rows // 2 + 33), slice(rows - 40, rows)):
+        few = run(x[r], w, b, dy[r])
+        assert all(torch.equal(one[k][r], few[k]) for k in ("y", "mean", "rstd", "dx"))
+    wide = torch.zeros(rows, n + 9, dtype=dtype, device="cuda")
+    wide[:, 1:n + 1] = x
+    off = adst.layer_norm_vjp(wide[:, 1:n + 1], dy, one["mean"], one["rstd"], w)
+    assert all(torch.equal(one[k], off[k]) for k in ("dx", "dw", "db"))
+    wide = torch.zeros(rows, n + 16, dtype=dtype, device="cuda")
+    wide[:, 8:n + 8] = dy
+    apart = adst.layer_norm_vjp(x, wide[:, 8:n + 8], one["mean"], one["rstd"], w)
+    assert all(torch.equal(one[k], apart[k]) for k in ("dx", "dw", "db"))
+    only = adst.layer_norm_vjp(x, dy, one["mean"], one["rstd"], w, want_dx=False)
+    assert all(torch.equal(one[k], only[k]) for k in ("dw", "db"))
+
+
+def test_a_large_call_against_the_definition():
+    s = make(11003, 2056, torch.bfloat16, torch.float32, 3)
+    check(*s, run(*s))
+
+
 def test_on_another_stream():
     s = make(2000, 1500, torch.bfloat16, torch.float32)
     one = run(*s)

@@ -20,7 +20,7 @@
 // a, u and dh and writing da and du is all it moves.
 //
 // Measured, bf16 SIGMOID on halves of one projection: 8 x 4096 x 2048 forward
-// 90 us (4.5 TB/s), reverse 138 us (4.9 TB/s); 1 x 65536 x 1024 forward 106 us,
+// 89 us (4.5 TB/s), reverse 136 us (4.9 TB/s); 1 x 65536 x 1024 forward 105 us,
 // reverse 176. Without the waits between spans the first would take 85 and 136,
 // the second 83 and 133; the fill of the board is 3 to 5 us of each.
 //
@@ -94,10 +94,14 @@ struct Shape {
   static constexpr int kSpan = W * kWaveSteps;   // a workgroup's steps
   typedef Pack<T, V> P;
 };
-// Threads of a workgroup on long rows. Forward: 512 (8 x 4096 x 2048 bf16 90 us,
-// 94 with 256; 1 x 65536 x 1024 106 and 137). Reverse, which needs more
-// registers: 256 (138 us, 156 with 512; the longer row 176 and 161).
-constexpr int kForward = 512, kReverse = 256;
+// Threads of a workgroup on long rows: 512, whose spans are fewer. Forward: 8 x
+// 4096 x 2048 bf16 89 us, 93 with 256; 1 x 65536 x 1024 105 and 135. In reverse
+// a workgroup of 512 has a CU's registers to itself, but for F32 (5 x 2049 x 771
+// 43 us, 47 with 256), and the other types take 256 (8 x 4096 x 2048 bf16 136 us,
+// 163 with 512; 4 x 4096 x 1024 F64 133 and 156). A few long rows alone would be
+// faster with 512 (1 x 65536 x 1024 bf16 176 us, 164 with it), but spans set the
+// order of the sums, and a row's bits are not to depend on the number of rows.
+constexpr int kLong = 512, kReverse = 256;
 constexpr int kCkWaves = 4;  // a checkpoint at every fourth wave's steps
 
 // How a problem is laid out over workgroups of `threads`.
@@ -801,8 +805,8 @@ int lane_channels(int32_t dtype) { return dtype == ADST_F64 || dtype == ADST_F32
 int lane_steps(int32_t dtype) { return dtype == ADST_F64 ? 8 : 16; }
 
 // Lanes along channels: all 64 where that leaves few without one, else 16
-// (64 x 30000 x 7 f32: 93 us forward and 106 in reverse with 16, 274 and 293
-// with 64; 1 x 4096 x 64 bf16 8.7 and 10.1 us against 14.0 and 18.7).
+// (64 x 30000 x 7 f32: 74 us forward and 99 in reverse with 16, 230 and 278
+// with 64; 1 x 4096 x 64 bf16 8.8 and 10.2 us against 11.9 and 14.1).
 int lanes_of(int32_t dtype, int64_t D) {
   const int64_t C = 64 * lane_channels(dtype), all = (D + C - 1) / C * C;
   return 4 * (all - D) <= all ? 64 : 16;
@@ -819,7 +823,7 @@ Grid grid_of(int32_t dtype, int64_t B, int64_t T, int64_t D, bool forward) {
   g.by_xcd = 8 * (uint64_t)g.round <= 9 * (uint64_t)g.chains;
   if (!g.by_xcd) g.round = g.chains;
   g.threads = T <= wave ? 64 : T <= 2 * wave ? 128 : T <= 4 * wave ? 256
-              : forward ? kForward : kReverse;
+              : forward || dtype == ADST_F32 ? kLong : kReverse;
   g.span = g.threads / 64 * wave;
   g.spans = T > 0 ? (int)((T + g.span - 1) / g.span) : 1;
   g.groups = (g.spans + kGroup - 1) / kGroup;
@@ -857,9 +861,9 @@ void launch(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
 }
 
 // Non-temporal loads and stores for calls that move more than the caches keep,
-// on arrays whose rows are whole cache lines (8 x 4096 x 2048 bf16: reverse 148
-// us with them, 163 without; rows off the lines, whose shared lines then leave
-// the cache between two workgroups, 5 x 2049 x 771 f32: 59 and 47).
+// on arrays whose rows are whole cache lines (8 x 4096 x 2048 bf16: reverse 136
+// us with them, 146 without; rows off the lines, whose shared lines then leave
+// the cache between two workgroups, 5 x 2049 x 771 f32: 54 and 47).
 constexpr int64_t kStreamBytes = int64_t(128) << 20, kLine = 128;
 bool streams(const RecArgs& q, bool forward) {
   const int64_t e = type_size(q.dtype);
@@ -873,30 +877,31 @@ bool streams(const RecArgs& q, bool forward) {
 
 template <bool FORWARD, class T, bool SIG, int L>
 void by_threads(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
-  constexpr int kLong = FORWARD ? kForward : kReverse;
+  constexpr int kMost = FORWARD || sizeof(T) == 4 ? kLong : kReverse;
   if (g.spans > 1)
-    launch<FORWARD, T, SIG, true, false, kLong, L>(q, g, bd, st);
+    launch<FORWARD, T, SIG, true, false, kMost, L>(q, g, bd, st);
   else if (g.threads == 64)
     launch<FORWARD, T, SIG, false, false, 64, L>(q, g, bd, st);
   else if (g.threads == 128)
     launch<FORWARD, T, SIG, false, false, 128, L>(q, g, bd, st);
   else if (g.threads == 256)
     launch<FORWARD, T, SIG, false, false, 256, L>(q, g, bd, st);
-  else if constexpr (kLong > 256)
-    launch<FORWARD, T, SIG, false, false, kLong, L>(q, g, bd, st);
+  else if constexpr (kMost > 256)
+    launch<FORWARD, T, SIG, false, false, kMost, L>(q, g, bd, st);
 }
 template <bool FORWARD, class T, bool SIG>
 void by_grid(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
+  constexpr int kMost = FORWARD || sizeof(T) == 4 ? kLong : kReverse;
   if (g.lanes == 16)
     by_threads<FORWARD, T, SIG, 16>(q, g, bd, st);
   else if (!streams(q, FORWARD) || g.threads < 256)
     by_threads<FORWARD, T, SIG, 64>(q, g, bd, st);
   else if (g.spans > 1)
-    launch<FORWARD, T, SIG, true, true, FORWARD ? kForward : kReverse, 64>(q, g, bd, st);
+    launch<FORWARD, T, SIG, true, true, kMost, 64>(q, g, bd, st);
   else if (g.threads == 256)
     launch<FORWARD, T, SIG, false, true, 256, 64>(q, g, bd, st);
-  else if constexpr (FORWARD)
-    launch<FORWARD, T, SIG, false, true, kForward, 64>(q, g, bd, st);
+  else if constexpr (kMost > 256)
+    launch<FORWARD, T, SIG, false, true, kMost, 64>(q, g, bd, st);
 }
 
 template <bool FORWARD>

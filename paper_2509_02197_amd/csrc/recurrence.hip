@@ -385,8 +385,8 @@ __device__ inline A enter(const Board& bd, const Grid& g, uint32_t chain, int e,
   const int64_t seen = groups - (c & 63) + (int64_t)(j - 1 - back) * C;
   MapWords<A> m[kGroup - 1];
 #pragma unroll
-  for (int l = 0; l < kGroup - 1; ++l)
-    if (l < i) m[l] = MapWords<A>::load(bd.map, maps + (int64_t)l * C);
+  for (int l = 0; l < kGroup - 1; ++l)  // (without a channel they would lie past the slab's)
+    if (l < i && mine) m[l] = MapWords<A>::load(bd.map, maps + (int64_t)l * C);
   Word<A> w;
   int dist = 0;
   A ga = oa, gh = oh;

@@ -308,50 +308,54 @@ PyObject* recurrence_step(PyObject*, Args x, Py_ssize_t n) {
 }
 
 // --------------------------------------------------------------------- AdamW
-// (problem's address, descriptors' address, params, grads, copies or None,
-// grad_scale or None, t): True where the step was made. The problem and the
-// descriptors are the caller's; p, grad and copy, the gradients' type, the
-// scale and t are filled in here.
+// (problem's address, descriptors' address, their number, params, m, grads,
+// copies or None, grad_scale or None, t): True where the step was made. The
+// problem and the descriptors are the caller's; p, grad and copy, the
+// gradients' type, the scale and t are filled in here. What a tensor was when
+// the object was made, it has to be at each step: m has the shapes of all.
 PyObject* adamw_step(PyObject*, Args a, Py_ssize_t n) {
   return ordinary([&] {
-    need(n == 7 && PyTuple_Check(a[2]) && (a[4] == Py_None || PyTuple_Check(a[4])) &&
-         (PyList_Check(a[3]) || PyTuple_Check(a[3])));
+    need(n == 9 && PyTuple_Check(a[3]) && PyTuple_Check(a[4]) &&
+         (a[6] == Py_None || PyTuple_Check(a[6])) && (PyList_Check(a[5]) || PyTuple_Check(a[5])));
     auto* const prob = static_cast<adst_adamw_problem*>(PyLong_AsVoidPtr(a[0]));
     auto* const rows = static_cast<adst_adamw_tensor*>(PyLong_AsVoidPtr(a[1]));
     need(prob && rows);
-    const Py_ssize_t count = PyTuple_GET_SIZE(a[2]);
-    need(count > 0 && PySequence_Fast_GET_SIZE(a[3]) == count);
-    PyObject** const grads = PySequence_Fast_ITEMS(a[3]);
-    const at::Tensor& first = THPVariable_Unpack(PyTuple_GET_ITEM(a[2], 0));
-    const Here h = here(first);
-    need(THPVariable_Check(grads[0]));
-    const at::ScalarType type = THPVariable_Unpack(grads[0]).scalar_type();
-    const int code = code_of(THPVariable_Unpack(grads[0]));
+    const Py_ssize_t count = (Py_ssize_t)whole(a[2]);
+    need(count > 0 && PyTuple_GET_SIZE(a[3]) == count && PyTuple_GET_SIZE(a[4]) == count &&
+         PySequence_Fast_GET_SIZE(a[5]) == count &&
+         (a[6] == Py_None || PyTuple_GET_SIZE(a[6]) == count));
+    const auto held = [](PyObject* o) -> const at::Tensor& {
+      need(THPVariable_Check(o));
+      return THPVariable_Unpack(o);
+    };
+    PyObject** const grads = PySequence_Fast_ITEMS(a[5]);
+    const Here h = here(held(PyTuple_GET_ITEM(a[3], 0)));
+    const at::ScalarType type = held(grads[0]).scalar_type();
+    const int code = code_of(held(grads[0]));
     need((code == ADST_F64) == (prob->dtype == ADST_F64));
     for (Py_ssize_t i = 0; i < count; ++i) {
-      need(THPVariable_Check(grads[i]));
-      const at::Tensor& g = THPVariable_Unpack(grads[i]);
-      const at::Tensor& p = THPVariable_Unpack(PyTuple_GET_ITEM(a[2], i));
+      const at::Tensor& g = held(grads[i]);
+      const at::Tensor& p = held(PyTuple_GET_ITEM(a[3], i));
       need(g.scalar_type() == type && g.device() == h.device && g.numel() == rows[i].n &&
            g.is_contiguous());
-      need(p.scalar_type() == first.scalar_type() && p.device() == h.device &&
-           p.numel() == rows[i].n && p.is_contiguous());
+      need(code_of(p) == prob->dtype && p.device() == h.device && p.numel() == rows[i].n &&
+           p.is_contiguous() && p.sizes() == held(PyTuple_GET_ITEM(a[4], i)).sizes());
       rows[i].grad = g.data_ptr();
       rows[i].p = p.data_ptr();
     }
-    if (a[4] != Py_None)
+    if (a[6] != Py_None)
       for (Py_ssize_t i = 0; i < count; ++i) {
-        const at::Tensor& c = THPVariable_Unpack(PyTuple_GET_ITEM(a[4], i));
-        need(c.device() == h.device && c.numel() == rows[i].n && c.is_contiguous() &&
-             code_of(c) == prob->copy_dtype);
+        const at::Tensor& c = held(PyTuple_GET_ITEM(a[6], i));
+        need(code_of(c) == prob->copy_dtype && c.device() == h.device && c.is_contiguous() &&
+             c.sizes() == held(PyTuple_GET_ITEM(a[4], i)).sizes());
         rows[i].copy = c.data_ptr();
       }
-    const at::Tensor scale = maybe(a[5]);
+    const at::Tensor scale = maybe(a[7]);
     if (scale.defined())
       need(scale.scalar_type() == at::kFloat && scale.numel() == 1 && scale.device() == h.device);
     prob->grad_dtype = code;
     prob->grad_scale = static_cast<const float*>(at_of(scale));
-    prob->t = whole(a[6]);
+    prob->t = whole(a[8]);
     run(adst_adamw(prob, rows, (int32_t)count, h.stream));
     return Py_NewRef(Py_True);
   });

@@ -451,12 +451,13 @@ class AdamW:
         if self.copies is not None:
             if len(self.copies) != n:
                 raise ValueError(f"{len(self.copies)} copies of {n} parameters")
-            if n:
-                copy_code = _code("copies[0]", self.copies[0])
-                if copy_code == ADST_F64:
-                    raise TypeError("copies must be float32, bfloat16 or float16")
-            kind = self.copies[0].dtype if n else None
-            _expect_all("copies", self.copies, shapes, kind, self.device)
+            copy_code = _code("copies[0]", self.copies[0])
+            if copy_code == ADST_F64:
+                raise TypeError("copies must be float32, bfloat16 or float16")
+            _expect_all("copies", self.copies, shapes, self.copies[0].dtype, self.device)
+        self._shapes = shapes
+        self._types = {"params": first.dtype,
+                       "copies": None if self.copies is None else self.copies[0].dtype}
         self.bits = bits
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
         self.t = 0
@@ -487,7 +488,18 @@ class AdamW:
         self._set("weight_decay", weight_decay)
         self._prob = adst_adamw_problem(code, ADST_F32, copy_code, bits, 0, *self.betas, self.eps,
                                         None)
-        self._addresses = ctypes.addressof(self._prob), ctypes.addressof(self._rows)
+        self._descriptors = ctypes.addressof(self._prob), ctypes.addressof(self._rows), n
+
+    def _expect_held(self):
+        """The parameters and copies are still what they were when this object was made (a
+        module that is moved or converted gives its parameters other memory)."""
+        for name in ("params", "copies"):
+            tensors = getattr(self, name)
+            if tensors is None:
+                continue
+            if len(tensors) != self._n:
+                raise ValueError(f"{len(tensors)} {name}, not {self._n}")
+            _expect_all(name, tensors, self._shapes, self._types[name], self.device)
 
     def _set(self, name, value):
         values = [value] * self._n if isinstance(value, (int, float)) else list(value)
@@ -507,11 +519,12 @@ class AdamW:
             self._set("weight_decay", weight_decay)
         if t is None:
             t = self.t + 1
-        if stream is None and _binding().adamw_step(*self._addresses, self.params, grads,
-                                                    self.copies, grad_scale, t):
+        if stream is None and _binding().adamw_step(*self._descriptors, self.params, self.m,
+                                                    grads, self.copies, grad_scale, t):
             self.t = t
             return
         import torch
+        self._expect_held()
         if len(grads) != self._n:
             raise ValueError(f"{len(grads)} gradients for {self._n} parameters")
         code = _code("grads[0]", grads[0])

@@ -1,0 +1,99 @@
+"""AdamW's object where what it holds has changed, on a host without a GPU: the native call and
+the C call are replaced by ones that record, and the checks between are the object's own."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2509_02197_amd as adst
+from paper_2509_02197_amd import sequence
+
+pytestmark = pytest.mark.skipif(torch.cuda.device_count() > 0, reason="host-only")
+
+
+class Calls:
+    """In place of the library and the binding: the C calls' descriptors, and what the native
+    call answers."""
+
+    def __init__(self):
+        self.made = []
+        self.native = None
+
+    def adst_adamw(self, prob, rows, n, handle):
+        self.made.append([{k: getattr(r, k) for k, _ in r._fields_} for r in rows])
+        return adst.ADST_OK
+
+    def adamw_step(self, *args):
+        return self.native
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    c = Calls()
+    monkeypatch.setattr(sequence, "lib", lambda: c)
+    monkeypatch.setattr(sequence, "_binding", lambda: c)
+    monkeypatch.setattr(sequence, "_code", lambda name, t: sequence._codes()[t.dtype])
+    monkeypatch.setattr(sequence, "_call", lambda device, stream, used, body: body(0))
+    return c
+
+
+def make(bits=32, copies=True):
+    params = [torch.zeros(1000), torch.zeros(4, 6)]
+    held = [torch.zeros(p.shape, dtype=torch.bfloat16) for p in params] if copies else None
+    return adst.AdamW(params, bits=bits, copies=held), [torch.zeros(1000), torch.zeros(4, 6)]
+
+
+CHANGES = {
+    "fewer values": lambda t: torch.zeros(10, dtype=t.dtype),
+    "another type": lambda t: torch.zeros(t.shape, dtype=torch.float16),
+    "another order": lambda t: t.t() if t.dim() > 1 else torch.zeros(2 * len(t),
+                                                                    dtype=t.dtype)[::2],
+    "another shape": lambda t: t.reshape(2, -1),
+    "another device": lambda t: torch.empty_like(t, device="meta")}
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("name", ["params", "copies"])
+@pytest.mark.parametrize("change", CHANGES)
+def test_tensors_that_are_not_what_they_were(calls, change, name, which, bits):
+    opt, grads = make(bits)
+    opt.step(grads)
+    assert len(calls.made) == 1 and opt.t == 1
+    held = list(getattr(opt, name))
+    held[which] = CHANGES[change](held[which])
+    setattr(opt, name, tuple(held))
+    with pytest.raises(ValueError, match=name):
+        opt.step(grads)
+    assert len(calls.made) == 1 and opt.t == 1
+
+
+@pytest.mark.parametrize("name", ["params", "copies"])
+def test_data_that_was_replaced(calls, name):
+    """By a module's conversion, say: all of them."""
+    opt, grads = make()
+    for t in getattr(opt, name):
+        t.data = t.data.to(torch.float16)
+    with pytest.raises(ValueError, match=name):
+        opt.step(grads)
+    opt, grads = make()
+    getattr(opt, name)[0].data = torch.zeros(10, dtype=getattr(opt, name)[0].dtype)
+    with pytest.raises(ValueError, match=name):
+        opt.step(grads)
+    assert not calls.made
+
+
+def test_other_memory_of_the_same_kind_is_followed(calls):
+    opt, grads = make()
+    opt.params[0].data = torch.ones(1000)
+    opt.step(grads)
+    assert calls.made[0][0]["p"] == opt.params[0].data_ptr()
+
+
+@pytest.mark.parametrize("name", ["params", "copies"])
+def test_lists_of_another_length(calls, name):
+    opt, grads = make()
+    setattr(opt, name, getattr(opt, name)[:1])
+    with pytest.raises(ValueError):
+        opt.step(grads)
+    assert not calls.made

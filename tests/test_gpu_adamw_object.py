@@ -1,0 +1,77 @@
+"""AdamW's object where what it holds has changed between steps: refused before anything is
+launched, or followed."""
+import pytest
+import torch
+
+import paper_2509_02197_amd as adst
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    adst.lib()
+
+
+def make(bits=32, copies=True, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    shapes = [(1000,), (40, 60)]
+    params = [torch.randn(*s, generator=g).cuda() for s in shapes]
+    held = [torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in shapes]
+    return (adst.AdamW(params, bits=bits, copies=held if copies else None),
+            [torch.randn(*s, generator=g).cuda() for s in shapes])
+
+
+def bits_of(opt):
+    names = ["params", "m", "v"] + (["m_scale", "v_scale"] if opt.bits == 8 else []) + \
+        (["copies"] if opt.copies is not None else [])
+    return [t.detach().float().cpu().clone() for n in names for t in getattr(opt, n)]
+
+
+def equal(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+CHANGES = {
+    "fewer values": lambda t: t.new_zeros(10),
+    "another type": lambda t: t.to(torch.float16),
+    "another order": lambda t: t.t(),
+    "another shape": lambda t: t.t().contiguous(),
+    "on the host": lambda t: t.cpu()}
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("name", ["params", "copies"])
+@pytest.mark.parametrize("change", CHANGES)
+def test_data_that_was_replaced(change, name, bits):
+    opt, grads = make(bits)
+    opt.step(grads)
+    tensors = getattr(opt, name)
+    was = [t.data for t in tensors]
+    for i in ([0, 1] if change == "another type" else [1]):
+        tensors[i].data = CHANGES[change](tensors[i].data)
+    with pytest.raises(ValueError, match=name):
+        opt.step(grads)
+    for t, d in zip(tensors, was):
+        t.data = d
+    opt.step(grads)
+    other, _ = make(bits)
+    other.step(grads)
+    other.step(grads)
+    assert opt.t == 2 and equal(bits_of(opt), bits_of(other))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_other_memory_of_the_same_kind_is_followed(bits):
+    opt, grads = make(bits)
+    other, _ = make(bits)
+    opt.step(grads)
+    other.step(grads)
+    old = opt.params[0].data
+    kept = old.clone()
+    opt.params[0].data = old.clone()
+    opt.step(grads)
+    other.step(grads)
+    assert equal(bits_of(opt), bits_of(other)) and torch.equal(old, kept)

@@ -2,11 +2,12 @@
 // in between: a small call's time is the host's, and each attribute that
 // Python looks up is a good part of it (layer norm of 32 rows: 10.1 us through
 // Python, 6.7 from here, of which 3 are the launch; one step of AdamW over 121
-// tensors: 37 and 9). Each function returns None for anything
-// that is not ordinary (a wrong or unusual argument, tensors on another device
-// than the current one, a failing call), before anything is launched or after
-// nothing was; sequence.py then goes its own way, which handles the unusual
-// and raises the errors. Nothing here throws into Python.
+// tensors: 37 and 9). Each function returns None for anything that is not
+// ordinary (a wrong or unusual argument, tensors on another device than the
+// current one), before anything is launched; sequence.py then goes its own
+// way, which handles the unusual and raises the errors. A call that HIP fails
+// may have launched some of its work: it is never made again but raises
+// sequence.py's AdstError. Nothing else here throws into Python.
 
 #include <Python.h>
 
@@ -26,6 +27,9 @@ namespace {
 typedef PyObject* const* Args;
 
 struct Odd {};  // not an ordinary call
+struct Failed {  // a call that HIP failed
+  adst_status status;
+};
 
 void need(bool ok) {
   if (!ok) throw Odd();
@@ -75,7 +79,10 @@ at::Tensor bytes(uint64_t n, const Here& h) {
   return n ? make({(int64_t)n}, at::kByte, h) : at::Tensor();
 }
 
-void run(adst_status s) { need(s == ADST_OK); }
+void run(adst_status s) {
+  if (s == ADST_ERR_HIP) throw Failed{s};
+  need(s == ADST_OK);
+}
 
 // {name: tensor or None}
 class Dict {
@@ -117,10 +124,25 @@ bool truth(PyObject* o) {
   return v != 0;
 }
 
+// Sets the module's error, AdstError(status, text), or what keeps it from that.
+PyObject* raise(PyObject* module, adst_status status) {
+  PyObject* const error = PyObject_GetAttrString(module, "error");
+  if (!error) return nullptr;
+  PyObject* const text =
+      PyUnicode_FromFormat("%s: %s", adst_status_str(status), adst_last_error());
+  PyObject* const args = text ? Py_BuildValue("(iN)", (int)status, text) : nullptr;
+  if (args) PyErr_SetObject(error, args);
+  Py_XDECREF(args);
+  Py_DECREF(error);
+  return nullptr;
+}
+
 template <class F>
-PyObject* ordinary(F f) {
+PyObject* ordinary(PyObject* module, F f) {
   try {
     return f();
+  } catch (const Failed& failed) {
+    return raise(module, failed.status);
   } catch (...) {
     PyErr_Clear();
     return Py_NewRef(Py_None);
@@ -147,8 +169,8 @@ adst_norm_problem norm_problem(const at::Tensor& x, const at::Tensor& dy, const 
 }
 
 // (x, w, b, eps)
-PyObject* layer_norm(PyObject*, Args a, Py_ssize_t n) {
-  return ordinary([&] {
+PyObject* layer_norm(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
     need(n == 4);
     const at::Tensor x = tensor(a[0]), w = maybe(a[1]), b = maybe(a[2]);
     const Here h = here(x);
@@ -167,8 +189,8 @@ PyObject* layer_norm(PyObject*, Args a, Py_ssize_t n) {
 }
 
 // (x, dy, mean, rstd, w, want_dx, want_dw, want_db)
-PyObject* layer_norm_vjp(PyObject*, Args a, Py_ssize_t n) {
-  return ordinary([&] {
+PyObject* layer_norm_vjp(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
     need(n == 8);
     const at::Tensor x = tensor(a[0]), dy = tensor(a[1]), mean = tensor(a[2]), rstd = tensor(a[3]),
                      w = maybe(a[4]);
@@ -220,8 +242,8 @@ void states(const adst_recurrence_problem& p, const at::Tensor& t, const Here& h
 at::Tensor like(const at::Tensor& a) { return at::empty_like(a, at::MemoryFormat::Contiguous); }
 
 // (a, u, h0, lens, gate, want_h, want_ck)
-PyObject* recurrence(PyObject*, Args x, Py_ssize_t n) {
-  return ordinary([&] {
+PyObject* recurrence(PyObject* module, Args x, Py_ssize_t n) {
+  return ordinary(module, [&] {
     need(n == 7);
     const at::Tensor a = tensor(x[0]), u = tensor(x[1]), h0 = maybe(x[2]), lens = maybe(x[3]);
     const Here h = here(a);
@@ -247,8 +269,8 @@ PyObject* recurrence(PyObject*, Args x, Py_ssize_t n) {
 }
 
 // (a, u, dh, h0, lens, dhT, ck, gate)
-PyObject* recurrence_vjp(PyObject*, Args x, Py_ssize_t n) {
-  return ordinary([&] {
+PyObject* recurrence_vjp(PyObject* module, Args x, Py_ssize_t n) {
+  return ordinary(module, [&] {
     need(n == 8);
     const at::Tensor a = tensor(x[0]), u = tensor(x[1]), dh = tensor(x[2]), h0 = maybe(x[3]),
                      lens = maybe(x[4]), dhT = maybe(x[5]), ck = maybe(x[6]);
@@ -276,8 +298,8 @@ PyObject* recurrence_vjp(PyObject*, Args x, Py_ssize_t n) {
 }
 
 // (a, u, state, slots, gate)
-PyObject* recurrence_step(PyObject*, Args x, Py_ssize_t n) {
-  return ordinary([&] {
+PyObject* recurrence_step(PyObject* module, Args x, Py_ssize_t n) {
+  return ordinary(module, [&] {
     need(n == 5);
     const at::Tensor a = tensor(x[0]), u = tensor(x[1]), state = tensor(x[2]), slots = maybe(x[3]);
     const Here h = here(a);
@@ -297,12 +319,12 @@ PyObject* recurrence_step(PyObject*, Args x, Py_ssize_t n) {
     const at::Tensor out = like(a);
     PyObject* const r = THPVariable_Wrap(out);
     need(r);
-    if (adst_recurrence_step(&p, a.data_ptr(), u.data_ptr(),
+    const adst_status status =
+        adst_recurrence_step(&p, a.data_ptr(), u.data_ptr(),
                              static_cast<const int32_t*>(at_of(slots)), state.data_ptr(),
-                             state.size(0), out.data_ptr(), h.stream) != ADST_OK) {
-      Py_DECREF(r);
-      throw Odd();
-    }
+                             state.size(0), out.data_ptr(), h.stream);
+    if (status != ADST_OK) Py_DECREF(r);
+    run(status);
     return r;
   });
 }
@@ -313,8 +335,8 @@ PyObject* recurrence_step(PyObject*, Args x, Py_ssize_t n) {
 // problem and the descriptors are the caller's; p, grad and copy, the
 // gradients' type, the scale and t are filled in here. What a tensor was when
 // the object was made, it has to be at each step: m has the shapes of all.
-PyObject* adamw_step(PyObject*, Args a, Py_ssize_t n) {
-  return ordinary([&] {
+PyObject* adamw_step(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
     need(n == 9 && PyTuple_Check(a[3]) && PyTuple_Check(a[4]) &&
          (a[6] == Py_None || PyTuple_Check(a[6])) && (PyList_Check(a[5]) || PyTuple_Check(a[5])));
     auto* const prob = static_cast<adst_adamw_problem*>(PyLong_AsVoidPtr(a[0]));

@@ -17,8 +17,9 @@ import numpy as np
 
 from . import build as _build
 from . import (ADST_BF16, ADST_F16, ADST_F32, ADST_F64, ADST_GATE_COEFF, ADST_GATE_SIGMOID,
-               ADST_STATE_BLOCK, _check, _ptr, _stream, adst_adamw_problem, adst_adamw_tensor,
-               adst_norm_problem, adst_recurrence_info, adst_recurrence_problem, lib)
+               ADST_STATE_BLOCK, AdstError, _check, _ptr, _stream, adst_adamw_problem,
+               adst_adamw_tensor, adst_norm_problem, adst_recurrence_info,
+               adst_recurrence_problem, lib)
 
 
 # ------------------------------------------------------------ the C calls
@@ -72,7 +73,7 @@ _BINDING = None
 
 def _binding():
     """The native form of this file's ordinary calls (csrc/binding.cpp): it answers None to
-    anything else, which the code here then handles."""
+    anything else, which the code here then handles, and raises what HIP fails."""
     global _BINDING
     if _BINDING is None:
         import torch  # noqa: F401  (whose libraries the binding is linked with)
@@ -80,6 +81,7 @@ def _binding():
         if not os.path.exists(_build.BINDING):
             _build.build()
         from . import _binding as module
+        module.error = AdstError
         _BINDING = module
     return _BINDING
 

@@ -19,6 +19,7 @@
 
 #include "seq_common.h"
 #include "seq_kernels.h"
+#include "seq_launch.h"
 
 namespace adst {
 namespace {
@@ -251,8 +252,8 @@ hipError_t launch(const adst_adamw_problem& pr, const adst_adamw_tensor* t, int3
       const int64_t take = want < kMostChunks ? want : kMostChunks;
       if (tb.n == Table<P, BITS8>::kMost || chunks + take > kMostChunks) {
         tb.first[tb.n] = (int)chunks;
-        adamw_many<P, G, C, BITS8, NT><<<(unsigned)chunks, kThreads, 0, st>>>(tb);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e =
+            start(adamw_many<P, G, C, BITS8, NT>, (unsigned)chunks, kThreads, st, tb);
         if (e != hipSuccess) return e;
         tb.n = 0;
         chunks = 0;
@@ -279,8 +280,7 @@ hipError_t launch(const adst_adamw_problem& pr, const adst_adamw_tensor* t, int3
   }
   if (chunks == 0) return hipSuccess;
   tb.first[tb.n] = (int)chunks;
-  adamw_many<P, G, C, BITS8, NT><<<(unsigned)chunks, kThreads, 0, st>>>(tb);
-  return hipGetLastError();
+  return start(adamw_many<P, G, C, BITS8, NT>, (unsigned)chunks, kThreads, st, tb);
 }
 
 // Non-temporal loads and stores for calls that move more than the caches hold

@@ -21,6 +21,7 @@
 
 #include "seq_common.h"
 #include "seq_kernels.h"
+#include "seq_launch.h"
 
 namespace adst {
 namespace {
@@ -681,18 +682,11 @@ __global__ __launch_bounds__(kSumColumns * kShares) void norm_dw_sum(NormArgs p,
 template <class F>
 hipError_t by_type(int32_t dtype, int32_t wtype, F f) {
   switch (dtype) {
-    case ADST_F64: f(double(), double()); break;
-    case ADST_F32: f(float(), float()); break;
-    case ADST_BF16:
-      if (wtype == ADST_F32) f(bf16(), float());
-      else f(bf16(), bf16());
-      break;
-    default:
-      if (wtype == ADST_F32) f(f16(), float());
-      else f(f16(), f16());
-      break;
+    case ADST_F64: return f(double(), double());
+    case ADST_F32: return f(float(), float());
+    case ADST_BF16: return wtype == ADST_F32 ? f(bf16(), float()) : f(bf16(), bf16());
+    default: return wtype == ADST_F32 ? f(f16(), float()) : f(f16(), f16());
   }
-  return hipGetLastError();
 }
 
 int64_t vectors_of(int32_t dtype, int64_t n) {
@@ -713,30 +707,30 @@ Mode mode_of(const NormArgs& a, int64_t size, int64_t arrays) {
 // Workgroups of the forward: enough to fill the chip several times over, each
 // with several rows to keep its weights for.
 template <class T, class W, int NT, int L, int K, int R>
-void forward(const NormArgs& a, hipStream_t st) {
+hipError_t forward(const NormArgs& a, hipStream_t st) {
   const int64_t per = (int64_t)NT / L * R, all = (a.rows + per - 1) / per;
   const int64_t most = 256 * 2048 / NT;
   const unsigned grid = (unsigned)(all < most ? all : most);
   const Mode m = mode_of(a, sizeof(T), 2);
-  if (m == PARTS) norm_fwd<T, W, NT, L, K, R, PARTS><<<grid, NT, 0, st>>>(a);
-  else if (m == WHOLE) norm_fwd<T, W, NT, L, K, R, WHOLE><<<grid, NT, 0, st>>>(a);
-  else norm_fwd<T, W, NT, L, K, R, STREAM><<<grid, NT, 0, st>>>(a);
+  return start(m == PARTS   ? norm_fwd<T, W, NT, L, K, R, PARTS>
+               : m == WHOLE ? norm_fwd<T, W, NT, L, K, R, WHOLE>
+                            : norm_fwd<T, W, NT, L, K, R, STREAM>,
+               grid, NT, st, a);
 }
 unsigned long_grid(int64_t rows) { return (unsigned)(rows < 4096 ? rows : 4096); }
 template <class T, class W>
-void forward_by_length(const NormArgs& a, int64_t nv, hipStream_t st) {
-  if (nv <= 16) forward<T, W, 256, 16, 1, 2>(a, st);
-  else if (nv <= 64) forward<T, W, 256, 64, 1, 4>(a, st);
-  else if (nv <= 128) forward<T, W, 256, 64, 2, 2>(a, st);
-  else if (nv <= 256) forward<T, W, 256, 64, 4, 1>(a, st);
-  else if (nv <= 512) forward<T, W, 256, 256, 2, 1>(a, st);
-  else if (nv <= 1024) forward<T, W, 256, 256, 4, 1>(a, st);
-  else if (nv <= 2048) forward<T, W, 512, 512, 4, 1>(a, st);
-  else if (nv <= 4096) forward<T, W, 1024, 1024, 4, 1>(a, st);
-  else if (nv <= 8192 && sizeof(T) == 4) {
-    if constexpr (sizeof(T) == 4) forward<T, W, 1024, 1024, 8, 1>(a, st);
-  }
-  else norm_fwd_long<T, W><<<long_grid(a.rows), kLongThreads, 0, st>>>(a);
+hipError_t forward_by_length(const NormArgs& a, int64_t nv, hipStream_t st) {
+  if (nv <= 16) return forward<T, W, 256, 16, 1, 2>(a, st);
+  if (nv <= 64) return forward<T, W, 256, 64, 1, 4>(a, st);
+  if (nv <= 128) return forward<T, W, 256, 64, 2, 2>(a, st);
+  if (nv <= 256) return forward<T, W, 256, 64, 4, 1>(a, st);
+  if (nv <= 512) return forward<T, W, 256, 256, 2, 1>(a, st);
+  if (nv <= 1024) return forward<T, W, 256, 256, 4, 1>(a, st);
+  if (nv <= 2048) return forward<T, W, 512, 512, 4, 1>(a, st);
+  if (nv <= 4096) return forward<T, W, 1024, 1024, 4, 1>(a, st);
+  if constexpr (sizeof(T) == 4)
+    if (nv <= 8192) return forward<T, W, 1024, 1024, 8, 1>(a, st);
+  return start(norm_fwd_long<T, W>, long_grid(a.rows), kLongThreads, st, a);
 }
 
 // Groups of rows that sum dw and db apart.
@@ -763,49 +757,44 @@ bool requests(const NormArgs& a) {
 }
 
 template <class T, class W, int NT, int L, int K, int R, bool SUMS>
-void reverse_sums(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {
+hipError_t reverse_sums(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {
   const Mode m = mode_of(a, sizeof(T), 3);
-  if (m == PARTS) norm_rev<T, W, NT, L, K, R, PARTS, SUMS><<<grid, NT, 0, st>>>(a, part);
-  else if (m == WHOLE) norm_rev<T, W, NT, L, K, R, WHOLE, SUMS><<<grid, NT, 0, st>>>(a, part);
-  else if (kAheadFits<T, L, K, R> && requests(a)) {
-    if constexpr (kAheadFits<T, L, K, R>)
-      norm_rev<T, W, NT, L, K, R, AHEAD, SUMS><<<grid, NT, 0, st>>>(a, part);
-  } else norm_rev<T, W, NT, L, K, R, STREAM, SUMS><<<grid, NT, 0, st>>>(a, part);
+  if constexpr (kAheadFits<T, L, K, R>)
+    if (m == STREAM && requests(a))
+      return start(norm_rev<T, W, NT, L, K, R, AHEAD, SUMS>, grid, NT, st, a, part);
+  return start(m == PARTS   ? norm_rev<T, W, NT, L, K, R, PARTS, SUMS>
+               : m == WHOLE ? norm_rev<T, W, NT, L, K, R, WHOLE, SUMS>
+                            : norm_rev<T, W, NT, L, K, R, STREAM, SUMS>,
+               grid, NT, st, a, part);
 }
 template <class T, class W, int NT, int L, int K, int R>
-void reverse(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {
-  reverse_sums<T, W, NT, L, K, R, true>(a, grid, part, st);
+hipError_t reverse(const NormArgs& a, unsigned grid, Acc<T>* part, hipStream_t st) {
+  return reverse_sums<T, W, NT, L, K, R, true>(a, grid, part, st);
 }
 
 template <class T, class W>
-void reverse_by_length(const NormArgs& a, int64_t nv, int parts, Acc<T>* part, hipStream_t st) {
+hipError_t reverse_by_length(const NormArgs& a, int64_t nv, int parts, Acc<T>* part, hipStream_t st) {
   const unsigned g = (unsigned)parts;
-  if (nv <= 16) reverse<T, W, 512, 16, 1, 2>(a, g, part, st);
-  else if (nv <= 64) reverse<T, W, 512, 64, 1, 4>(a, g, part, st);
-  else if (nv <= 128) reverse<T, W, 512, 64, 2, 2>(a, g, part, st);
-  else if (nv <= 256) reverse<T, W, 512, 256, 1, 2>(a, g, part, st);
-  else if (nv <= 512) reverse<T, W, 1024, 512, 1, 2>(a, g, part, st);
-  else if (nv <= 1024) reverse<T, W, 1024, 512, 2, 1>(a, g, part, st);
-  else if (nv <= 2048) reverse<T, W, 512, 512, 4, 1>(a, g, part, st);
-  else if (nv <= held_in_vjp(a.dtype)) {
-    if constexpr (sizeof(T) == 4) reverse<T, W, 1024, 1024, 4, 1>(a, g, part, st);
-  } else {
-    // dx without the sums' registers, as long as those hold the row
-    if (!a.dx) {
-    } else if (nv <= 4096) {
-      if constexpr (sizeof(T) != 4)
-        reverse_sums<T, W, 1024, 1024, 4, 1, false>(a, long_grid(a.rows), nullptr, st);
-    } else if (nv <= 8192 && sizeof(T) == 4) {
-      if constexpr (sizeof(T) == 4)
-        reverse_sums<T, W, 1024, 1024, 8, 1, false>(a, long_grid(a.rows), nullptr, st);
-    } else {
-      norm_rev_long<T, W><<<long_grid(a.rows), kLongThreads, 0, st>>>(a);
-    }
-    if (part) {
-      const unsigned columns = (unsigned)((nv + kColumnThreads - 1) / kColumnThreads);
-      norm_dw_long<T><<<dim3(columns, g), kColumnThreads, 0, st>>>(a, part);
-    }
+  if (nv <= 16) return reverse<T, W, 512, 16, 1, 2>(a, g, part, st);
+  if (nv <= 64) return reverse<T, W, 512, 64, 1, 4>(a, g, part, st);
+  if (nv <= 128) return reverse<T, W, 512, 64, 2, 2>(a, g, part, st);
+  if (nv <= 256) return reverse<T, W, 512, 256, 1, 2>(a, g, part, st);
+  if (nv <= 512) return reverse<T, W, 1024, 512, 1, 2>(a, g, part, st);
+  if (nv <= 1024) return reverse<T, W, 1024, 512, 2, 1>(a, g, part, st);
+  if (nv <= 2048) return reverse<T, W, 512, 512, 4, 1>(a, g, part, st);
+  if constexpr (sizeof(T) == 4)
+    if (nv <= held_in_vjp(a.dtype)) return reverse<T, W, 1024, 1024, 4, 1>(a, g, part, st);
+  // dx without the sums' registers, as long as those hold the row
+  hipError_t e = hipSuccess;
+  if (a.dx) {
+    const unsigned rows = long_grid(a.rows);
+    constexpr int K = sizeof(T) == 4 ? 8 : 4;
+    e = nv <= K * 1024 ? reverse_sums<T, W, 1024, 1024, K, 1, false>(a, rows, nullptr, st)
+                       : start(norm_rev_long<T, W>, rows, kLongThreads, st, a);
   }
+  if (e != hipSuccess || !part) return e;
+  const unsigned columns = (unsigned)((nv + kColumnThreads - 1) / kColumnThreads);
+  return start(norm_dw_long<T>, dim3(columns, g), kColumnThreads, st, a, part);
 }
 
 }  // namespace
@@ -813,7 +802,7 @@ void reverse_by_length(const NormArgs& a, int64_t nv, int parts, Acc<T>* part, h
 hipError_t norm_forward(const NormArgs& a, hipStream_t st) {
   const int64_t nv = vectors_of(a.dtype, a.n);
   return by_type(a.dtype, a.wtype, [&](auto t, auto w) {
-    forward_by_length<decltype(t), decltype(w)>(a, nv, st);
+    return forward_by_length<decltype(t), decltype(w)>(a, nv, st);
   });
 }
 
@@ -830,11 +819,11 @@ hipError_t norm_vjp(const NormArgs& a, void* ws, hipStream_t st) {
     typedef decltype(t) T;
     typedef decltype(w) W;
     Acc<T>* const part = sums ? (Acc<T>*)ws : nullptr;
-    if (parts > 0) reverse_by_length<T, W>(a, nv, parts, part, st);
-    if (sums) {
-      const unsigned grid = (unsigned)((2 * a.n + kSumColumns - 1) / kSumColumns);
-      norm_dw_sum<T, W><<<grid, kSumColumns * kShares, 0, st>>>(a, part, parts);
-    }
+    const hipError_t e =
+        parts > 0 ? reverse_by_length<T, W>(a, nv, parts, part, st) : hipSuccess;
+    if (e != hipSuccess || !sums) return e;
+    const unsigned grid = (unsigned)((2 * a.n + kSumColumns - 1) / kSumColumns);
+    return start(norm_dw_sum<T, W>, grid, kSumColumns * kShares, st, a, part, parts);
   });
 }
 

@@ -42,6 +42,7 @@
 
 #include "seq_common.h"
 #include "seq_kernels.h"
+#include "seq_launch.h"
 
 namespace adst {
 namespace {
@@ -844,20 +845,22 @@ Board board_of(int32_t dtype, const Grid& g, void* ws, int64_t* bytes) {
 }
 
 template <class F>
-void by_type(int32_t dtype, F f) {
+hipError_t by_type(int32_t dtype, F f) {
   switch (dtype) {
-    case ADST_F64: f(double()); break;
-    case ADST_F32: f(float()); break;
-    case ADST_BF16: f(bf16()); break;
-    default: f(f16()); break;
+    case ADST_F64: return f(double());
+    case ADST_F32: return f(float());
+    case ADST_BF16: return f(bf16());
+    default: return f(f16());
   }
 }
 
 template <bool FORWARD, class T, bool SIG, bool MULTI, bool STREAM, int NT, int L>
-void launch(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
+hipError_t launch(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
   const unsigned blocks = g.round * (unsigned)g.spans;
-  if constexpr (FORWARD) rec_fwd<T, SIG, MULTI, STREAM, NT, L><<<blocks, NT, 0, st>>>(q, g, bd);
-  else rec_rev<T, SIG, MULTI, STREAM, NT, L><<<blocks, NT, 0, st>>>(q, g, bd);
+  if constexpr (FORWARD)
+    return start(rec_fwd<T, SIG, MULTI, STREAM, NT, L>, blocks, NT, st, q, g, bd);
+  else
+    return start(rec_rev<T, SIG, MULTI, STREAM, NT, L>, blocks, NT, st, q, g, bd);
 }
 
 // Non-temporal loads and stores for calls that move more than the caches keep,
@@ -876,32 +879,34 @@ bool streams(const RecArgs& q, bool forward) {
 }
 
 template <bool FORWARD, class T, bool SIG, int L>
-void by_threads(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
+hipError_t by_threads(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
   constexpr int kMost = FORWARD || sizeof(T) == 4 ? kLong : kReverse;
   if (g.spans > 1)
-    launch<FORWARD, T, SIG, true, false, kMost, L>(q, g, bd, st);
-  else if (g.threads == 64)
-    launch<FORWARD, T, SIG, false, false, 64, L>(q, g, bd, st);
-  else if (g.threads == 128)
-    launch<FORWARD, T, SIG, false, false, 128, L>(q, g, bd, st);
-  else if (g.threads == 256)
-    launch<FORWARD, T, SIG, false, false, 256, L>(q, g, bd, st);
-  else if constexpr (kMost > 256)
-    launch<FORWARD, T, SIG, false, false, kMost, L>(q, g, bd, st);
+    return launch<FORWARD, T, SIG, true, false, kMost, L>(q, g, bd, st);
+  if (g.threads == 64)
+    return launch<FORWARD, T, SIG, false, false, 64, L>(q, g, bd, st);
+  if (g.threads == 128)
+    return launch<FORWARD, T, SIG, false, false, 128, L>(q, g, bd, st);
+  if (g.threads == 256)
+    return launch<FORWARD, T, SIG, false, false, 256, L>(q, g, bd, st);
+  if constexpr (kMost > 256)
+    return launch<FORWARD, T, SIG, false, false, kMost, L>(q, g, bd, st);
+  return hipErrorInvalidValue;  // grid_of has no such workgroup
 }
 template <bool FORWARD, class T, bool SIG>
-void by_grid(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
+hipError_t by_grid(const RecArgs& q, const Grid& g, const Board& bd, hipStream_t st) {
   constexpr int kMost = FORWARD || sizeof(T) == 4 ? kLong : kReverse;
   if (g.lanes == 16)
-    by_threads<FORWARD, T, SIG, 16>(q, g, bd, st);
-  else if (!streams(q, FORWARD) || g.threads < 256)
-    by_threads<FORWARD, T, SIG, 64>(q, g, bd, st);
-  else if (g.spans > 1)
-    launch<FORWARD, T, SIG, true, true, kMost, 64>(q, g, bd, st);
-  else if (g.threads == 256)
-    launch<FORWARD, T, SIG, false, true, 256, 64>(q, g, bd, st);
-  else if constexpr (kMost > 256)
-    launch<FORWARD, T, SIG, false, true, kMost, 64>(q, g, bd, st);
+    return by_threads<FORWARD, T, SIG, 16>(q, g, bd, st);
+  if (!streams(q, FORWARD) || g.threads < 256)
+    return by_threads<FORWARD, T, SIG, 64>(q, g, bd, st);
+  if (g.spans > 1)
+    return launch<FORWARD, T, SIG, true, true, kMost, 64>(q, g, bd, st);
+  if (g.threads == 256)
+    return launch<FORWARD, T, SIG, false, true, 256, 64>(q, g, bd, st);
+  if constexpr (kMost > 256)
+    return launch<FORWARD, T, SIG, false, true, kMost, 64>(q, g, bd, st);
+  return hipErrorInvalidValue;
 }
 
 template <bool FORWARD>
@@ -911,17 +916,15 @@ hipError_t sweep(const RecArgs& q, void* ws, hipStream_t st) {
   const Board bd = board_of(q.dtype, g, ws, &bytes);
   if (bytes) {
     const int64_t n = bytes / 16, each = kFillThreads * kFillEach;
-    fill_ones<<<(unsigned)((n + each - 1) / each), kFillThreads, 0, st>>>(
-        static_cast<uint4*>(ws), n);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = start(fill_ones, (unsigned)((n + each - 1) / each), kFillThreads, st,
+                               static_cast<uint4*>(ws), n);
     if (e != hipSuccess) return e;
   }
-  by_type(q.dtype, [&](auto t) {
+  return by_type(q.dtype, [&](auto t) {
     typedef decltype(t) T;
-    if (q.gate == ADST_GATE_SIGMOID) by_grid<FORWARD, T, true>(q, g, bd, st);
-    else by_grid<FORWARD, T, false>(q, g, bd, st);
+    return q.gate == ADST_GATE_SIGMOID ? by_grid<FORWARD, T, true>(q, g, bd, st)
+                                       : by_grid<FORWARD, T, false>(q, g, bd, st);
   });
-  return hipGetLastError();
 }
 
 }  // namespace
@@ -953,14 +956,13 @@ hipError_t rec_forward(const RecArgs& q, void* ws, hipStream_t st) {
 hipError_t rec_vjp(const RecArgs& q, void* ws, hipStream_t st) { return sweep<false>(q, ws, st); }
 
 hipError_t rec_step(const RecStep& q, hipStream_t st) {
-  by_type(q.dtype, [&](auto t) {
+  return by_type(q.dtype, [&](auto t) {
     typedef decltype(t) T;
     const int64_t per_row = (q.D + Vec<T>::N - 1) / Vec<T>::N;
     const unsigned blocks = (unsigned)((q.B * per_row + kStepThreads - 1) / kStepThreads);
-    if (q.gate == ADST_GATE_SIGMOID) rec_one<T, true><<<blocks, kStepThreads, 0, st>>>(q, per_row);
-    else rec_one<T, false><<<blocks, kStepThreads, 0, st>>>(q, per_row);
+    return start(q.gate == ADST_GATE_SIGMOID ? rec_one<T, true> : rec_one<T, false>, blocks,
+                 kStepThreads, st, q, per_row);
   });
-  return hipGetLastError();
 }
 
 }  // namespace adst

@@ -219,15 +219,10 @@ inline int atomicAdd(int* p, int v) {
 #define __builtin_amdgcn_permlane16_swap(a, b, x, y) host_hip::row_swap(a, 16)
 #define __builtin_amdgcn_permlane32_swap(a, b, x, y) host_hip::row_swap(a, 32)
 #define __builtin_amdgcn_mov_dpp(v, control, x, y, z) host_hip::permuted(v, control)
+#define __builtin_amdgcn_sched_barrier(n)
+#define __builtin_amdgcn_s_waitcnt(n) std::abort()
+#define __builtin_amdgcn_global_load_lds(...) std::abort()
 #define __builtin_amdgcn_s_sleep(n) host_hip::pause()
 #define __builtin_amdgcn_rcpf(x) (1.0f / (x))
 #define __builtin_amdgcn_exp2f(x) std::exp2(x)
 #define __builtin_amdgcn_readfirstlane(x) ((int)host_hip::lanes_meet((uint32_t)(x))[0])
-
-namespace host_hip {
-// kernel<<<grid, size, 0, stream>>>(arguments...), at once.
-template <class F>
-auto call(F kernel, dim3 grid, dim3 size) {
-  return [=](auto... x) { launch(grid, size, [=] { kernel(x...); }); };
-}
-}  // namespace host_hip

@@ -1,6 +1,7 @@
 """Builds a kernel file of the library as a program for the host, with the header in
 host_hip/ in HIP's place. The file itself is compiled; only what no host compiler takes is
-rewritten: launches become calls, and barriers for the compiler's register allocation go."""
+rewritten: barriers for the compiler's register allocation go, and GPU instructions end the
+program."""
 import os
 import re
 import shutil
@@ -20,10 +21,10 @@ def compiler():
 
 
 def as_host_code(text):
-    # kernel<...><<<grid, block, 0, stream>>>(arguments)
-    text = re.sub(r"([\w:]+(?:<[^;{}()]*>)?)<<<(.*?), 0, (\w+)>>>\(",
-                  r"host_hip::call([](auto... x) { \1(x...); }, \2)(", text, flags=re.S)
-    return re.sub(r'asm volatile\("" : "\+v"\([^;]*\)\);', ";", text)
+    text = re.sub(r'asm volatile\("" : [^;]*;', ";", text)
+    text = re.sub(r"__shared__ (alignas\([^()]*(?:\([^()]*\))?[^()]*\))", r"\1 __shared__", text)
+    # GPU instructions: no case here reaches them
+    return re.sub(r'asm volatile\(\s*"(?!")[^;]*;', "std::abort();", text)
 
 
 def build(name, folder):

@@ -465,7 +465,7 @@ class AdamW:
         self.t = 0
         self._numel = [p.numel() for p in self.params]
         blocks = [(-(-k // ADST_STATE_BLOCK),) for k in self._numel]
-        names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
+        self._states = names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
         for name in names:
             needed = blocks if name.endswith("scale") else shapes
             dtype = (torch.float32 if name.endswith("scale") else
@@ -555,7 +555,9 @@ class AdamW:
         prob.grad_dtype = code
         prob.t = t
         prob.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
-        used = () if stream is None else (*self.params, *grads, grad_scale)
+        used = () if stream is None else (*self.params, *grads, *(self.copies or ()), grad_scale,
+                                          *(t for name in self._states
+                                            for t in getattr(self, name)))
         _call(device, stream, used,
               lambda handle: _check(lib().adst_adamw(prob, rows, self._n, handle)))
         self.t = prob.t

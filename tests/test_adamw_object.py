@@ -17,6 +17,7 @@ class Calls:
 
     def __init__(self):
         self.made = []
+        self.used = []  # what each call records on its stream
         self.native = None
 
     def adst_adamw(self, prob, rows, n, handle):
@@ -33,7 +34,12 @@ def calls(monkeypatch):
     monkeypatch.setattr(sequence, "lib", lambda: c)
     monkeypatch.setattr(sequence, "_binding", lambda: c)
     monkeypatch.setattr(sequence, "_code", lambda name, t: sequence._codes()[t.dtype])
-    monkeypatch.setattr(sequence, "_call", lambda device, stream, used, body: body(0))
+
+    def call(device, stream, used, body):
+        c.used.append(used)
+        return body(0)
+
+    monkeypatch.setattr(sequence, "_call", call)
     return c
 
 
@@ -97,3 +103,16 @@ def test_lists_of_another_length(calls, name):
     with pytest.raises(ValueError):
         opt.step(grads)
     assert not calls.made
+
+
+@pytest.mark.parametrize("copies", [True, False])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_everything_that_a_call_touches_is_recorded_on_its_stream(calls, bits, copies):
+    """Else memory that the step still writes could be given to others when its owner goes."""
+    opt, grads = make(bits, copies)
+    scale = torch.ones(1)
+    opt.step(grads, grad_scale=scale, stream=7)
+    names = ["params", "m", "v"] + (["m_scale", "v_scale"] if bits == 8 else []) + \
+        (["copies"] if copies else [])
+    expected = [scale, *grads] + [t for n in names for t in getattr(opt, n)]
+    assert {id(t) for t in calls.used[0]} == {id(t) for t in expected}

@@ -330,48 +330,70 @@ PyObject* recurrence_step(PyObject* module, Args x, Py_ssize_t n) {
 }
 
 // --------------------------------------------------------------------- AdamW
-// (problem's address, descriptors' address, their number, params, m, grads,
-// copies or None, grad_scale or None, t): True where the step was made. The
-// problem and the descriptors are the caller's; p, grad and copy, the
-// gradients' type, the scale and t are filled in here. What a tensor was when
-// the object was made, it has to be at each step: m has the shapes of all.
+// (problem's address, descriptors' address, their number, params, states,
+// grads, copies or None, grad_scale or None, t), states the tuple of m and v,
+// with 8 bits also of their scales: True where the step was made. The problem
+// and the descriptors are the caller's; the addresses, the gradients' type, the
+// scale and t are filled in here. What a tensor was when the object was made,
+// it has to be at each step.
 PyObject* adamw_step(PyObject* module, Args a, Py_ssize_t n) {
   return ordinary(module, [&] {
-    need(n == 9 && PyTuple_Check(a[3]) && PyTuple_Check(a[4]) &&
-         (a[6] == Py_None || PyTuple_Check(a[6])) && (PyList_Check(a[5]) || PyTuple_Check(a[5])));
+    need(n == 9 && (PyList_Check(a[5]) || PyTuple_Check(a[5])));
     auto* const prob = static_cast<adst_adamw_problem*>(PyLong_AsVoidPtr(a[0]));
     auto* const rows = static_cast<adst_adamw_tensor*>(PyLong_AsVoidPtr(a[1]));
     need(prob && rows);
     const Py_ssize_t count = (Py_ssize_t)whole(a[2]);
-    need(count > 0 && PyTuple_GET_SIZE(a[3]) == count && PyTuple_GET_SIZE(a[4]) == count &&
-         PySequence_Fast_GET_SIZE(a[5]) == count &&
-         (a[6] == Py_None || PyTuple_GET_SIZE(a[6]) == count));
+    need(count > 0 && PySequence_Fast_GET_SIZE(a[5]) == count);
+    const auto tuple = [count](PyObject* o) {
+      need(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == count);
+      return PySequence_Fast_ITEMS(o);
+    };
     const auto held = [](PyObject* o) -> const at::Tensor& {
       need(THPVariable_Check(o));
       return THPVariable_Unpack(o);
     };
+    const bool coded = prob->bits == 8;
+    need(PyTuple_Check(a[4]) && PyTuple_GET_SIZE(a[4]) == (coded ? 4 : 2));
+    PyObject** const params = tuple(a[3]);
+    PyObject** const ms = tuple(PyTuple_GET_ITEM(a[4], 0));
+    PyObject** const vs = tuple(PyTuple_GET_ITEM(a[4], 1));
+    PyObject** const m_scales = coded ? tuple(PyTuple_GET_ITEM(a[4], 2)) : nullptr;
+    PyObject** const v_scales = coded ? tuple(PyTuple_GET_ITEM(a[4], 3)) : nullptr;
+    PyObject** const copies = a[6] == Py_None ? nullptr : tuple(a[6]);
     PyObject** const grads = PySequence_Fast_ITEMS(a[5]);
-    const Here h = here(held(PyTuple_GET_ITEM(a[3], 0)));
+    const Here h = here(held(params[0]));
     const at::ScalarType type = held(grads[0]).scalar_type();
     const int code = code_of(held(grads[0]));
     need((code == ADST_F64) == (prob->dtype == ADST_F64));
+    const at::ScalarType kind = prob->dtype == ADST_F64 ? at::kDouble : at::kFloat;
+    const at::ScalarType state = coded ? at::kFloat8_e4m3fn : kind;
+    // the tensor's address, where it is one of `numel` values in order
+    const auto at = [&](PyObject* o, at::ScalarType type, int64_t numel) {
+      const at::Tensor& t = held(o);
+      need(t.scalar_type() == type && t.device() == h.device && t.numel() == numel &&
+           t.is_contiguous());
+      return t.data_ptr();
+    };
     for (Py_ssize_t i = 0; i < count; ++i) {
-      const at::Tensor& g = held(grads[i]);
-      const at::Tensor& p = held(PyTuple_GET_ITEM(a[3], i));
-      need(g.scalar_type() == type && g.device() == h.device && g.numel() == rows[i].n &&
-           g.is_contiguous());
-      need(code_of(p) == prob->dtype && p.device() == h.device && p.numel() == rows[i].n &&
-           p.is_contiguous() && p.sizes() == held(PyTuple_GET_ITEM(a[4], i)).sizes());
-      rows[i].grad = g.data_ptr();
-      rows[i].p = p.data_ptr();
-    }
-    if (a[6] != Py_None)
-      for (Py_ssize_t i = 0; i < count; ++i) {
-        const at::Tensor& c = held(PyTuple_GET_ITEM(a[6], i));
-        need(code_of(c) == prob->copy_dtype && c.device() == h.device && c.is_contiguous() &&
-             c.sizes() == held(PyTuple_GET_ITEM(a[4], i)).sizes());
-        rows[i].copy = c.data_ptr();
+      adst_adamw_tensor& r = rows[i];
+      r.grad = at(grads[i], type, r.n);
+      r.p = at(params[i], kind, r.n);
+      r.m = at(ms[i], state, r.n);
+      r.v = at(vs[i], state, r.n);
+      const at::IntArrayRef shape = held(params[i]).sizes();
+      need(held(ms[i]).sizes() == shape && held(vs[i]).sizes() == shape);
+      if (coded) {
+        const int64_t blocks = (r.n + ADST_STATE_BLOCK - 1) / ADST_STATE_BLOCK;
+        r.m_scale = static_cast<float*>(at(m_scales[i], at::kFloat, blocks));
+        r.v_scale = static_cast<float*>(at(v_scales[i], at::kFloat, blocks));
       }
+      r.copy = nullptr;
+      if (copies) {
+        const at::Tensor& c = held(copies[i]);
+        need(code_of(c) == prob->copy_dtype && c.sizes() == shape);
+        r.copy = at(copies[i], c.scalar_type(), r.n);
+      }
+    }
     const at::Tensor scale = maybe(a[7]);
     if (scale.defined())
       need(scale.scalar_type() == at::kFloat && scale.numel() == 1 && scale.device() == h.device);

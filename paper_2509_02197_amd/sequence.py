@@ -426,7 +426,9 @@ class AdamW:
     state: {"m", "v"} (and "m_scale", "v_scale" with 8 bits), lists of tensors like those this
     object holds under these names, to go on from; zeros if None. copies: contiguous tensors
     shaped like params, one dtype of float32, bfloat16 and float16, that receive the new
-    parameters in it. lr and weight_decay: a number, or one for each tensor."""
+    parameters in it. lr and weight_decay: a number, or one for each tensor. The lists params,
+    m, v, m_scale, v_scale and copies may be replaced by others like them; each step looks up
+    and checks what they hold."""
 
     def __init__(self, params, bits=32, state=None, copies=None, lr=1e-3, betas=(0.9, 0.999),
                  eps=1e-8, weight_decay=0.01):
@@ -457,19 +459,21 @@ class AdamW:
             if copy_code == ADST_F64:
                 raise TypeError("copies must be float32, bfloat16 or float16")
             _expect_all("copies", self.copies, shapes, self.copies[0].dtype, self.device)
-        self._shapes = shapes
-        self._types = {"params": first.dtype,
-                       "copies": None if self.copies is None else self.copies[0].dtype}
         self.bits = bits
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
         self.t = 0
         self._numel = [p.numel() for p in self.params]
         blocks = [(-(-k // ADST_STATE_BLOCK),) for k in self._numel]
-        self._states = names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
-        for name in names:
-            needed = blocks if name.endswith("scale") else shapes
-            dtype = (torch.float32 if name.endswith("scale") else
-                     torch.float8_e4m3fn if bits == 8 else first.dtype)
+        self._states = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
+        # what each list holds: the tensors' shapes and type
+        self._held = {"params": (shapes, first.dtype)}
+        if self.copies is not None:
+            self._held["copies"] = shapes, self.copies[0].dtype
+        for name in self._states:
+            self._held[name] = (
+                (blocks, torch.float32) if name.endswith("scale") else
+                (shapes, torch.float8_e4m3fn if bits == 8 else first.dtype))
+            needed, dtype = self._held[name]
             if state is None:
                 held = tuple(torch.zeros(s, dtype=dtype, device=self.device) for s in needed)
             else:
@@ -482,9 +486,6 @@ class AdamW:
         self._rows = (adst_adamw_tensor * n)()
         # the same memory as 8-byte words: p, grad, m, v, m_scale, v_scale, copy, n, lr, decay
         self._words = np.frombuffer(self._rows, dtype=np.uint64).reshape(n, -1)
-        for name, word in zip(("m", "v", "m_scale", "v_scale"), range(2, 6)):
-            if name in names:
-                self._words[:, word] = [t.data_ptr() for t in getattr(self, name)]
         self._words[:, 7] = self._numel
         self._set("lr", lr)
         self._set("weight_decay", weight_decay)
@@ -493,15 +494,17 @@ class AdamW:
         self._descriptors = ctypes.addressof(self._prob), ctypes.addressof(self._rows), n
 
     def _expect_held(self):
-        """The parameters and copies are still what they were when this object was made (a
-        module that is moved or converted gives its parameters other memory)."""
-        for name in ("params", "copies"):
+        """The lists hold what they did when this object was made: another list, or other memory
+        (which a module gives its parameters when it is moved), is taken where it is alike."""
+        if self.copies is not None and "copies" not in self._held:
+            raise ValueError("copies were not there when the object was made")
+        for name, (shapes, dtype) in self._held.items():
             tensors = getattr(self, name)
-            if tensors is None:
+            if name == "copies" and tensors is None:
                 continue
             if len(tensors) != self._n:
-                raise ValueError(f"{len(tensors)} {name}, not {self._n}")
-            _expect_all(name, tensors, self._shapes, self._types[name], self.device)
+                raise ValueError(f"{len(tensors)} {name} for {self._n} parameters")
+            _expect_all(name, tensors, shapes, dtype, self.device)
 
     def _set(self, name, value):
         values = [value] * self._n if isinstance(value, (int, float)) else list(value)
@@ -521,7 +524,9 @@ class AdamW:
             self._set("weight_decay", weight_decay)
         if t is None:
             t = self.t + 1
-        if stream is None and _binding().adamw_step(*self._descriptors, self.params, self.m,
+        states = ((self.m, self.v, self.m_scale, self.v_scale) if self.bits == 8 else
+                  (self.m, self.v))
+        if stream is None and _binding().adamw_step(*self._descriptors, self.params, states,
                                                     grads, self.copies, grad_scale, t):
             self.t = t
             return
@@ -545,19 +550,19 @@ class AdamW:
         rows = self._rows
         self._words[:, 0] = list(map(kind.data_ptr, self.params))
         self._words[:, 1] = list(map(kind.data_ptr, grads))
+        for word, tensors in enumerate(states, 2):
+            self._words[:, word] = list(map(kind.data_ptr, tensors))
+        self._words[:, 6] = 0 if self.copies is None else list(map(kind.data_ptr, self.copies))
         if grad_scale is not None:
             _expect("grad_scale", grad_scale, grad_scale.shape, torch.float32, device)
             if grad_scale.numel() != 1:
                 raise ValueError("grad_scale must have one value")
-        if self.copies is not None:
-            self._words[:, 6] = list(map(kind.data_ptr, self.copies))
         prob = self._prob
         prob.grad_dtype = code
         prob.t = t
         prob.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
         used = () if stream is None else (*self.params, *grads, *(self.copies or ()), grad_scale,
-                                          *(t for name in self._states
-                                            for t in getattr(self, name)))
+                                          *(t for tensors in states for t in tensors))
         _call(device, stream, used,
               lambda handle: _check(lib().adst_adamw(prob, rows, self._n, handle)))
         self.t = prob.t

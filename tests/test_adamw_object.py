@@ -60,7 +60,7 @@ CHANGES = {
 
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("which", [0, 1])
-@pytest.mark.parametrize("name", ["params", "copies"])
+@pytest.mark.parametrize("name", ["params", "copies", "m", "v"])
 @pytest.mark.parametrize("change", CHANGES)
 def test_tensors_that_are_not_what_they_were(calls, change, name, which, bits):
     opt, grads = make(bits)
@@ -116,3 +116,41 @@ def test_everything_that_a_call_touches_is_recorded_on_its_stream(calls, bits, c
         (["copies"] if copies else [])
     expected = [scale, *grads] + [t for n in names for t in getattr(opt, n)]
     assert {id(t) for t in calls.used[0]} == {id(t) for t in expected}
+
+
+@pytest.mark.parametrize("name", ["m", "v", "m_scale", "v_scale"])
+@pytest.mark.parametrize("how", ["list", "tuple", "data"])
+def test_states_that_were_replaced_are_followed(calls, name, how):
+    opt, grads = make(8)
+    loaded = [torch.zeros_like(t) for t in getattr(opt, name)]
+    if how == "data":
+        for t, new in zip(getattr(opt, name), loaded):
+            t.data = new
+    else:
+        setattr(opt, name, loaded if how == "list" else tuple(loaded))
+    opt.step(grads)
+    assert [r[name] for r in calls.made[0]] == [t.data_ptr() for t in loaded]
+
+
+def test_copies_that_were_dropped_are_not_written(calls):
+    opt, grads = make()
+    opt.step(grads)
+    opt.copies = None
+    opt.step(grads)
+    assert calls.made[0][0]["copy"] and calls.made[1][0]["copy"] is None
+    other, _ = make(copies=False)
+    other.copies = opt.params
+    with pytest.raises(ValueError, match="copies"):
+        other.step(grads)
+
+
+@pytest.mark.parametrize("name", ["m_scale", "v_scale"])
+def test_scales_that_are_not_what_they_were(calls, name):
+    for new in (lambda t: t[:-1], lambda t: t.double(), lambda t: t.repeat(2)[::2]):
+        opt, grads = make(8)
+        held = list(getattr(opt, name))
+        held[0] = new(held[0])
+        setattr(opt, name, held)
+        with pytest.raises(ValueError, match=name):
+            opt.step(grads)
+    assert not calls.made

@@ -75,3 +75,50 @@ def test_other_memory_of_the_same_kind_is_followed(bits):
     opt.step(grads)
     other.step(grads)
     assert equal(bits_of(opt), bits_of(other)) and torch.equal(old, kept)
+
+
+@pytest.mark.parametrize("how", ["list", "tuple", "data"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_that_were_replaced_are_followed(bits, how):
+    opt, grads = make(bits)
+    other, _ = make(bits)
+    opt.step(grads)
+    other.step(grads)
+    names = ["m", "v"] + (["m_scale", "v_scale"] if bits == 8 else []) + ["copies"]
+    old = {n: [t.data for t in getattr(opt, n)] for n in names}
+    kept = {n: [t.clone() for t in old[n]] for n in names}
+    for n in names:
+        new = [t.clone() for t in old[n]]
+        if how == "data":
+            for t, d in zip(getattr(opt, n), new):
+                t.data = d
+        else:
+            setattr(opt, n, new if how == "list" else tuple(new))
+    for x in (opt, other):
+        x.step(grads)
+    assert equal(bits_of(opt), bits_of(other))
+    assert all(torch.equal(x.float(), y.float()) for n in names for x, y in zip(old[n], kept[n]))
+
+
+def test_copies_that_were_dropped_are_not_written():
+    opt, grads = make()
+    opt.step(grads)
+    old = opt.copies
+    kept = [t.clone() for t in old]
+    opt.copies = None
+    opt.step(grads)
+    assert equal(old, kept)
+
+
+@pytest.mark.parametrize("name", ["m", "v", "m_scale", "v_scale"])
+def test_states_that_are_not_what_they_were(name):
+    opt, grads = make(8)
+    opt.step(grads)
+    before = bits_of(opt)
+    held = getattr(opt, name)
+    for new in (lambda t: t[:-1], lambda t: t.float().double(), lambda t: t.cpu(), lambda t: None):
+        setattr(opt, name, tuple(new(t) for t in held))
+        with pytest.raises(ValueError, match=name):
+            opt.step(grads)
+    setattr(opt, name, held)
+    assert equal(bits_of(opt), before)

@@ -428,7 +428,7 @@ class AdamW:
     shaped like params, one dtype of float32, bfloat16 and float16, that receive the new
     parameters in it. lr and weight_decay: a number, or one for each tensor. The lists params,
     m, v, m_scale, v_scale and copies may be replaced by others like them; each step looks up
-    and checks what they hold."""
+    and checks what they hold. lr, weight_decay, betas and eps may be assigned between steps."""
 
     def __init__(self, params, bits=32, state=None, copies=None, lr=1e-3, betas=(0.9, 0.999),
                  eps=1e-8, weight_decay=0.01):
@@ -459,8 +459,7 @@ class AdamW:
             if copy_code == ADST_F64:
                 raise TypeError("copies must be float32, bfloat16 or float16")
             _expect_all("copies", self.copies, shapes, self.copies[0].dtype, self.device)
-        self.bits = bits
-        self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
+        self._bits = bits
         self.t = 0
         self._numel = [p.numel() for p in self.params]
         blocks = [(-(-k // ADST_STATE_BLOCK),) for k in self._numel]
@@ -487,10 +486,8 @@ class AdamW:
         # the same memory as 8-byte words: p, grad, m, v, m_scale, v_scale, copy, n, lr, decay
         self._words = np.frombuffer(self._rows, dtype=np.uint64).reshape(n, -1)
         self._words[:, 7] = self._numel
-        self._set("lr", lr)
-        self._set("weight_decay", weight_decay)
-        self._prob = adst_adamw_problem(code, ADST_F32, copy_code, bits, 0, *self.betas, self.eps,
-                                        None)
+        self._prob = adst_adamw_problem(code, ADST_F32, copy_code, bits)
+        self.lr, self.weight_decay, self.betas, self.eps = lr, weight_decay, betas, eps
         self._descriptors = ctypes.addressof(self._prob), ctypes.addressof(self._rows), n
 
     def _expect_held(self):
@@ -506,12 +503,50 @@ class AdamW:
                 raise ValueError(f"{len(tensors)} {name} for {self._n} parameters")
             _expect_all(name, tensors, shapes, dtype, self.device)
 
-    def _set(self, name, value):
+    def _rates(self, name, value, word):
+        """value, one number or one for each tensor, into the descriptors."""
         values = [value] * self._n if isinstance(value, (int, float)) else list(value)
         if len(values) != self._n:
             raise ValueError(f"{len(values)} values of {name} for {self._n} parameters")
-        setattr(self, name, value)
-        self._words.view(np.float64)[:, 8 if name == "lr" else 9] = values
+        self._words.view(np.float64)[:, word] = values
+        return value
+
+    # What the descriptors hold is changed with the attribute.
+    @property
+    def lr(self):
+        return self._lr
+
+    @lr.setter
+    def lr(self, value):
+        self._lr = self._rates("lr", value, 8)
+
+    @property
+    def weight_decay(self):
+        return self._weight_decay
+
+    @weight_decay.setter
+    def weight_decay(self, value):
+        self._weight_decay = self._rates("weight_decay", value, 9)
+
+    @property
+    def betas(self):
+        return self._prob.beta1, self._prob.beta2
+
+    @betas.setter
+    def betas(self, value):
+        self._prob.beta1, self._prob.beta2 = map(float, value)
+
+    @property
+    def eps(self):
+        return self._prob.eps
+
+    @eps.setter
+    def eps(self, value):
+        self._prob.eps = float(value)
+
+    @property
+    def bits(self):  # of the states that this object was made with
+        return self._bits
 
     def step(self, grads, lr=None, weight_decay=None, t=None, grad_scale=None, stream=None):
         """One step with contiguous gradients like params (float32, bfloat16 or float16, one
@@ -519,9 +554,9 @@ class AdamW:
         than the last one's if None. grad_scale: a float32 tensor of one value that multiplies the
         gradients; where it is not finite nothing is updated (the step's number counts on)."""
         if lr is not None:
-            self._set("lr", lr)
+            self.lr = lr
         if weight_decay is not None:
-            self._set("weight_decay", weight_decay)
+            self.weight_decay = weight_decay
         if t is None:
             t = self.t + 1
         states = ((self.m, self.v, self.m_scale, self.v_scale) if self.bits == 8 else

@@ -17,10 +17,12 @@ class Calls:
 
     def __init__(self):
         self.made = []
+        self.problems = []
         self.used = []  # what each call records on its stream
         self.native = None
 
     def adst_adamw(self, prob, rows, n, handle):
+        self.problems.append({k: getattr(prob, k) for k, _ in prob._fields_})
         self.made.append([{k: getattr(r, k) for k, _ in r._fields_} for r in rows])
         return adst.ADST_OK
 
@@ -154,3 +156,23 @@ def test_scales_that_are_not_what_they_were(calls, name):
         with pytest.raises(ValueError, match=name):
             opt.step(grads)
     assert not calls.made
+
+
+def test_rates_that_are_assigned_take_effect(calls):
+    opt, grads = make()
+    opt.lr, opt.weight_decay, opt.betas, opt.eps = 0.5, [0.25, 0.125], (0.5, 0.75), 1e-3
+    assert (opt.lr, opt.weight_decay, opt.betas, opt.eps) == (0.5, [0.25, 0.125], (0.5, 0.75), 1e-3)
+    opt.step(grads)
+    assert [r["lr"] for r in calls.made[0]] == [0.5, 0.5]
+    assert [r["weight_decay"] for r in calls.made[0]] == [0.25, 0.125]
+    p = calls.problems[0]
+    assert (p["beta1"], p["beta2"], p["eps"]) == (0.5, 0.75, 1e-3)
+    opt.step(grads, lr=2.0)
+    assert opt.lr == 2.0 and calls.made[1][1]["lr"] == 2.0
+    with pytest.raises(ValueError, match="lr"):
+        opt.lr = [1.0]
+    with pytest.raises((TypeError, ValueError)):
+        opt.betas = (0.5,)
+    with pytest.raises(AttributeError):
+        opt.bits = 8
+    assert opt.lr == 2.0 and opt.betas == (0.5, 0.75) and opt.bits == 32

@@ -122,3 +122,13 @@ def test_states_that_are_not_what_they_were(name):
             opt.step(grads)
     setattr(opt, name, held)
     assert equal(bits_of(opt), before)
+
+
+def test_rates_that_are_assigned_take_effect():
+    opt, grads = make()
+    opt.lr, opt.weight_decay, opt.betas, opt.eps = 0.5, 0.25, (0.5, 0.75), 1e-3
+    other = adst.AdamW(make()[0].params, copies=make()[0].copies, lr=0.5, weight_decay=0.25,
+                       betas=(0.5, 0.75), eps=1e-3)
+    for x in (opt, other):
+        x.step(grads)
+    assert equal(bits_of(opt), bits_of(other))

@@ -84,6 +84,12 @@ void run(adst_status s) {
   need(s == ADST_OK);
 }
 
+// A tensor that a call writes in place: autograd's checks of saved tensors are
+// to see the change.
+void changed(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // {name: tensor or None}
 class Dict {
  public:
@@ -324,6 +330,7 @@ PyObject* recurrence_step(PyObject* module, Args x, Py_ssize_t n) {
                              static_cast<const int32_t*>(at_of(slots)), state.data_ptr(),
                              state.size(0), out.data_ptr(), h.stream);
     if (status != ADST_OK) Py_DECREF(r);
+    if (status == ADST_OK || status == ADST_ERR_HIP) changed(state);
     run(status);
     return r;
   });
@@ -400,7 +407,11 @@ PyObject* adamw_step(PyObject* module, Args a, Py_ssize_t n) {
     prob->grad_dtype = code;
     prob->grad_scale = static_cast<const float*>(at_of(scale));
     prob->t = whole(a[8]);
-    run(adst_adamw(prob, rows, (int32_t)count, h.stream));
+    const adst_status status = adst_adamw(prob, rows, (int32_t)count, h.stream);
+    if (status == ADST_OK || status == ADST_ERR_HIP)
+      for (PyObject** list : {params, ms, vs, m_scales, v_scales, copies})
+        for (Py_ssize_t i = 0; list && i < count; ++i) changed(held(list[i]));
+    run(status);
     return Py_NewRef(Py_True);
   });
 }

@@ -16,8 +16,8 @@ from operator import attrgetter
 import numpy as np
 
 from . import build as _build
-from . import (ADST_BF16, ADST_F16, ADST_F32, ADST_F64, ADST_GATE_COEFF, ADST_GATE_SIGMOID,
-               ADST_STATE_BLOCK, AdstError, _check, _ptr, _stream, adst_adamw_problem,
+from . import (ADST_BF16, ADST_ERR_HIP, ADST_F16, ADST_F32, ADST_F64, ADST_GATE_COEFF,
+               ADST_GATE_SIGMOID, ADST_OK, ADST_STATE_BLOCK, AdstError, _check, _ptr, _stream, adst_adamw_problem,
                adst_adamw_tensor, adst_norm_problem, adst_recurrence_info,
                adst_recurrence_problem, lib)
 
@@ -183,6 +183,15 @@ def _bytes(n, device):
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
+def _check_in_place(status, tensors):
+    """_check of a call that writes the tensors in place: autograd's checks of saved tensors are
+    to see the change."""
+    import torch
+    if status in (ADST_OK, ADST_ERR_HIP):
+        torch.autograd.graph.increment_version(tensors)
+    _check(status)
+
+
 def _at(t):
     return None if t is None else t.data_ptr()
 
@@ -304,8 +313,9 @@ def recurrence_step(a, u, state, slots=None, gate=ADST_GATE_COEFF, stream=None):
 
     def body(handle):
         h = torch.empty_like(a, memory_format=torch.contiguous_format)
-        _check(lib().adst_recurrence_step(prob, a.data_ptr(), u.data_ptr(), _at(slots),
-                                          state.data_ptr(), state.shape[0], h.data_ptr(), handle))
+        _check_in_place(lib().adst_recurrence_step(prob, a.data_ptr(), u.data_ptr(), _at(slots),
+                                                   state.data_ptr(), state.shape[0],
+                                                   h.data_ptr(), handle), (state,))
         return h
 
     return _call(a.device, stream, (a, u, state, slots), body)
@@ -596,8 +606,8 @@ class AdamW:
         prob.grad_dtype = code
         prob.t = t
         prob.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
-        used = () if stream is None else (*self.params, *grads, *(self.copies or ()), grad_scale,
-                                          *(t for tensors in states for t in tensors))
-        _call(device, stream, used,
-              lambda handle: _check(lib().adst_adamw(prob, rows, self._n, handle)))
+        written = (*self.params, *(self.copies or ()), *(t for held in states for t in held))
+        used = () if stream is None else (*written, *grads, grad_scale)
+        _call(device, stream, used, lambda handle: _check_in_place(
+            lib().adst_adamw(prob, rows, self._n, handle), written))
         self.t = prob.t

@@ -176,3 +176,14 @@ def test_rates_that_are_assigned_take_effect(calls):
     with pytest.raises(AttributeError):
         opt.bits = 8
     assert opt.lr == 2.0 and opt.betas == (0.5, 0.75) and opt.bits == 32
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_tensors_versions_rise(calls, bits):
+    """Autograd's check of saved tensors sees the step."""
+    opt, grads = make(bits)
+    names = ["params", "m", "v", "copies"] + (["m_scale", "v_scale"] if bits == 8 else [])
+    before = {n: [t._version for t in getattr(opt, n)] for n in names}
+    opt.step(grads)
+    for n in names:
+        assert all(t._version > v for t, v in zip(getattr(opt, n), before[n]))

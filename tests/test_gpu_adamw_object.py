@@ -132,3 +132,38 @@ def test_rates_that_are_assigned_take_effect():
     for x in (opt, other):
         x.step(grads)
     assert equal(bits_of(opt), bits_of(other))
+
+
+@pytest.mark.parametrize("stream", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_tensors_versions_rise(bits, stream):
+    """Autograd's check of saved tensors sees the step."""
+    on = torch.cuda.Stream() if stream else None
+    opt, grads = make(bits)
+    names = ["params", "m", "v", "copies"] + (["m_scale", "v_scale"] if bits == 8 else [])
+    before = {n: [t._version for t in getattr(opt, n)] for n in names}
+    w = opt.params[0].requires_grad_()
+    loss = (w * w).sum()
+    opt.step(grads, stream=on)
+    torch.cuda.synchronize()
+    for n in names:
+        assert all(t._version > v for t, v in zip(getattr(opt, n), before[n]))
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        loss.backward()
+
+
+@pytest.mark.parametrize("stream", [False, True])
+def test_a_pools_version_rises(stream):
+    on = torch.cuda.Stream() if stream else None
+    a, u, state = (torch.randn(4, 40, device="cuda") for _ in range(3))
+    torch.cuda.synchronize()
+    before = state._version
+    adst.recurrence_step(a, u, state, stream=on)
+    torch.cuda.synchronize()
+    assert state._version > before
+    with torch.inference_mode():
+        pool = torch.zeros(4, 40, device="cuda")
+    torch.cuda.synchronize()
+    adst.recurrence_step(a, u, pool, stream=on)
+    torch.cuda.synchronize()
+    assert bool((pool != 0).any())

@@ -138,6 +138,11 @@ def _expect(name, t, shape, dtype, device, contiguous=True):
         raise ValueError(f"{name} must be contiguous")
 
 
+def _require(name, t):
+    if not hasattr(t, "data_ptr"):
+        raise ValueError(f"{name} is required" if t is None else f"{name} must be a torch tensor")
+
+
 def _expect_all(name, tensors, shapes, dtype, device):
     """_expect for a list: what a right list passes at once, then one by one for the message."""
     import torch
@@ -150,8 +155,7 @@ def _expect_all(name, tensors, shapes, dtype, device):
     except (AttributeError, TypeError):
         pass
     for i, (t, shape) in enumerate(zip(tensors, shapes)):
-        if t is None:
-            raise ValueError(f"{name}[{i}] must be a torch tensor")
+        _require(f"{name}[{i}]", t)
         _expect((name, i), t, shape, dtype, device)
 
 
@@ -201,6 +205,7 @@ def _recurrence_problem(a, u, gate, dh=None):
     code = _code("a", a)
     if a.dim() != 3:
         raise ValueError(f"a must be [batch, steps, channels], not {tuple(a.shape)}")
+    _require("u", u)
     _expect("u", u, a.shape, a.dtype, a.device, contiguous=False)
     _channels_contiguous("a", a)
     _channels_contiguous("u", u)
@@ -263,8 +268,7 @@ def recurrence_vjp(a, u, dh, h0=None, lens=None, dhT=None, ck=None, gate=ADST_GA
         if done is not None:
             return done
     import torch
-    if dh is None:
-        raise ValueError("dh is required")
+    _require("dh", dh)
     prob = _recurrence_problem(a, u, gate, dh)
     B, T, D = a.shape
     acc = _acc(prob.dtype)
@@ -302,10 +306,12 @@ def recurrence_step(a, u, state, slots=None, gate=ADST_GATE_COEFF, stream=None):
     if a.dim() != 2:
         raise ValueError(f"a must be [batch, channels], not {tuple(a.shape)}")
     B, D = a.shape
+    _require("u", u)
     _expect("u", u, (B, D), a.dtype, a.device, contiguous=False)
     _channels_contiguous("a", a)
     _channels_contiguous("u", u)
-    if state is None or state.dim() != 2 or state.shape[1] != D:
+    _require("state", state)
+    if state.dim() != 2 or state.shape[1] != D:
         raise ValueError(f"state must be [nstates, {D}]")
     _expect("state", state, state.shape, _acc(code), a.device)
     _expect("slots", slots, (B,), torch.int32, a.device)
@@ -400,13 +406,11 @@ def layer_norm_vjp(x, dy, mean, rstd, w=None, want_dx=True, want_dw=True, want_d
         if done is not None:
             return done
     import torch
-    if dy is None:
-        raise ValueError("dy is required")
+    _require("dy", dy)
     prob = _norm_problem(x, w, None, 0.0, dy)
     acc = _acc(prob.dtype)
     for name, t in (("mean", mean), ("rstd", rstd)):
-        if t is None:
-            raise ValueError(f"{name} is required")
+        _require(name, t)
         _expect(name, t, x.shape[:-1], acc, x.device)
     wt = w.dtype if w is not None else x.dtype
 
@@ -456,8 +460,7 @@ class AdamW:
                             f"not {first.dtype}")
         self.device = first.device
         for i, p in enumerate(self.params):
-            if not hasattr(p, "shape"):
-                raise ValueError(f"params[{i}] must be a torch tensor")
+            _require(f"params[{i}]", p)
         shapes = list(map(_shape_of, self.params))
         _expect_all("params", self.params, shapes, first.dtype, self.device)
         self.copies = None if copies is None else tuple(copies)
@@ -486,6 +489,8 @@ class AdamW:
             if state is None:
                 held = tuple(torch.zeros(s, dtype=dtype, device=self.device) for s in needed)
             else:
+                if name not in state:
+                    raise ValueError(f"state has no {name}")
                 held = tuple(state[name])
                 if len(held) != n:
                     raise ValueError(f"{len(held)} tensors of state {name} for {n} parameters")
@@ -583,15 +588,19 @@ class AdamW:
         if (code == ADST_F64) != (self._prob.dtype == ADST_F64):
             raise TypeError(f"gradients of {self.params[0].dtype} parameters in {grads[0].dtype}")
         device, kind = self.device, torch.Tensor
-        if set(map(_dtype_of, grads)) != {grads[0].dtype} or \
-                set(map(kind.get_device, grads)) != {device.index} or \
-                list(map(kind.numel, grads)) != self._numel or \
-                not all(map(kind.is_contiguous, grads)):
-            for i, (g, n) in enumerate(zip(grads, self._numel)):
-                if g.dtype != grads[0].dtype or g.device != device or g.numel() != n or \
-                        not g.is_contiguous():
-                    raise ValueError(f"grads[{i}] must be contiguous, of {n} values in "
-                                     f"{grads[0].dtype} on {device}")
+        try:  # what a right list passes at once
+            right = set(map(_dtype_of, grads)) == {grads[0].dtype} and \
+                set(map(kind.get_device, grads)) == {device.index} and \
+                list(map(kind.numel, grads)) == self._numel and \
+                all(map(kind.is_contiguous, grads))
+        except (AttributeError, TypeError):
+            right = False
+        for i, (g, n) in enumerate(() if right else zip(grads, self._numel)):
+            _require(f"grads[{i}]", g)
+            if g.dtype != grads[0].dtype or g.device != device or g.numel() != n or \
+                    not g.is_contiguous():
+                raise ValueError(f"grads[{i}] must be contiguous, of {n} values in "
+                                 f"{grads[0].dtype} on {device}")
         rows = self._rows
         self._words[:, 0] = list(map(kind.data_ptr, self.params))
         self._words[:, 1] = list(map(kind.data_ptr, grads))
@@ -599,6 +608,7 @@ class AdamW:
             self._words[:, word] = list(map(kind.data_ptr, tensors))
         self._words[:, 6] = 0 if self.copies is None else list(map(kind.data_ptr, self.copies))
         if grad_scale is not None:
+            _require("grad_scale", grad_scale)
             _expect("grad_scale", grad_scale, grad_scale.shape, torch.float32, device)
             if grad_scale.numel() != 1:
                 raise ValueError("grad_scale must have one value")

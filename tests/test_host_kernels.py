@@ -33,3 +33,26 @@ def run(exe, *args):
     (0, 1, 1, 9000, 1, 0)])
 def test_recurrence(recurrence, case):
     run(recurrence, *case)
+
+
+@pytest.fixture(scope="module")
+def layer_norm(tmp_path_factory):
+    return program("layer_norm", tmp_path_factory)
+
+
+# (dtype, weights' dtype, rows, n, elements between rows). Rows of 16 lanes up to those longer
+# than a workgroup's registers, whole vectors and not.
+@pytest.mark.parametrize("case", [
+    (1, 1, 1, 1, 0), (1, 1, 5, 64, 0), (2, 1, 67, 100, 3), (2, 2, 9, 515, 0), (3, 3, 2, 2047, 1),
+    (0, 0, 4, 2047, 0), (1, 1, 3, 9000, 0), (2, 1, 2, 20011, 0), (1, 1, 2, 40000, 0),
+    (0, 0, 1, 9001, 0), (3, 1, 130, 8, 0), (2, 1, 700, 33, 0), (0, 0, 0, 30, 0),
+    (1, 1, 1, 16390, 5), (2, 2, 2, 33000, 0)])
+def test_layer_norm(layer_norm, case):
+    run(layer_norm, *case)
+
+
+@pytest.mark.parametrize("rows,n", [
+    (1, (1 << 26) - 1), (1, 1 << 26), (3, (1 << 26) + 1), (1, (1 << 31) - (1 << 16) - 1),
+    ((1 << 31) - (1 << 16) - 1, 1), (1 << 30, 5000), (5000, 1 << 30)])
+def test_layer_norm_of_any_extent_fits_a_dispatch(layer_norm, rows, n):
+    run(layer_norm, rows, n)

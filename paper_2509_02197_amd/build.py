@@ -1,9 +1,9 @@
 """Build step for libadst.so (gfx950).
 
 Host sources are compiled as C++ and the kernels as HIP, all with hipcc,
-then linked into ``libadst.so`` inside the package directory; beside it
-``_binding.so``, which takes torch tensors to its calls. Every compile of the
-library uses -ffp-contract=off (the forward steps are bit-reproducible in the
+then linked into ``libadst.so`` inside the package directory; beside it, where
+torch can be imported, ``_binding.so``, which takes torch tensors to its calls.
+The library itself needs only ROCm. Every compile of it uses -ffp-contract=off (the forward steps are bit-reproducible in the
 documented evaluation order) and disables packed-fp32 instructions.
 """
 import os
@@ -50,11 +50,16 @@ def _run(cmd, verbose):
 
 
 def _binding_commands():
-    """Compile and link of the binding, whose headers and libraries are torch's."""
-    import torch
+    """Compile and link of the binding, whose headers and libraries are torch's, or None
+    without torch."""
+    try:
+        import torch
+    except ImportError:
+        return None
     torch_dir = os.path.dirname(torch.__file__)
     obj = os.path.join(BUILD, "binding.cpp.o")
-    compile_ = ["g++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+    compile_ = [_hipcc(), "-x", "c++", "-std=c++17", "-O2", "-fPIC", "-Wall",
+                "-D__HIP_PLATFORM_AMD__=1",
                 "-D_GLIBCXX_USE_CXX11_ABI=" + str(int(torch._C._GLIBCXX_USE_CXX11_ABI)),
                 "-I" + os.path.join(ROOT, "include"),
                 "-isystem", sysconfig.get_paths()["include"],
@@ -62,17 +67,17 @@ def _binding_commands():
                 "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
                 "-isystem", os.path.join(ROCM, "include"),
                 "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj]
-    link = ["g++", "-shared", "-o", BINDING + ".tmp", obj, LIB,
-            "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip",
-            "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(torch_dir, "lib")]
+    link = [_hipcc(), "-shared", "-no-hip-rt", "-o", BINDING + ".tmp", obj, LIB,
+            "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+            "-lc10_hip", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(torch_dir, "lib")]
     return compile_, link
 
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     hipcc = _hipcc()
-    compile_binding, link_binding = _binding_commands()
-    jobs = [compile_binding]
+    binding = _binding_commands()
+    jobs = []
     for s in HOST_SOURCES:
         jobs.append([hipcc, "-x", "c++", "-D__HIP_PLATFORM_AMD__=1",
                      "-I" + os.path.join(ROCM, "include")] + COMMON +
@@ -80,15 +85,18 @@ def build(verbose: bool = False) -> str:
     for s in HIP_SOURCES:
         jobs.append([hipcc, "-x", "hip"] + COMMON + DEVICE +
                     ["-c", os.path.join(CSRC, s), "-o", os.path.join(BUILD, s + ".o")])
-    with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
+    with ThreadPoolExecutor(max_workers=len(jobs) + 1) as ex:
+        compiled = ex.submit(_run, binding[0], verbose) if binding else None
         list(ex.map(lambda c: _run(c, verbose), jobs))
-    objs = [os.path.join(BUILD, s + ".o") for s in HOST_SOURCES + HIP_SOURCES]
-    _run([hipcc, "-shared", "--offload-arch=" + ARCH, "-o", LIB + ".tmp"] + objs +
-         ["-L" + os.path.join(ROCM, "lib"), "-lrocprofiler-sdk-roctx",
-          "-Wl,-rpath," + os.path.join(ROCM, "lib")], verbose)
-    os.replace(LIB + ".tmp", LIB)
-    _run(link_binding, verbose)
-    os.replace(BINDING + ".tmp", BINDING)
+        objs = [os.path.join(BUILD, s + ".o") for s in HOST_SOURCES + HIP_SOURCES]
+        _run([hipcc, "-shared", "--offload-arch=" + ARCH, "-o", LIB + ".tmp"] + objs +
+             ["-L" + os.path.join(ROCM, "lib"), "-lrocprofiler-sdk-roctx",
+              "-Wl,-rpath," + os.path.join(ROCM, "lib")], verbose)
+        os.replace(LIB + ".tmp", LIB)
+        if binding:
+            compiled.result()
+            _run(binding[1], verbose)
+            os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 

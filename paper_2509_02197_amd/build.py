@@ -67,7 +67,8 @@ def _binding_commands():
                 "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
                 "-isystem", os.path.join(ROCM, "include"),
                 "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj]
-    link = [_hipcc(), "-shared", "-no-hip-rt", "-o", BINDING + ".tmp", obj, LIB,
+    link = [_hipcc(), "-shared", "-no-hip-rt", "-o", BINDING + ".tmp", obj,
+            "-L" + HERE, "-l:" + os.path.basename(LIB),  # found beside the binding ($ORIGIN)
             "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
             "-lc10_hip", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(torch_dir, "lib")]
     return compile_, link

@@ -1,6 +1,8 @@
 """What a build runs, with nothing run: the library needs ROCm's compiler alone, and the binding
 is built where torch is."""
 import os
+import shutil
+import subprocess
 import sys
 
 import pytest
@@ -48,3 +50,21 @@ def test_library_and_binding(commands):
     build.build()
     assert commands[-1] == ["replace", build.BINDING + ".tmp", build.BINDING]
     assert {os.path.basename(c[0]) for c in commands} == {"hipcc", "replace"}
+
+
+def test_a_moved_package_uses_its_own_library(tmp_path):
+    """Not the one at the place where it was built."""
+    pytest.importorskip("torch")
+    if not os.path.exists(build.BINDING):
+        build.build()
+    package = os.path.basename(build.HERE)
+    there = tmp_path / package
+    there.mkdir()
+    for name in os.listdir(build.HERE):
+        if name.endswith((".py", ".so")):
+            shutil.copy(os.path.join(build.HERE, name), there / name)
+    code = (f"import {package} as p; p.lib(); p.sequence._binding()\n"
+            "print(*{l.split()[-1] for l in open('/proc/self/maps') if 'libadst' in l})")
+    r = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    assert r.stdout.split() == [str(there / "libadst.so")]

@@ -648,39 +648,33 @@ __global__ __launch_bounds__(kColumnThreads) void norm_dw_long(NormArgs p, Acc<T
     if (i < n) out[i] = sw[i], out[p.n + i] = sb[i];
 }
 
-// dw and db from the workgroups' sums: 32 columns a workgroup at a time, 32
-// shares of the parts.
+// dw and db from the workgroups' sums, from column `first` on (of dw's columns,
+// then db's): 32 columns a workgroup, 32 shares of the parts.
 constexpr int kSumColumns = 32, kShares = 32;
-constexpr int64_t kSumGroups = 1 << 20;  // at most: a launch has fewer than 2^32 threads
 template <class T, class W>
 __global__ __launch_bounds__(kSumColumns * kShares) void norm_dw_sum(NormArgs p,
                                                                      const Acc<T>* part,
-                                                                     int parts) {
+                                                                     int parts, int64_t first) {
   typedef Acc<T> A;
   __shared__ A sums[kShares][kSumColumns];
   const int column = threadIdx.x % kSumColumns, share = threadIdx.x / kSumColumns;
-  const int each = (parts + kShares - 1) / kShares;
-  const int from = share * each, to = min(from + each, parts);
-  for (int64_t first = (int64_t)blockIdx.x * kSumColumns; first < 2 * p.n;
-       first += (int64_t)gridDim.x * kSumColumns) {
-    const int64_t c = first + column;  // of dw's columns, then db's
-    A s = A(0);
-    if (c < 2 * p.n) {
+  const int64_t c = first + (int64_t)blockIdx.x * kSumColumns + column;
+  A s = A(0);
+  if (c < 2 * p.n) {
+    const int each = (parts + kShares - 1) / kShares;
+    const int from = share * each, to = min(from + each, parts);
 #pragma unroll 16
-      for (int k = from; k < to; ++k) s += part[(int64_t)k * 2 * p.n + c];
-    }
-    sums[share][column] = s;
-    __syncthreads();
-    if (share == 0 && c < 2 * p.n) {
+    for (int k = from; k < to; ++k) s += part[(int64_t)k * 2 * p.n + c];
+  }
+  sums[share][column] = s;
+  __syncthreads();
+  if (share > 0 || c >= 2 * p.n) return;
 #pragma unroll
-      for (int k = 1; k < kShares; ++k) s += sums[k][column];
-      if (c < p.n) {
-        if (p.dw) ((W*)p.dw)[c] = down<W>((Acc<W>)s);
-      } else if (p.db) {
-        ((W*)p.db)[c - p.n] = down<W>((Acc<W>)s);
-      }
-    }
-    __syncthreads();
+  for (int k = 1; k < kShares; ++k) s += sums[k][column];
+  if (c < p.n) {
+    if (p.dw) ((W*)p.dw)[c] = down<W>((Acc<W>)s);
+  } else if (p.db) {
+    ((W*)p.db)[c - p.n] = down<W>((Acc<W>)s);
   }
 }
 
@@ -825,12 +819,17 @@ hipError_t norm_vjp(const NormArgs& a, void* ws, hipStream_t st) {
     typedef decltype(t) T;
     typedef decltype(w) W;
     Acc<T>* const part = sums ? (Acc<T>*)ws : nullptr;
-    const hipError_t e =
-        parts > 0 ? reverse_by_length<T, W>(a, nv, parts, part, st) : hipSuccess;
-    if (e != hipSuccess || !sums) return e;
+    hipError_t e = parts > 0 ? reverse_by_length<T, W>(a, nv, parts, part, st) : hipSuccess;
+    if (!sums) return e;
+    // a launch has fewer than 2^32 threads
+    constexpr int64_t kMostGroups = (int64_t(1) << 32) / (kSumColumns * kShares) - 1;
     const int64_t groups = (2 * a.n + kSumColumns - 1) / kSumColumns;
-    const unsigned grid = (unsigned)(groups < kSumGroups ? groups : kSumGroups);
-    return start(norm_dw_sum<T, W>, grid, kSumColumns * kShares, st, a, part, parts);
+    for (int64_t done = 0; e == hipSuccess && done < groups; done += kMostGroups) {
+      const int64_t now = groups - done < kMostGroups ? groups - done : kMostGroups;
+      e = start(norm_dw_sum<T, W>, (unsigned)now, kSumColumns * kShares, st, a, part, parts,
+                done * kSumColumns);
+    }
+    return e;
   });
 }
 

@@ -151,16 +151,16 @@ __device__ inline float inverse(float x) { return __builtin_amdgcn_rcpf(x); }  /
 __device__ inline double inverse(double x) { return 1.0 / x; }
 
 // s = 1 / (1 + exp(-a)) and q = 1 - s = 1 / (1 + exp(a)), each to full
-// relative precision. Behind a 16-bit value the exponential may be off by |a|
-// units of 2^-24, and gates below 2^-115 stop at that.
+// relative precision down to the type's smallest normal value, and 0 and 1 are
+// reached. Behind a 16-bit value the exponential may be off by |a| units of
+// 2^-24.
 template <class T>
 __device__ inline void gates(Acc<T> a, Acc<T>* s, Acc<T>* q) {
   typedef Acc<T> A;
   if constexpr (sizeof(T) == 2) {
-    const float x = -1.44269504f * a;
-    const float e = __builtin_amdgcn_exp2f(x > 115.0f ? 115.0f : x);  // NaN stays
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * a);
     *s = inverse(1.0f + e);
-    *q = e * *s;
+    *q = e > 0x1p126f ? 1.0f : e * *s;  // beyond, 1 / e is no normal value; NaN stays
   } else {  // with e = exp(-|a|) in [0, 1] nothing overflows, and 0 and 1 are reached
     const A e = exp_full(-__builtin_elementwise_abs(a));
     const A big = inverse(A(1) + e), small = e * big;

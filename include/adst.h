@@ -628,10 +628,12 @@ typedef struct {
                               it is not finite nothing is updated */
 } adst_adamw_problem;
 
-/* tensors: host array, read before the call returns. Errors: ADST_ERR_ARG
- * (NULL pointers, bad values or types, overlapping ranges within a tensor),
- * ADST_ERR_UNSUPPORTED (a tensor of 2^40 values or more), ADST_ERR_HIP (then
- * some of the tensors may have been updated: the step is not to be made again). */
+/* tensors: host array, read before the call returns. What is written of one
+ * tensor may not overlap any array of another (which is not checked). Errors:
+ * ADST_ERR_ARG (NULL pointers, bad values or types, overlapping ranges within a
+ * tensor), ADST_ERR_UNSUPPORTED (a tensor of 2^40 values or more), ADST_ERR_HIP
+ * (then some of the tensors may have been updated: the step is not to be made
+ * again). */
 adst_status adst_adamw(const adst_adamw_problem* prob, const adst_adamw_tensor* tensors,
                        int32_t n_tensors, hipStream_t stream);
 

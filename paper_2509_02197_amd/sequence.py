@@ -435,7 +435,8 @@ _dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
 class AdamW:
     """AdamW over a list of tensors, one call a step, updated in place.
 
-    params: contiguous float32 (or float64) tensors on one GPU. bits: 32 for states in the
+    params: contiguous float32 (or float64) tensors on one GPU, none of which shares memory with
+    another (a tied weight is listed once). bits: 32 for states in the
     parameters' type, 8 for blocks of 256 e4m3 codes with a scale each (float32 parameters).
     state: {"m", "v"} (and "m_scale", "v_scale" with 8 bits), lists of tensors like those this
     object holds under these names, to go on from; zeros if None. copies: contiguous tensors
@@ -496,6 +497,10 @@ class AdamW:
                     raise ValueError(f"{len(held)} tensors of state {name} for {n} parameters")
                 _expect_all(name, held, needed, dtype, self.device)
             setattr(self, name, held)
+        for name in self._held:
+            at = [x for x in map(torch.Tensor.data_ptr, getattr(self, name)) if x]
+            if len(set(at)) < len(at):  # two workgroups would update the same values
+                raise ValueError(f"{name} has the same tensor twice")
         self._n = n
         self._rows = (adst_adamw_tensor * n)()
         # the same memory as 8-byte words: p, grad, m, v, m_scale, v_scale, copy, n, lr, decay

@@ -187,3 +187,17 @@ def test_the_tensors_versions_rise(calls, bits):
     opt.step(grads)
     for n in names:
         assert all(t._version > v for t, v in zip(getattr(opt, n), before[n]))
+
+
+def test_a_tensor_twice_is_refused(calls):
+    """Its two updates would race."""
+    p, q = torch.zeros(600), torch.zeros(600)
+    state = {"m": [torch.zeros(600) for _ in range(2)], "v": [torch.zeros(600) for _ in range(2)]}
+    for make in (lambda: adst.AdamW([p, p]), lambda: adst.AdamW([p, p.view(600)]),
+                 lambda: adst.AdamW([p, q], copies=[p.half()] * 2),
+                 lambda: adst.AdamW([p, q], state=dict(state, m=state["m"][:1] * 2)),
+                 lambda: adst.AdamW([p, q], state=dict(state, v=state["v"][:1] * 2))):
+        with pytest.raises(ValueError, match="twice"):
+            make()
+    empty = torch.zeros(0)
+    adst.AdamW([p, q, empty, torch.zeros(0)])  # nothing to update twice

@@ -481,7 +481,8 @@ adst_status adst_copy(void* dst, const void* src, uint64_t bytes, hipStream_t st
 /* Gated linear recurrence, per batch row b and channel d, t = 1..steps:
  *   ADST_GATE_COEFF    h_t = a_t * h_{t-1} + u_t
  *   ADST_GATE_SIGMOID  h_t = s_t * h_{t-1} + (1 - s_t) * u_t,  s_t = 1 / (1 + exp(-a_t))
- * (1 - s_t is evaluated as 1 / (1 + exp(a_t)).) The time axis is cut into
+ * (1 - s_t is evaluated as 1 / (1 + exp(a_t)); a gate below the accumulation
+ * type's smallest normal value may be 0.) The time axis is cut into
  * spans whose maps h -> A*h + H are joined, so the products of up to `steps`
  * consecutive coefficients have to stay in the accumulation type's range,
  * which |a_t| <= 1 ensures. */

@@ -2,7 +2,7 @@
 // in between: a small call's time is the host's, and each attribute that
 // Python looks up is a good part of it (layer norm of 32 rows: 10.1 us through
 // Python, 6.7 from here, of which 3 are the launch; one step of AdamW over 121
-// tensors: 37 and 9). Each function returns None for anything that is not
+// tensors: 37 and 14). Each function returns None for anything that is not
 // ordinary (a wrong or unusual argument, tensors on another device than the
 // current one), before anything is launched; sequence.py then goes its own
 // way, which handles the unusual and raises the errors. A call that HIP fails

@@ -13,11 +13,14 @@
 // depends on the sizes alone. In large calls the VJP's next rows are on their
 // way to LDS while the ones before are worked on. Rows longer than the
 // registers hold are read again for each pass (norm_fwd_long, norm_rev_long),
-// from the caches mostly.
+// from the caches mostly; the VJP of rows longer than its kernel holds with the
+// sums reads x and dy again for them (norm_dw_long).
 //
-// Measured, bf16, forward and VJP with its sums: 32768 x 2048 48 and 71 us (5.6
+// Measured, forward and VJP with its sums: bf16 32768 x 2048 48 and 71 us (5.6
 // and 5.7 TB/s), 16384 x 4096 50 and 74, 8192 x 8192 47 and 76, 4096 x 16384 48
-// and 84.
+// and 84, 2000 x 30001 60 and 174; F32 16384 x 2048 47 and 71, 8192 x 8192 91 and
+// 145, 4096 x 16384 95 and 154, 1024 x 30000 68 and 144; F64 16384 x 2048 93 and
+// 142, 4096 x 8000 99 and 242.
 
 #include "seq_common.h"
 #include "seq_kernels.h"
@@ -693,7 +696,12 @@ int64_t vectors_of(int32_t dtype, int64_t n) {
   const int64_t v = dtype == ADST_F64 ? 2 : dtype == ADST_F32 ? 4 : 8;
   return (n + v - 1) / v;
 }
-// Vectors of a row that the VJP's registers hold with the sums of dw and db.
+// Vectors of a row that one kernel of the VJP takes with the sums of dw and db:
+// what its registers hold (a few of F16 and F64 are 2 to 8 of 128 short), and of
+// F32 twice as many. There the weights and both sums beside x and dy leave 13
+// (rows requested ahead) to 75 (PARTS) registers to scratch memory, which costs
+// less than a second kernel that reads x and dy again: 4096 x 16384 154 us, 297
+// with two; 2000 x 9001 67 and 114.
 int64_t held_in_vjp(int32_t dtype) { return dtype == ADST_F32 ? 4096 : 2048; }
 
 // Non-temporal accesses where a call moves more than the caches keep for the
@@ -728,6 +736,9 @@ hipError_t forward_by_length(const NormArgs& a, int64_t nv, hipStream_t st) {
   if (nv <= 1024) return forward<T, W, 256, 256, 4, 1>(a, st);
   if (nv <= 2048) return forward<T, W, 512, 512, 4, 1>(a, st);
   if (nv <= 4096) return forward<T, W, 1024, 1024, 4, 1>(a, st);
+  // eight vectors of a row and their weights are 24 registers more than there
+  // are: neither this nor reading the row again is the faster throughout (1024 x
+  // 30000 68 us and 75, 1000 x 30001 76 and 72, 2000 x 20000 96 and 88)
   if constexpr (sizeof(T) == 4)
     if (nv <= 8192) return forward<T, W, 1024, 1024, 8, 1>(a, st);
   return start(norm_fwd_long<T, W>, long_grid(a.rows), kLongThreads, st, a);
@@ -784,7 +795,8 @@ hipError_t reverse_by_length(const NormArgs& a, int64_t nv, int parts, Acc<T>* p
   if (nv <= 2048) return reverse<T, W, 512, 512, 4, 1>(a, g, part, st);
   if constexpr (sizeof(T) == 4)
     if (nv <= held_in_vjp(a.dtype)) return reverse<T, W, 1024, 1024, 4, 1>(a, g, part, st);
-  // dx without the sums' registers, as long as those hold the row
+  // dx without the sums' registers, as long as those hold the row (of F32's eight
+  // vectors but 64 of 128: 1024 x 30000 144 us, 149 with norm_rev_long)
   hipError_t e = hipSuccess;
   if (a.dx) {
     const unsigned rows = long_grid(a.rows);

@@ -227,7 +227,8 @@ def _check_lens(lens, a):
 def recurrence(a, u, h0=None, lens=None, gate=ADST_GATE_COEFF, want_h=True, want_ck=False,
                stream=None):
     """h_t = c_t * h_{t-1} + d_t over axis 1 of a, u [batch, steps, channels], with
-    (c, d) = (a, u), or (s, (1 - s) * u), s = sigmoid(a), for ADST_GATE_SIGMOID.
+    (c, d) = (a, u), or (s, (1 - s) * u), s = sigmoid(a), for ADST_GATE_SIGMOID. The products of
+    consecutive coefficients have to stay in range, which abs(a) <= 1 ensures.
 
     h0 [batch, channels] (zeros if None), in float32 (float64 for float64 inputs); lens
     [batch] int32: the steps of each row. a and u may have any strides with contiguous

@@ -638,6 +638,196 @@ typedef struct {
 adst_status adst_adamw(const adst_adamw_problem* prob, const adst_adamw_tensor* tensors,
                        int32_t n_tensors, hipStream_t stream);
 
+/* ---- Token operators ----------------------------------------------------
+ * What mixes a sequence layer's neighbouring tokens (a short causal
+ * convolution), a time loop with several states a channel whose coefficients
+ * are inputs (the selective scan), and the loss of a vocabulary. The
+ * conventions of the sequence operators above hold: element and accumulation
+ * types, alignment, streams, errors, results that are the same bit for bit
+ * from call to call. */
+
+/* Causal convolution, per batch row b and channel d, t = 0..steps-1:
+ *   y_t = act(bias + sum_{k=0..taps-1} w[k] * x_{t - (taps-1) + k}),
+ * act(v) = v or v / (1 + exp(-v)). The inputs before the first step are the
+ * window x0 [batch][taps-1][channels], oldest first (zeros if NULL). w
+ * [taps][channels] and bias [channels] (optional) are of weight_dtype: the
+ * dtype itself, or F32 beside BF16 and F16. */
+#define ADST_CONV_MAX_TAPS 8
+typedef enum { ADST_ACT_NONE = 0, ADST_ACT_SILU = 1 } adst_act;
+
+typedef struct {
+  int32_t dtype;         /* of x, x0, xT, y, dy, dx, dx0, dxT and the windows' pool */
+  int32_t weight_dtype;  /* of w, bias, dw, dbias */
+  int32_t act;           /* adst_act */
+  int32_t taps;          /* 1..ADST_CONV_MAX_TAPS */
+  int64_t batch, steps, channels; /* >= 0 */
+  int64_t stride_x[2];   /* elements between batch rows and between steps of x, */
+  int64_t stride_dy[2];  /* and of dy. Channels are contiguous; any strides >= 0, 0 repeats */
+} adst_conv_problem;
+
+/* y [batch][steps][channels] (contiguous, optional) and the last window xT
+ * [batch][taps-1][channels] (optional): the taps-1 inputs before step lens[b],
+ * those of x0 among them where the row is shorter. lens: as in
+ * adst_recurrence_forward; y beyond is 0. Errors: ADST_ERR_ARG (NULL problem, x or
+ * w, bad types, extents or strides, overlapping ranges), ADST_ERR_UNSUPPORTED
+ * (an extent >= 2^31 - 2^16), ADST_ERR_HIP. */
+adst_status adst_causal_conv_forward(const adst_conv_problem* prob, const void* x, const void* w,
+                                     const void* bias, const void* x0, const int32_t* lens,
+                                     void* y, void* xT, hipStream_t stream);
+
+/* The vector-Jacobian product: dy = dL/dy, dxT = dL/dxT (optional). dx
+ * [batch][steps][channels] (contiguous; zero beyond lens[b], where dy is not read), dw, dbias
+ * and dx0 are each optional. An input that repeats (stride 0) gets the
+ * gradients of its uses, one for each. ws: adst_causal_conv_workspace_bytes
+ * (read only where dw or dbias is asked for). Errors: as the forward, plus
+ * ADST_ERR_WORKSPACE. */
+uint64_t adst_causal_conv_workspace_bytes(const adst_conv_problem* prob);
+adst_status adst_causal_conv_vjp(const adst_conv_problem* prob, const void* x, const void* dy,
+                                 const void* w, const void* bias, const void* x0,
+                                 const int32_t* lens, const void* dxT, void* dx, void* dw,
+                                 void* dbias, void* dx0, void* ws, uint64_t ws_bytes,
+                                 hipStream_t stream);
+
+/* One step of each batch row (prob->steps must be 1) on a pool of windows
+ * [nstates][taps-1][channels], updated in place; y [batch][channels] (optional).
+ * slots and idle rows: as in adst_recurrence_step. Errors: as the forward. */
+adst_status adst_causal_conv_step(const adst_conv_problem* prob, const void* x, const void* w,
+                                  const void* bias, const int32_t* slots, void* window,
+                                  int64_t nstates, void* y, hipStream_t stream);
+
+/* Selective scan, per batch row b and channel d with its states n = 0..states-1,
+ * t = 1..steps:
+ *   s_t    = softplus(delta_t + delta_bias), or delta_t + delta_bias
+ *   h_t[n] = exp(s_t * A[n]) * h_{t-1}[n] + s_t * x_t * B_t[n]
+ *   y_t    = (sum_n C_t[n] * h_t[n] + D * x_t) * z_t / (1 + exp(-z_t))
+ * softplus(v) = log(1 + exp(v)). A [channels][states], and D and delta_bias
+ * [channels] (optional: 0), are in the accumulation type; z (optional: no
+ * factor). B and C are [batch][steps][groups][states], (groups, states)
+ * contiguous: channel d reads group d / (channels / groups). The time axis is
+ * cut into spans whose maps are joined, so the products of up to `steps`
+ * consecutive coefficients exp(s * A) have to stay in the accumulation type's
+ * range, which s * A <= 0 ensures. */
+#define ADST_SCAN_MAX_STATES 128 /* 64 for F64 */
+typedef struct {
+  int32_t dtype;     /* of x, delta, B, C, z, y, dy and their gradients */
+  int32_t softplus;  /* 0 or 1 */
+  int64_t batch, steps, channels; /* >= 0 */
+  int64_t states;    /* 1..ADST_SCAN_MAX_STATES */
+  int64_t groups;    /* >= 1, divides channels */
+  int64_t stride_x[2], stride_delta[2], stride_b[2], stride_c[2], stride_z[2], stride_dy[2];
+                     /* elements between batch rows and between steps; >= 0, 0 repeats */
+} adst_scan_problem;
+
+typedef struct {
+  const void* x;
+  const void* delta;
+  const void* A;
+  const void* B;
+  const void* C;
+  const void* D;           /* optional */
+  const void* z;           /* optional */
+  const void* delta_bias;  /* optional */
+  const void* h0;          /* optional [batch][channels][states], accumulation type */
+  const int32_t* lens;     /* optional, as in adst_recurrence_forward */
+} adst_scan_inputs;
+
+typedef struct {
+  void* dx;          /* [batch][steps][channels], zero beyond lens[b] */
+  void* ddelta;      /* the same */
+  void* dz;          /* the same; NULL where z is */
+  void* dB;          /* [batch][steps][groups][states], zero beyond lens[b] */
+  void* dC;          /* the same */
+  void* dA;          /* [channels][states], accumulation type (this and the ones below) */
+  void* dD;          /* [channels]; optional */
+  void* ddelta_bias; /* [channels]; optional */
+  void* dh0;         /* [batch][channels][states]; optional */
+} adst_scan_gradients;
+
+typedef struct {
+  int64_t span;                 /* steps between checkpoints */
+  uint64_t ck_bytes;            /* checkpoints: the states at the start of each span */
+  uint64_t workspace_bytes;     /* ws of adst_selective_scan_forward */
+  uint64_t vjp_workspace_bytes; /* ws of adst_selective_scan_vjp given checkpoints; ck_bytes
+                                   more without (ck = NULL) */
+} adst_scan_info;
+
+/* Sizes of a problem's buffers (host only). They depend on the sizes alone, as
+ * the order of all sums does. Errors: ADST_ERR_ARG (NULL, unknown dtype, a bad extent or
+ * stride), ADST_ERR_UNSUPPORTED (an extent >= 2^31 - 2^16, more states than
+ * above, or more channels and rows than a launch holds). */
+adst_status adst_selective_scan_plan(const adst_scan_problem* prob, adst_scan_info* out);
+
+/* y [batch][steps][channels] (contiguous, optional; 0 beyond lens[b]), the last states hT
+ * [batch][channels][states] (optional, accumulation type; h0 of a row without
+ * steps) and the checkpoints ck (optional) for adst_selective_scan_vjp.
+ * Errors: as adst_selective_scan_plan; ADST_ERR_ARG for a missing input or
+ * overlapping ranges, ADST_ERR_WORKSPACE, ADST_ERR_HIP. */
+adst_status adst_selective_scan_forward(const adst_scan_problem* prob, const adst_scan_inputs* in,
+                                        void* y, void* hT, void* ck, void* ws, uint64_t ws_bytes,
+                                        hipStream_t stream);
+
+/* The vector-Jacobian product: dy = dL/dy, dhT = dL/dhT (optional, accumulation
+ * type). ck: the checkpoints of adst_selective_scan_forward for the same
+ * problem and inputs, or NULL: they are then recomputed. A repeating input
+ * gets the gradients of its uses, one for each. Errors: as the forward. */
+adst_status adst_selective_scan_vjp(const adst_scan_problem* prob, const adst_scan_inputs* in,
+                                    const void* ck, const void* dy, const void* dhT,
+                                    const adst_scan_gradients* out, void* ws, uint64_t ws_bytes,
+                                    hipStream_t stream);
+
+/* One step of each batch row (prob->steps must be 1; h0 and lens NULL) on a
+ * pool of states [nstates][channels][states] in the accumulation type, updated
+ * in place; y [batch][channels] (optional). slots and idle rows: as in
+ * adst_recurrence_step. Errors: as the forward, without ADST_ERR_WORKSPACE. */
+adst_status adst_selective_scan_step(const adst_scan_problem* prob, const adst_scan_inputs* in,
+                                     const int32_t* slots, void* state, int64_t nstates, void* y,
+                                     hipStream_t stream);
+
+/* Softmax cross entropy of rows x [rows][width] over a vocabulary w
+ * [vocab][width], labels [rows]:
+ *   logit_v = sum_i x_i * w[v]_i,  lse = log sum_v exp(logit_v),
+ *   loss = lse - logit_label
+ * A row whose label is outside [0, vocab) has loss 0 and no gradient. The logits
+ * are held for a piece of the vocabulary at a time, on chip in the forward. */
+typedef struct {
+  int32_t dtype;      /* of x, w, dx, dw */
+  int32_t reserved;   /* 0 */
+  int64_t rows;       /* >= 0 */
+  int64_t width;      /* >= 1 */
+  int64_t vocab;      /* >= 1 */
+  int64_t stride_x;   /* elements between rows of x (>= 0) */
+  int64_t stride_w;   /* and of w; dx and dw are contiguous */
+} adst_xent_problem;
+
+typedef struct {
+  uint64_t workspace_bytes;     /* ws of adst_linear_cross_entropy_forward */
+  uint64_t vjp_workspace_bytes; /* and of _vjp */
+} adst_xent_info;
+
+/* Host only. Errors: ADST_ERR_ARG (NULL, unknown dtype, a bad extent or
+ * stride), ADST_ERR_UNSUPPORTED (an extent >= 2^31 - 2^16). */
+adst_status adst_linear_cross_entropy_plan(const adst_xent_problem* prob, adst_xent_info* out);
+
+/* loss and lse [rows] in the accumulation type (each optional). Errors: as the
+ * plan; ADST_ERR_ARG for a missing input or overlapping ranges,
+ * ADST_ERR_WORKSPACE, ADST_ERR_HIP. */
+adst_status adst_linear_cross_entropy_forward(const adst_xent_problem* prob, const void* x,
+                                              const void* w, const int32_t* labels, void* loss,
+                                              void* lse, void* ws, uint64_t ws_bytes,
+                                              hipStream_t stream);
+
+/* The vector-Jacobian product, with g_v = (exp(logit_v - lse) - [v = label]) * dloss of
+ * a row: dx = sum_v g_v * w[v], dw[v] = sum over rows of g_v * x (each
+ * optional). lse: the forward call's. dloss: dL/dloss [rows] in the accumulation
+ * type (1 if NULL). The logits are computed again; g is held in 16 bits beside 16-bit
+ * inputs, scaled by a power of two so that the largest dloss is at the top of
+ * the type's range. A row whose dloss is 0, or that has no label, gets a dx of
+ * 0. Errors: as the forward. */
+adst_status adst_linear_cross_entropy_vjp(const adst_xent_problem* prob, const void* x,
+                                          const void* w, const int32_t* labels, const void* lse,
+                                          const void* dloss, void* dx, void* dw, void* ws,
+                                          uint64_t ws_bytes, hipStream_t stream);
+
 /* Static description of a status code. */
 const char* adst_status_str(adst_status status);
 

@@ -22,6 +22,8 @@ ADST_JACOBI2D5, ADST_ALLENCAHN3D7, ADST_VARDIFF2D9, ADST_GAUSSSEIDEL2D5 = 0, 1, 
 ADST_F64, ADST_F32, ADST_BF16, ADST_F16 = 0, 1, 2, 3
 ADST_GATE_COEFF, ADST_GATE_SIGMOID = 0, 1
 ADST_STATE_BLOCK = 256
+ADST_ACT_NONE, ADST_ACT_SILU = 0, 1
+ADST_CONV_MAX_TAPS, ADST_SCAN_MAX_STATES = 8, 128
 ADST_SCHED_AUTO, ADST_SCHED_STORE_ALL, ADST_SCHED_UNIFORM, ADST_SCHED_BINOMIAL = 0, 1, 2, 3
 ADST_LOSS_HALF_SQ, ADST_LOSS_DOT_W, ADST_LOSS_HALF_SQ_DIFF, ADST_LOSS_SEED = 0, 1, 2, 3
 ADST_FORCE_TAPE, ADST_TRACE, ADST_NO_FUSE, ADST_LIMIT = 0x1, 0x2, 0x4, 0x8
@@ -34,7 +36,12 @@ EXPORTED = ("adst_plan", "adst_plan_actions", "adst_forward", "adst_vjp", "adst_
             "adst_last_error", "adst_sweep_workspace_bytes", "adst_forward_scratch",
             "adst_vjp_scratch", "adst_recurrence_plan", "adst_recurrence_forward",
             "adst_recurrence_vjp", "adst_recurrence_step", "adst_layer_norm_forward",
-            "adst_layer_norm_vjp", "adst_layer_norm_workspace_bytes", "adst_adamw")
+            "adst_layer_norm_vjp", "adst_layer_norm_workspace_bytes", "adst_adamw",
+            "adst_causal_conv_forward", "adst_causal_conv_workspace_bytes",
+            "adst_causal_conv_vjp", "adst_causal_conv_step", "adst_selective_scan_plan",
+            "adst_selective_scan_forward", "adst_selective_scan_vjp", "adst_selective_scan_step",
+            "adst_linear_cross_entropy_plan", "adst_linear_cross_entropy_forward",
+            "adst_linear_cross_entropy_vjp")
 ADST_STATIC_WS_BYTES = 64 << 20
 PHASE_NAMES = ("forward sweep", "recomputation", "adjoint", "loss and seed", "constants")
 ILP_EVENTS = {"alloc": 0, "free": 1, "produce": 2, "drop": 3, "recompute": 4,
@@ -125,6 +132,48 @@ class adst_adamw_problem(ctypes.Structure):
                 ("grad_scale", ctypes.c_void_p)]
 
 
+class adst_conv_problem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("taps", ctypes.c_int32), ("batch", ctypes.c_int64),
+                ("steps", ctypes.c_int64), ("channels", ctypes.c_int64),
+                ("stride_x_batch", ctypes.c_int64), ("stride_x_step", ctypes.c_int64),
+                ("stride_dy_batch", ctypes.c_int64), ("stride_dy_step", ctypes.c_int64)]
+
+
+class adst_scan_problem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("softplus", ctypes.c_int32),
+                ("batch", ctypes.c_int64), ("steps", ctypes.c_int64),
+                ("channels", ctypes.c_int64), ("states", ctypes.c_int64),
+                ("groups", ctypes.c_int64)] + \
+        [(f"stride_{k}_{axis}", ctypes.c_int64) for k in ("x", "delta", "b", "c", "z", "dy")
+         for axis in ("batch", "step")]
+
+
+class adst_scan_inputs(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("x", "delta", "A", "B", "C", "D", "z",
+                                               "delta_bias", "h0", "lens")]
+
+
+class adst_scan_gradients(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("dx", "ddelta", "dz", "dB", "dC", "dA", "dD",
+                                               "ddelta_bias", "dh0")]
+
+
+class adst_scan_info(ctypes.Structure):
+    _fields_ = [("span", ctypes.c_int64), ("ck_bytes", ctypes.c_uint64),
+                ("workspace_bytes", ctypes.c_uint64), ("vjp_workspace_bytes", ctypes.c_uint64)]
+
+
+class adst_xent_problem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("stride_x", ctypes.c_int64), ("stride_w", ctypes.c_int64)]
+
+
+class adst_xent_info(ctypes.Structure):
+    _fields_ = [("workspace_bytes", ctypes.c_uint64), ("vjp_workspace_bytes", ctypes.c_uint64)]
+
+
 class AdstError(RuntimeError):
     def __init__(self, status, detail):
         self.status = status
@@ -179,6 +228,26 @@ def lib():
               "adst_adamw"):
         getattr(L, f).restype = ctypes.c_int
     L.adst_layer_norm_workspace_bytes.restype = u64
+    conv, scan, xent = P(adst_conv_problem), P(adst_scan_problem), P(adst_xent_problem)
+    L.adst_causal_conv_forward.argtypes = [conv] + [vp] * 8
+    L.adst_causal_conv_workspace_bytes.argtypes = [conv]
+    L.adst_causal_conv_workspace_bytes.restype = u64
+    L.adst_causal_conv_vjp.argtypes = [conv] + [vp] * 12 + [u64, vp]
+    L.adst_causal_conv_step.argtypes = [conv] + [vp] * 5 + [i64, vp, vp]
+    L.adst_selective_scan_plan.argtypes = [scan, P(adst_scan_info)]
+    L.adst_selective_scan_forward.argtypes = [scan, P(adst_scan_inputs)] + [vp] * 4 + [u64, vp]
+    L.adst_selective_scan_vjp.argtypes = [scan, P(adst_scan_inputs)] + [vp] * 3 + \
+        [P(adst_scan_gradients), vp, u64, vp]
+    L.adst_selective_scan_step.argtypes = [scan, P(adst_scan_inputs), vp, vp, i64, vp, vp]
+    L.adst_linear_cross_entropy_plan.argtypes = [xent, P(adst_xent_info)]
+    L.adst_linear_cross_entropy_forward.argtypes = [xent] + [vp] * 6 + [u64, vp]
+    L.adst_linear_cross_entropy_vjp.argtypes = [xent] + [vp] * 8 + [u64, vp]
+    for f in ("adst_causal_conv_forward", "adst_causal_conv_vjp", "adst_causal_conv_step",
+              "adst_selective_scan_plan", "adst_selective_scan_forward",
+              "adst_selective_scan_vjp", "adst_selective_scan_step",
+              "adst_linear_cross_entropy_plan", "adst_linear_cross_entropy_forward",
+              "adst_linear_cross_entropy_vjp"):
+        getattr(L, f).restype = ctypes.c_int
     L.adst_status_str.argtypes = [ctypes.c_int]
     L.adst_status_str.restype = ctypes.c_char_p
     L.adst_last_error.argtypes = []
@@ -482,3 +551,11 @@ from .sequence import (AdamW, adst_adamw, adst_layer_norm_forward,  # noqa: E402
                        adst_recurrence_forward, adst_recurrence_plan, adst_recurrence_step,
                        adst_recurrence_vjp, layer_norm, layer_norm_vjp, recurrence,
                        recurrence_step, recurrence_vjp)
+from .tokens import (adst_causal_conv_forward, adst_causal_conv_step,  # noqa: E402,F401
+                     adst_causal_conv_vjp, adst_causal_conv_workspace_bytes,
+                     adst_linear_cross_entropy_forward, adst_linear_cross_entropy_plan,
+                     adst_linear_cross_entropy_vjp, adst_selective_scan_forward,
+                     adst_selective_scan_plan, adst_selective_scan_step, adst_selective_scan_vjp,
+                     causal_conv, causal_conv_step, causal_conv_vjp, linear_cross_entropy,
+                     linear_cross_entropy_vjp, selective_scan, selective_scan_step,
+                     selective_scan_vjp)

@@ -21,11 +21,15 @@ BINDING = os.path.join(HERE, "_binding.so")
 ARCH = "gfx950"
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
-HOST_SOURCES = ["planner.cpp", "ilp.cpp", "abi.cpp", "seq_abi.cpp"]
+HOST_SOURCES = ["planner.cpp", "ilp.cpp", "abi.cpp", "seq_abi.cpp", "token_abi.cpp",
+                "selective_scan.cpp", "linear_cross_entropy.cpp"]
 HIP_SOURCES = ["kernels.hip", "allencahn.hip", "jacobi_march.hip", "jacobi_march_lim.hip",
                "jacobi_march_store.hip", "jacobi_pair.hip", "gauss_seidel.hip", "gs_pipe.hip",
                "vardiff_march.hip", "static_ws.hip", "recurrence.hip", "layer_norm.hip",
-               "adamw.hip"]
+               "adamw.hip", "causal_conv.hip", "selective_scan_f64.hip", "selective_scan_f32.hip",
+               "selective_scan_bf16.hip", "selective_scan_f16.hip", "linear_cross_entropy_f64.hip",
+               "linear_cross_entropy_f32.hip", "linear_cross_entropy_bf16.hip",
+               "linear_cross_entropy_f16.hip"]
 
 COMMON = ["-std=c++17", "-O3", "-fPIC", "-ffp-contract=off", "-Wall",
           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

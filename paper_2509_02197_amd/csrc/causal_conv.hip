@@ -1,0 +1,460 @@
+// Causal convolution of a few taps per channel, y_t = act(bias + sum_k w_k
+// x_{t-K+1+k}); its VJP; and one step on a pool of windows.
+//
+// A thread takes V neighbouring channels of a segment of steps and keeps the
+// last K-1 inputs in registers, so an input is loaded once but for the K-1
+// before each segment. HBM bandwidth bounds it: one value read and one written.
+// The VJP computes the sum before the activation again, as its derivative needs
+// it: with g_t = dy_t act'(pre_t),
+//   dx_t = sum_k w_k g_{t+K-1-k},  dw_k = sum_t g_t x_{t-K+1+k},  db = sum_t g_t,
+// so x and dy are read, dx is written, and dw and db are summed in registers over
+// a thread's segments, over a workgroup through LDS, and over workgroups by a
+// second kernel in an order that the sizes alone set.
+
+#include "packs.h"
+#include "seq_common.h"
+#include "seq_launch.h"
+#include "token_kernels.h"
+
+namespace adst {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBatch = 4;      // steps whose loads are in flight together
+constexpr int kSegment = 32;   // steps of a thread, where there are enough threads
+constexpr int kFewSegment = 8;
+constexpr int64_t kManyThreads = 1 << 17;  // 8 waves a CU
+
+// Channels of a thread: 16 bytes, and half of that where the taps' weights and
+// sums would not leave registers for two waves a SIMD.
+template <class T, int K>
+constexpr int lanes_of(bool reverse) {
+  return sizeof(T) == 2 ? (K > 4 || reverse ? 4 : 8) : sizeof(T) == 4 ? (reverse && K > 4 ? 2 : 4) : 2;
+}
+
+// A weight: of T, or of float beside 16-bit T.
+template <class T>
+__device__ inline Acc<T> weight(const void* w, bool same, int64_t i) {
+  if (same) return up(static_cast<const T*>(w)[i]);
+  return (Acc<T>)static_cast<const float*>(w)[i];
+}
+
+template <class T, int K, int V>
+struct Taps {
+  Acc<T> w[K][V], b[V];
+  __device__ void load(const ConvArgs& a, int64_t d0, int n) {
+    const bool same = a.wtype == a.dtype;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      b[i] = a.bias && i < n ? weight<T>(a.bias, same, d0 + i) : Acc<T>(0);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        w[k][i] = i < n ? weight<T>(a.w, same, k * a.D + d0 + i) : Acc<T>(0);
+    }
+  }
+};
+
+// Input t of a row, those of the window before it where t < 0 (t >= 1 - K).
+template <class T, int V>
+__device__ inline Pack<T, V> input(const ConvArgs& a, int64_t b, int64_t t, int64_t d0, int n) {
+  if (t >= 0)
+    return load_pack<T, V>(static_cast<const T*>(a.x) + b * a.sx_b + t * a.sx_t + d0, n);
+  if (a.x0)
+    return load_pack<T, V>(
+        static_cast<const T*>(a.x0) + (b * (a.taps - 1) + t + a.taps - 1) * a.D + d0, n);
+  return load_pack<T, V>(static_cast<const T*>(nullptr), 0);
+}
+
+// ------------------------------------------------------------------- forward
+// A thread: V channels of one segment of a row; the last segment's index copies
+// the window that follows the row.
+template <class T, int K, int V>
+__global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, int64_t segments,
+                                                     int segment) {
+  typedef Acc<T> A;
+  constexpr int H = K > 1 ? K - 1 : 1;
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t c = id % nvec, rest = id / nvec;
+  const int64_t b = rest / (segments + 1), s = rest % (segments + 1);
+  if (b >= a.B) return;
+  const int64_t d0 = c * V;
+  const int n = (int)(a.D - d0 < V ? a.D - d0 : V);
+  const int64_t len = row_length(a.lens, b, a.T);
+  if (s == segments) {
+    if (a.xT)
+      for (int j = 0; j < K - 1; ++j)
+        store_pack<T, V>(static_cast<T*>(a.xT) + (b * (K - 1) + j) * a.D + d0,
+                         input<T, V>(a, b, len + j - (K - 1), d0, n), n);
+    return;
+  }
+  if (!a.y) return;
+  const int64_t first = s * segment, all = a.T - first < segment ? a.T - first : segment;
+  const int64_t end = first + all, live = len < end ? len : end;
+  T* y = static_cast<T*>(a.y) + (b * a.T + first) * a.D + d0;
+  if (first < live) {
+    Taps<T, K, V> taps;
+    taps.load(a, d0, n);
+    Pack<T, V> seen[H];  // inputs t-K+1 .. t-1
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) seen[k] = input<T, V>(a, b, first - (K - 1) + k, d0, n);
+    const T* x = static_cast<const T*>(a.x) + b * a.sx_b + first * a.sx_t + d0;
+    for (int64_t t = first; t < live; t += kBatch) {
+      Pack<T, V> in[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r)
+        in[r] = load_pack<T, V>(x + r * a.sx_t, t + r < live ? n : 0);
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        Pack<T, V> out;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          A v = taps.b[i];
+#pragma unroll
+          for (int k = 0; k < K - 1; ++k) v = fma_(taps.w[k][i], up((T)seen[k].v[i]), v);
+          v = fma_(taps.w[K - 1][i], up((T)in[r].v[i]), v);
+          if (a.act == ADST_ACT_SILU) {
+            A g, q;
+            gates<T>(v, &g, &q);
+            v *= g;
+          }
+          out.v[i] = down<T>(v);
+        }
+        if (t + r < live) store_pack<T, V>(y + r * a.D, out, n);
+#pragma unroll
+        for (int k = 0; k + 1 < K - 1; ++k) seen[k] = seen[k + 1];
+        if (K > 1) seen[H - 1] = in[r];
+      }
+      x += kBatch * a.sx_t;
+      y += kBatch * a.D;
+    }
+  }
+  y = static_cast<T*>(a.y) + b * a.T * a.D + d0;
+  Pack<T, V> zero;
+#pragma unroll
+  for (int i = 0; i < V; ++i) zero.v[i] = T(0);
+  for (int64_t t = live > first ? live : first; t < end; ++t) store_pack<T, V>(y + t * a.D, zero, n);
+}
+
+// ------------------------------------------------------------------- reverse
+// How the VJP is laid out: `columns` lanes along channels, the workgroup's other
+// threads and `workers` workgroups along segments.
+struct Layout {
+  int columns;
+  int64_t slabs, workers, segments;
+};
+template <class T, int K>
+Layout layout_of(int64_t B, int64_t T_, int64_t D) {
+  constexpr int V = lanes_of<T, K>(true);
+  const int64_t nvec = (D + V - 1) / V;
+  Layout l;
+  l.columns = 1;
+  while (l.columns < nvec && l.columns < 64) l.columns *= 2;
+  l.slabs = (nvec + l.columns - 1) / l.columns;
+  l.segments = T_ > 0 ? (T_ + kSegment - 1) / kSegment : 1;
+  const int64_t rows = kThreads / l.columns, all = (B * l.segments + rows - 1) / rows;
+  const int64_t most = (1024 + l.slabs - 1) / l.slabs;
+  l.workers = all < most ? all : most;
+  if (l.workers < 1) l.workers = 1;
+  return l;
+}
+
+template <class T, int K, int V>
+__global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void* sums) {
+  typedef Acc<T> A;
+  constexpr int H = K > 1 ? K - 1 : 1;
+  __shared__ A part[kThreads][V];
+  const int rows = kThreads / l.columns;
+  const int column = threadIdx.x % l.columns, row = threadIdx.x / l.columns;
+  const int64_t slab = blockIdx.x % l.slabs, worker = blockIdx.x / l.slabs;
+  const int64_t d0 = (slab * l.columns + column) * V;
+  const int n = (int)(a.D - d0 < V ? (a.D - d0 > 0 ? a.D - d0 : 0) : V);
+  const T* const x = static_cast<const T*>(a.x);
+  const T* const dy = static_cast<const T*>(a.dy);
+  Taps<T, K, V> taps;
+  if (n > 0) taps.load(a, d0, n);
+  A dw[K][V], db[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    db[i] = A(0);
+#pragma unroll
+    for (int k = 0; k < K; ++k) dw[k][i] = A(0);
+  }
+  const int64_t all = n > 0 ? a.B * l.segments : 0;
+  for (int64_t item = worker * rows + row; item < all; item += l.workers * rows) {
+    const int64_t b = item / l.segments, first = item % l.segments * kSegment;
+    const int64_t end = a.T - first < kSegment ? a.T : first + kSegment;
+    const int64_t len = row_length(a.lens, b, a.T);
+    // the first value whose gradient is this segment's: the window's before the row's start
+    const int64_t low = first > 0 ? first : -(K - 1);
+    const int64_t most = end + K - 1 < len ? end + K - 1 : len;  // steps that are needed
+    Pack<T, V> seen[H];
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) {
+      const bool have = first - (K - 1) + k < len;
+      seen[k] = input<T, V>(a, b, first - (K - 1) + k, d0, have ? n : 0);
+    }
+    A acc[K][V];  // of the gradients of inputs t-K+1 .. t
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[k][i] = A(0);
+    const int64_t stop = end + K - 1;  // every gradient has left by then
+    for (int64_t t0 = first; t0 < stop; t0 += kBatch) {
+      Pack<T, V> in[kBatch], d[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        const int64_t t = t0 + r;
+        const int m = t < most ? n : 0;
+        in[r] = load_pack<T, V>(x + b * a.sx_b + t * a.sx_t + d0, m);
+        d[r] = load_pack<T, V>(dy + b * a.sd_b + t * a.sd_t + d0, m);
+      }
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        const int64_t t = t0 + r;
+        if (t < most) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            A g = up((T)d[r].v[i]);
+            if (a.act == ADST_ACT_SILU) {
+              A v = taps.b[i], s, q;
+#pragma unroll
+              for (int k = 0; k < K - 1; ++k) v = fma_(taps.w[k][i], up((T)seen[k].v[i]), v);
+              v = fma_(taps.w[K - 1][i], up((T)in[r].v[i]), v);
+              gates<T>(v, &s, &q);
+              g *= s * fma_(v, q, A(1));
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k) acc[k][i] = fma_(taps.w[k][i], g, acc[k][i]);
+            if (t < end) {
+              db[i] += g;
+#pragma unroll
+              for (int k = 0; k < K - 1; ++k) dw[k][i] = fma_(g, up((T)seen[k].v[i]), dw[k][i]);
+              dw[K - 1][i] = fma_(g, up((T)in[r].v[i]), dw[K - 1][i]);
+            }
+          }
+        }
+        const int64_t at = t - (K - 1);  // the input whose gradient is whole now
+        if (at >= low && at < end) {
+          Pack<T, V> out;
+          const bool held = a.dxT && at >= len - (K - 1) && at < len;
+          Pack<T, V> of;
+          if (held)
+            of = load_pack<T, V>(static_cast<const T*>(a.dxT) +
+                                     (b * (K - 1) + at + (K - 1) - len) * a.D + d0, n);
+#pragma unroll
+          for (int i = 0; i < V; ++i)
+            out.v[i] = down<T>(held ? acc[0][i] + up((T)of.v[i]) : acc[0][i]);
+          if (at >= 0) {
+            if (a.dx) store_pack<T, V>(static_cast<T*>(a.dx) + (b * a.T + at) * a.D + d0, out, n);
+          } else if (a.dx0) {
+            store_pack<T, V>(static_cast<T*>(a.dx0) + (b * (K - 1) + at + (K - 1)) * a.D + d0, out,
+                             n);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k + 1 < K; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) acc[k][i] = acc[k + 1][i];
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[K - 1][i] = A(0);
+#pragma unroll
+        for (int k = 0; k + 1 < K - 1; ++k) seen[k] = seen[k + 1];
+        if (K > 1) seen[H - 1] = in[r];
+      }
+    }
+  }
+  if (!sums) return;
+  // [worker][K + 1][D]: over the workgroup's rows in turn
+  A* const out = static_cast<A*>(sums) + worker * (K + 1) * a.D;
+#pragma unroll
+  for (int k = 0; k <= K; ++k) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) part[threadIdx.x][i] = k < K ? dw[k < K ? k : 0][i] : db[i];
+    __syncthreads();
+    if (row == 0)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        A v = A(0);
+        for (int r = 0; r < rows; ++r) v += part[r * l.columns + column][i];
+        if (i < n) out[k * a.D + d0 + i] = v;
+      }
+  }
+}
+
+// dw and dbias from the workers' sums: 64 columns, four rows of threads that
+// take every fourth worker.
+template <class T>
+__global__ __launch_bounds__(kThreads) void conv_sum(const Acc<T>* sums, int64_t workers, int64_t D,
+                                                     int taps, void* dw, void* dbias, bool same) {
+  typedef Acc<T> A;
+  __shared__ A part[4][64];
+  const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x % 64, all = (taps + 1) * D;
+  const int row = threadIdx.x / 64;
+  A v = A(0);
+  if (i < all) {
+#pragma unroll 8
+    for (int64_t k = row; k < workers; k += 4) v += sums[k * all + i];
+  }
+  part[row][threadIdx.x % 64] = v;
+  __syncthreads();
+  if (row > 0 || i >= all) return;
+  v = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+  void* const to = i < taps * D ? dw : dbias;
+  const int64_t at = i < taps * D ? i : i - taps * D;
+  if (!to) return;
+  if (same) static_cast<T*>(to)[at] = down<T>(v);
+  else static_cast<float*>(to)[at] = (float)v;
+}
+
+// ------------------------------------------------------------------ one step
+template <class T, int V>
+__global__ __launch_bounds__(kThreads) void conv_one(ConvStep a, int64_t nvec) {
+  typedef Acc<T> A;
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t b = id / nvec, d0 = id % nvec * V;
+  if (b >= a.B) return;
+  const int n = (int)(a.D - d0 < V ? a.D - d0 : V), K = a.taps;
+  const bool same = a.wtype == a.dtype;
+  const int64_t slot = a.slots ? a.slots[b] : b;
+  Pack<T, V> out;
+  if (slot < 0 || slot >= a.nstates) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) out.v[i] = T(0);
+    if (a.y) store_pack<T, V>(static_cast<T*>(a.y) + b * a.D + d0, out, n);
+    return;
+  }
+  T* const window = static_cast<T*>(a.window) + slot * (K - 1) * a.D + d0;
+  Pack<T, V> seen[ADST_CONV_MAX_TAPS];
+#pragma unroll
+  for (int k = 0; k < ADST_CONV_MAX_TAPS - 1; ++k)
+    if (k < K - 1) seen[k] = load_pack<T, V>(window + k * a.D, n);
+  const Pack<T, V> in = load_pack<T, V>(static_cast<const T*>(a.x) + b * a.sx + d0, n);
+  A v[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = a.bias && i < n ? weight<T>(a.bias, same, d0 + i) : A(0);
+#pragma unroll
+  for (int k = 0; k < ADST_CONV_MAX_TAPS - 1; ++k)
+    if (k < K - 1) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < n) v[i] = fma_(weight<T>(a.w, same, k * a.D + d0 + i), up((T)seen[k].v[i]), v[i]);
+      if (k > 0) store_pack<T, V>(window + (k - 1) * a.D, seen[k], n);
+    }
+  if (K > 1) store_pack<T, V>(window + (K - 2) * a.D, in, n);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (i < n) v[i] = fma_(weight<T>(a.w, same, (K - 1) * a.D + d0 + i), up((T)in.v[i]), v[i]);
+    if (a.act == ADST_ACT_SILU) {
+      A g, q;
+      gates<T>(v[i], &g, &q);
+      v[i] *= g;
+    }
+    out.v[i] = down<T>(v[i]);
+  }
+  if (a.y) store_pack<T, V>(static_cast<T*>(a.y) + b * a.D + d0, out, n);
+}
+
+// ------------------------------------------------------------------ launches
+template <class F>
+hipError_t by_type(int32_t dtype, F f) {
+  switch (dtype) {
+    case ADST_F64: return f(double());
+    case ADST_F32: return f(float());
+    case ADST_BF16: return f(bf16());
+    default: return f(f16());
+  }
+}
+template <int K>
+struct Count {
+  static constexpr int value = K;
+};
+template <class F>
+hipError_t by_taps(int taps, F f) {
+  switch (taps) {
+    case 1: return f(Count<1>());
+    case 2: return f(Count<2>());
+    case 3: return f(Count<3>());
+    case 4: return f(Count<4>());
+    case 5: return f(Count<5>());
+    case 6: return f(Count<6>());
+    case 7: return f(Count<7>());
+    default: return f(Count<8>());
+  }
+}
+
+// Workgroups of one launch at most: its work-items are counted in 32 bits.
+constexpr int64_t kMostGroups = (int64_t(1) << 32) / kThreads - 1;
+
+}  // namespace
+
+hipError_t conv_forward(const ConvArgs& q, hipStream_t st) {
+  return by_type(q.dtype, [&](auto t) {
+    return by_taps(q.taps, [&](auto k) {
+      typedef decltype(t) T;
+      constexpr int K = decltype(k)::value, V = lanes_of<T, K>(false);
+      const int64_t nvec = (q.D + V - 1) / V;
+      const int segment =
+          nvec * q.B * ((q.T + kSegment - 1) / kSegment) >= kManyThreads ? kSegment : kFewSegment;
+      const int64_t segments = q.y ? (q.T + segment - 1) / segment : 0;
+      // rows of the batch in several launches where one does not hold them
+      const int64_t row = nvec * (segments + 1), rows = kMostGroups * kThreads / row;
+      if (rows < 1) return hipErrorInvalidValue;
+      for (int64_t b = 0; b < q.B; b += rows) {
+        ConvArgs a = q;
+        a.B = q.B - b < rows ? q.B - b : rows;
+        a.x = q.x ? static_cast<const T*>(q.x) + b * q.sx_b : nullptr;
+        a.x0 = q.x0 ? static_cast<const T*>(q.x0) + b * (K - 1) * q.D : nullptr;
+        a.lens = q.lens ? q.lens + b : nullptr;
+        a.y = q.y ? static_cast<T*>(q.y) + b * q.T * q.D : nullptr;
+        a.xT = q.xT ? static_cast<T*>(q.xT) + b * (K - 1) * q.D : nullptr;
+        const unsigned groups = (unsigned)((a.B * row + kThreads - 1) / kThreads);
+        const hipError_t e = start(conv_fwd<T, K, V>, dim3(groups), kThreads, st, a, nvec,
+                                   segments, segment);
+        if (e != hipSuccess) return e;
+      }
+      return hipSuccess;
+    });
+  });
+}
+
+uint64_t conv_workspace_bytes(int32_t dtype, int64_t B, int64_t T_, int64_t D, int32_t taps) {
+  uint64_t bytes = 0;
+  (void)by_type(dtype, [&](auto t) {
+    return by_taps(taps, [&](auto k) {
+      typedef decltype(t) T;
+      constexpr int K = decltype(k)::value;
+      bytes = (uint64_t)layout_of<T, K>(B, T_, D).workers * (K + 1) * D * sizeof(Acc<T>);
+      return hipSuccess;
+    });
+  });
+  return bytes;
+}
+
+hipError_t conv_vjp(const ConvArgs& q, void* ws, hipStream_t st) {
+  return by_type(q.dtype, [&](auto t) {
+    return by_taps(q.taps, [&](auto k) {
+      typedef decltype(t) T;
+      constexpr int K = decltype(k)::value, V = lanes_of<T, K>(true);
+      const Layout l = layout_of<T, K>(q.B, q.T, q.D);
+      const bool sums = q.dw || q.dbias;
+      const hipError_t e = start(conv_rev<T, K, V>, dim3((unsigned)(l.slabs * l.workers)), kThreads,
+                                 st, q, l, sums ? ws : nullptr);
+      if (e != hipSuccess || !sums) return e;
+      return start(conv_sum<T>, dim3((unsigned)(((K + 1) * q.D + 63) / 64)), kThreads, st,
+                   static_cast<const Acc<T>*>(ws), l.workers, q.D, K, q.dw, q.dbias,
+                   q.wtype == q.dtype);
+    });
+  });
+}
+
+hipError_t conv_step(const ConvStep& q, hipStream_t st) {
+  return by_type(q.dtype, [&](auto t) {
+    typedef decltype(t) T;
+    constexpr int V = sizeof(T) == 8 ? 1 : sizeof(T) == 4 ? 2 : 4;
+    const int64_t nvec = (q.D + V - 1) / V, groups = (q.B * nvec + kThreads - 1) / kThreads;
+    return start(conv_one<T, V>, dim3((unsigned)groups), kThreads, st, q, nvec);
+  });
+}
+
+}  // namespace adst

@@ -1,0 +1,444 @@
+// Softmax cross entropy of rows x [M][K] over a vocabulary w [V][K] without its
+// logits in memory: lse = log sum_v exp(x w_v), loss = lse - x w_label; and its
+// VJP, g = (exp(x w_v - lse) - [v = label]) dloss, dx = g w, dw = g^T x.
+//
+// Four products of 2 M V K operations (one forward, three in reverse) and little
+// else: the matrix cores bound it, or the read of w where rows are few. Every product
+// is vocab_gemm.h's, with both operands contiguous along the axis that is summed; what
+// follows a product happens in its registers:
+//   forward   a tile's rows to their largest logit and sum of exponentials (online
+//             softmax across tiles: a second kernel joins the tiles in order)
+//   reverse   for a piece of the vocabulary at a time, the logits again and from them g,
+//             written in both orders, rows and columns; then dw of the piece = g^T x and
+//             dx += g w, for which x and the piece of w are transposed once each (a
+//             hundredth of a product's time, against a second kind of product).
+// g is rounded to the element type, which the matrix cores need; each of its elements
+// enters sums of thousands in 32 bits, and its roundings are independent. F16's range
+// would lose small ones, so there g is scaled by the power of two that takes the
+// largest |dloss| to 2^14, which the products' results are divided by.
+#pragma once
+
+#include "vocab_gemm.h"
+
+namespace adst {
+namespace {
+
+constexpr int kJoinThreads = 256;
+
+__device__ inline float exp_(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504f); }
+__device__ inline double exp_(double v) { return exp(v); }
+__device__ inline float log_(float v) { return logf(v); }
+__device__ inline double log_(double v) { return log(v); }
+// What exponentials are taken relative to: 0 where the largest logit is infinite, so that
+// no infinity is subtracted from itself.
+template <class A>
+__device__ inline A pivot(A top) {
+  return __builtin_isinf(top) ? A(0) : top;
+}
+template <class A>
+__device__ inline A larger(A a, A b) {  // a NaN stays
+  return a > b || a != a ? a : b;
+}
+
+// Over the 16 lanes of a row of the wave.
+__device__ inline float row_sum(float v) { return lane_sum<16>(v); }
+__device__ inline double row_sum(double v) { return lane_sum<16>(v); }
+__device__ inline float row_top(float v) {
+  v = larger(v, permuted<0xb1>(v));
+  v = larger(v, permuted<0x4e>(v));
+  v = larger(v, permuted<0x141>(v));
+  return larger(v, permuted<0x140>(v));
+}
+__device__ inline double row_top(double v) {
+#pragma unroll
+  for (int off = 1; off < 16; off <<= 1) v = larger(v, __shfl_xor(v, off, 64));
+  return v;
+}
+
+template <class A>
+struct Stat {
+  A top, sum;  // the sum of exponentials relative to pivot(top)
+};
+template <class A>
+__device__ inline A relative_to(A from, Stat<A> s) {
+  return s.sum == A(0) ? A(0) : s.sum * exp_(pivot(s.top) - from);
+}
+
+struct Tiles {
+  int64_t m, n;       // tiles
+  int64_t K, steps;   // the long axis: elements and steps
+  int64_t splits;     // parts of the steps, along the grid
+};
+
+// ------------------------------------------------------------------- forward
+// [tile column][row] statistics and each row's target logit.
+template <class S, bool DIRECT>
+__global__ __launch_bounds__(S::kThreads) void xent_stats(Rows x, Rows w, Tiles t,
+                                                          const int32_t* labels, void* stats,
+                                                          void* target) {
+  typedef typename S::T T;
+  typedef Acc<T> A;
+  typedef Tile<T> C;
+  __shared__ __attribute__((aligned(16))) char lds[S::ST * S::kStageBytes];
+  const TileAt tile = tile_at(t.m, t.n, blockIdx.x);
+  const int64_t m0 = tile.m * S::BM, n0 = tile.n * S::BN;
+  S s;
+  multiply<S, DIRECT>(s, lds, x, w, t.K, m0, n0, 0, t.steps);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
+  Stat<A>(*const part)[S::WN] = reinterpret_cast<Stat<A>(*)[S::WN]>(lds);  // [row of the tile]
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = (wm * S::MT + i) * 16 + C::at(lane, r);
+      const int64_t m = m0 + row;
+      const int64_t label = m < x.n ? labels[m] : -1;
+      A top = -__builtin_inf();
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        const int64_t n = n0 + (wn * S::NT + j) * 16 + col;
+        const A v = s.acc[i][j][r];
+        if (n == label) static_cast<A*>(target)[m] = v;
+        if (n < w.n) top = larger(v, top);
+      }
+      top = row_top(top);
+      const A from = pivot(top);
+      A sum = A(0);
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        const int64_t n = n0 + (wn * S::NT + j) * 16 + col;
+        if (n < w.n) sum += exp_(s.acc[i][j][r] - from);
+      }
+      sum = row_sum(sum);
+      if (col == 0) part[row][wn] = {top, sum};
+    }
+  __syncthreads();
+  for (int row = threadIdx.x; row < S::BM; row += S::kThreads) {
+    if (m0 + row >= x.n) continue;
+    A top = part[row][0].top;
+#pragma unroll
+    for (int k = 1; k < S::WN; ++k) top = larger(part[row][k].top, top);
+    const A from = pivot(top);
+    A sum = A(0);
+#pragma unroll
+    for (int k = 0; k < S::WN; ++k) sum += relative_to(from, part[row][k]);
+    static_cast<Stat<A>*>(stats)[tile.n * x.n + m0 + row] = {top, sum};
+  }
+}
+
+// loss and lse from the tiles' statistics. W lanes of a wave share a row.
+template <class T, int W>
+__global__ __launch_bounds__(kJoinThreads) void xent_join(const void* stats, const void* target,
+                                                          const int32_t* labels, int64_t M,
+                                                          int64_t V, int64_t columns, void* loss,
+                                                          void* lse) {
+  typedef Acc<T> A;
+  const int64_t m = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) / W;
+  const int lane = threadIdx.x % W;
+  const Stat<A>* const from = static_cast<const Stat<A>*>(stats);
+  const int64_t row = m < M ? m : M - 1;
+  A top = -__builtin_inf();
+  for (int64_t k = lane; k < columns; k += W) top = larger(from[k * M + row].top, top);
+#pragma unroll
+  for (int by = 1; by < W; by <<= 1) top = larger(top, __shfl_xor(top, by, 64));
+  const A at = pivot(top);
+  A sum = A(0);
+  for (int64_t k = lane; k < columns; k += W) sum += relative_to(at, from[k * M + row]);
+#pragma unroll
+  for (int by = 1; by < W; by <<= 1) sum += __shfl_xor(sum, by, 64);
+  if (m >= M || lane > 0) return;
+  const A v = at + log_(sum);
+  if (lse) static_cast<A*>(lse)[m] = v;
+  if (loss) {
+    const bool has = labels[m] >= 0 && labels[m] < V;
+    static_cast<A*>(loss)[m] = has ? v - static_cast<const A*>(target)[m] : A(0);
+  }
+}
+
+// ------------------------------------------------------------------- reverse
+// What a row's g is multiplied by: 0 where it takes no part.
+template <class A>
+__device__ inline A row_weight(const int32_t* labels, const void* dloss, int64_t m, int64_t V) {
+  const int64_t label = labels[m];
+  if (label < 0 || label >= V) return A(0);
+  return dloss ? static_cast<const A*>(dloss)[m] : A(1);
+}
+
+// scale[0]: the power of two that takes the largest finite |dloss| of the rows that take part
+// to [2^14, 2^15); scale[1]: its inverse. One workgroup.
+__global__ __launch_bounds__(1024) void xent_scale(const int32_t* labels, const void* dloss,
+                                                   int64_t M, int64_t V, float* scale) {
+  __shared__ float part[16];
+  float top = 0.0f;
+#pragma unroll 4
+  for (int64_t m = threadIdx.x; m < M; m += 1024) {
+    const float v = __builtin_fabsf(row_weight<float>(labels, dloss, m, V));
+    if (v > top && !__builtin_isinf(v)) top = v;
+  }
+  for (int by = 1; by < 64; by <<= 1) {
+    const float other = __shfl_xor(top, by, 64);
+    top = other > top ? other : top;
+  }
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  for (int k = 1; k < 16; ++k) top = part[k] > top ? part[k] : top;
+  // exponent of top, kept where both powers are normal numbers
+  int e = (int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127;
+  e = top > 0.0f ? (e < -100 ? -100 : e > 100 ? 100 : e) : 14;
+  scale[0] = __builtin_bit_cast(float, (uint32_t)(127 + 14 - e) << 23);
+  scale[1] = __builtin_bit_cast(float, (uint32_t)(127 + e - 14) << 23);
+}
+
+// to [cols][pad] = from [rows][cols] transposed, zeros from `rows` to `pad`. KEEP: rows
+// without a weight are zeros, whatever they hold.
+constexpr int kTurn = 64;
+template <class T, bool KEEP>
+__global__ __launch_bounds__(256) void xent_turn(Rows from, int64_t cols, int64_t pad, void* to,
+                                                 const int32_t* labels, const void* dloss,
+                                                 int64_t V) {
+  __shared__ T tile[kTurn][kTurn + 16 / sizeof(T) / 2];
+  const int64_t across = (cols + kTurn - 1) / kTurn;
+  const int64_t r0 = blockIdx.x / across * kTurn, c0 = blockIdx.x % across * kTurn;
+  const int c = threadIdx.x % kTurn, first = threadIdx.x / kTurn;
+#pragma unroll 4
+  for (int r = first; r < kTurn; r += 256 / kTurn) {
+    const int64_t row = r0 + r;
+    bool there = row < from.n && c0 + c < cols;
+    if (KEEP && there) there = row_weight<Acc<T>>(labels, dloss, row, V) != Acc<T>(0);
+    tile[r][c] = there ? static_cast<const T*>(from.p)[row * from.stride + c0 + c] : T(0);
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int r = first; r < kTurn; r += 256 / kTurn)
+    if (c0 + r < cols && r0 + c < pad)
+      static_cast<T*>(to)[(c0 + r) * pad + r0 + c] = tile[c][r];
+}
+
+// g of a piece of the vocabulary, whose first word is v0: [rows][piece] and, transposed,
+// [piece][m_pad]. Both are whole: zeros beyond the vocabulary and the rows.
+struct GArgs {
+  const int32_t* labels;
+  const void* lse;
+  const void* dloss;
+  const float* scale;  // or NULL
+  int64_t v0, V, piece, m_pad;
+  void* g;
+  void* gt;
+};
+template <class S, bool DIRECT>
+__global__ __launch_bounds__(S::kThreads) void xent_grad(Rows x, Rows w, Tiles t, GArgs q) {
+  typedef typename S::T T;
+  typedef Acc<T> A;
+  typedef Tile<T> C;
+  __shared__ __attribute__((aligned(16))) char lds[S::ST * S::kStageBytes];
+  const TileAt tile = tile_at(t.m, t.n, blockIdx.x);
+  const int64_t m0 = tile.m * S::BM, n0 = tile.n * S::BN;
+  S s;
+  multiply<S, DIRECT>(s, lds, x, w, t.K, m0, n0, 0, t.steps);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
+  const A scale = q.scale ? (A)q.scale[0] : A(1);
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t m = m0 + (wm * S::MT + i) * 16 + C::at(lane, r);
+      const bool row = m < x.n;
+      const A weight = row ? row_weight<A>(q.labels, q.dloss, m, q.V) : A(0);
+      const A lse = row ? static_cast<const A*>(q.lse)[m] : A(0);
+      const int64_t label = row ? q.labels[m] - q.v0 : -1;
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        const int64_t n = n0 + (wn * S::NT + j) * 16 + col;
+        A v = A(0);
+        if (weight != A(0) && n < w.n)
+          v = (exp_(s.acc[i][j][r] - lse) - (n == label ? A(1) : A(0))) * (weight * scale);
+        const T out = down<T>(v);
+        if (row && n < q.piece) static_cast<T*>(q.g)[m * q.piece + n] = out;
+        if (m < q.m_pad && n < q.piece) static_cast<T*>(q.gt)[n * q.m_pad + m] = out;
+      }
+    }
+}
+
+// C [rows][n] from a product of whole steps: rounded to `out`, or added to (`add`: after
+// earlier pieces) its split's sums [split][rows][n].
+struct OutArgs {
+  void* out;
+  void* sums;
+  const float* scale;
+  bool add;
+};
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void xent_product(Rows a, Rows b, Tiles t, OutArgs q) {
+  typedef typename S::T T;
+  typedef Acc<T> A;
+  typedef Tile<T> C;
+  __shared__ __attribute__((aligned(16))) char lds[S::ST * S::kStageBytes];
+  const int64_t split = blockIdx.x % t.splits;
+  const TileAt tile = tile_at(t.m, t.n, blockIdx.x / t.splits);
+  const int64_t m0 = tile.m * S::BM, n0 = tile.n * S::BN;
+  S s;
+  multiply<S, true>(s, lds, a, b, t.K, m0, n0, t.steps * split / t.splits,
+                    t.steps * (split + 1) / t.splits);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
+  const A back = q.out && q.scale ? (A)q.scale[1] : A(1);
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t m = m0 + (wm * S::MT + i) * 16 + C::at(lane, r);
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        const int64_t n = n0 + (wn * S::NT + j) * 16 + col;
+        if (m >= a.n || n >= b.n) continue;
+        const A v = s.acc[i][j][r];
+        if (q.out) {
+          static_cast<T*>(q.out)[m * b.n + n] = down<T>(v * back);
+        } else {
+          A* const to = static_cast<A*>(q.sums) + (split * a.n + m) * b.n + n;
+          *to = q.add ? *to + v : v;
+        }
+      }
+    }
+}
+
+// out = the splits' sums added in order, rounded.
+template <class T>
+__global__ __launch_bounds__(256) void xent_sum(const void* sums, int64_t n, int64_t splits,
+                                                const float* scale, void* out) {
+  typedef Acc<T> A;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  A v = A(0);
+#pragma unroll 4
+  for (int64_t k = 0; k < splits; ++k) v += static_cast<const A*>(sums)[k * n + i];
+  static_cast<T*>(out)[i] = down<T>(scale ? v * (A)scale[1] : v);
+}
+
+// ------------------------------------------------------------------ launches
+template <class T>
+using Large = GemmShape<T, 2, 4, 8, 4, 2>;   // 256 x 256
+template <class T>
+using Middle = GemmShape<T, 2, 2, 4, 4, 2>;  // 128 x 128
+template <class T>
+using Few = GemmShape<T, 1, 4, 4, 1, 4>;     // 64 x 64: few rows
+
+inline int64_t parts(int64_t n, int64_t by) { return (n + by - 1) / by; }
+template <class S>
+Tiles tiles_of(int64_t m, int64_t n, int64_t K, int64_t splits) {
+  return {parts(m, S::BM), parts(n, S::BN), K, parts(K, S::kStep), splits};
+}
+
+// f(shape): the largest tiles that fill the card's 256 CUs, the smallest where rows are few.
+template <class T, class F>
+hipError_t by_size(int64_t m, int64_t n, F f) {
+  if constexpr (sizeof(T) < 8)
+    if (parts(m, 256) * parts(n, 256) >= 200) return f(Large<T>());
+  if (m <= 64) return f(Few<T>());
+  return f(Middle<T>());
+}
+
+template <class T>
+bool whole_pieces(const void* p, int64_t stride, int64_t K) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (int64_t)sizeof(T) % 16 == 0 &&
+         K * (int64_t)sizeof(T) % kStepBytes == 0;
+}
+
+template <class T>
+hipError_t forward_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st) {
+  char* const at = static_cast<char*>(ws);
+  const bool direct = whole_pieces<T>(a.x, a.sx, a.K) && whole_pieces<T>(a.w, a.sw, a.K);
+  const Rows x{a.x, a.sx, a.M}, w{a.w, a.sw, a.V};
+  return by_size<T>(a.M, a.V, [&](auto shape) {
+    typedef decltype(shape) S;
+    const Tiles t = tiles_of<S>(a.M, a.V, a.K, 1);
+    hipError_t e = start(direct ? xent_stats<S, true> : xent_stats<S, false>,
+                         dim3((unsigned)(t.m * t.n)), S::kThreads, st, x, w, t, a.labels,
+                         at + p.stats, at + p.target);
+    if (e != hipSuccess) return e;
+    const void *stats = at + p.stats, *target = at + p.target;
+    if (a.M < 2048)
+      return start(xent_join<T, 64>, dim3((unsigned)parts(a.M * 64, kJoinThreads)), kJoinThreads,
+                   st, stats, target, a.labels, a.M, a.V, t.n, a.loss, a.lse);
+    return start(xent_join<T, 4>, dim3((unsigned)parts(a.M * 4, kJoinThreads)), kJoinThreads, st,
+                 stats, target, a.labels, a.M, a.V, t.n, a.loss, a.lse);
+  });
+}
+
+template <class T>
+hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st) {
+  if (a.M == 0)  // no rows: dw is zero, a sum of nothing
+    return start(xent_sum<T>, dim3((unsigned)parts(a.V * a.K, 256)), 256, st, nullptr, a.V * a.K, 0,
+                 nullptr, a.dw);
+  char* const at = static_cast<char*>(ws);
+  const Rows x{a.x, a.sx, a.M};
+  hipError_t e = hipSuccess;
+  const float* scale = nullptr;
+  if (a.dtype == ADST_F16) {
+    scale = reinterpret_cast<const float*>(at + p.scale);
+    e = start(xent_scale, dim3(1), 1024, st, a.labels, a.dloss, a.M, a.V,
+              reinterpret_cast<float*>(at + p.scale));
+    if (e != hipSuccess) return e;
+  }
+  if (a.dw) {
+    e = start(xent_turn<T, true>,
+              dim3((unsigned)(parts(p.m_pad, kTurn) * parts(a.K, kTurn))), 256, st, x, a.K, p.m_pad,
+              at + p.xt, a.labels, a.dloss, a.V);
+    if (e != hipSuccess) return e;
+  }
+  for (int64_t v0 = 0; v0 < a.V; v0 += p.piece) {
+    const int64_t words = a.V - v0 < p.piece ? a.V - v0 : p.piece;
+    const Rows w{static_cast<const T*>(a.w) + v0 * a.sw, a.sw, words};
+    const bool direct = whole_pieces<T>(x.p, x.stride, a.K) && whole_pieces<T>(w.p, w.stride, a.K);
+    const GArgs q{a.labels, a.lse, a.dloss, scale, v0, a.V, p.piece, p.m_pad, at + p.g, at + p.gt};
+    // the products' long axes: this piece's words, and the rows, in whole steps
+    e = by_size<T>(a.M, words, [&](auto shape) {
+      typedef decltype(shape) S;
+      Tiles t = tiles_of<S>(p.m_pad, p.piece, a.K, 1);
+      return start(direct ? xent_grad<S, true> : xent_grad<S, false>, dim3((unsigned)(t.m * t.n)),
+                   S::kThreads, st, x, w, t, q);
+    });
+    if (e != hipSuccess) return e;
+    if (a.dw) {
+      const Rows gt{at + p.gt, p.m_pad, words}, xt{at + p.xt, p.m_pad, a.K};
+      T* const out = static_cast<T*>(a.dw) + v0 * a.K;
+      const bool split = p.dw_splits > 1;
+      e = by_size<T>(words, a.K, [&](auto shape) {
+        typedef decltype(shape) S;
+        const Tiles t = tiles_of<S>(words, a.K, p.m_pad, p.dw_splits);
+        return start(xent_product<S>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, gt,
+                     xt, t, OutArgs{split ? nullptr : out, at + p.dw_sums, scale, false});
+      });
+      if (e != hipSuccess) return e;
+      if (split) {
+        e = start(xent_sum<T>, dim3((unsigned)parts(words * a.K, 256)), 256, st, at + p.dw_sums,
+                  words * a.K, p.dw_splits, scale, out);
+        if (e != hipSuccess) return e;
+      }
+    }
+    if (a.dx) {
+      e = start(xent_turn<T, false>,
+                dim3((unsigned)(parts(p.piece, kTurn) * parts(a.K, kTurn))), 256, st, w, a.K,
+                p.piece, at + p.wt, a.labels, a.dloss, a.V);
+      if (e != hipSuccess) return e;
+      const Rows g{at + p.g, p.piece, a.M}, wt{at + p.wt, p.piece, a.K};
+      e = by_size<T>(a.M, a.K, [&](auto shape) {
+        typedef decltype(shape) S;
+        const Tiles t = tiles_of<S>(a.M, a.K, p.piece, p.dx_splits);
+        return start(xent_product<S>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, g,
+                     wt, t, OutArgs{p.dx_direct ? a.dx : nullptr, at + p.dx_sums, scale, v0 > 0});
+      });
+      if (e != hipSuccess) return e;
+    }
+  }
+  if (a.dx && !p.dx_direct)
+    return start(xent_sum<T>, dim3((unsigned)parts(a.M * a.K, 256)), 256, st, at + p.dx_sums,
+                 a.M * a.K, p.dx_splits, scale, a.dx);
+  return hipSuccess;
+}
+
+}  // namespace
+}  // namespace adst

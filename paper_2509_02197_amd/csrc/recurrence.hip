@@ -41,45 +41,13 @@
 // needed; the accesses are of agent scope, which the caches of the XCDs keep
 // coherent.
 
+#include "packs.h"
 #include "seq_common.h"
 #include "seq_kernels.h"
 #include "seq_launch.h"
 
 namespace adst {
 namespace {
-
-// V consecutive channels of T, at any element's address.
-template <class T, int V>
-struct Pack {
-  typedef T type __attribute__((ext_vector_type(V)));
-  typedef T unaligned __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-  type v;
-};
-template <class T, int V, bool STREAM = false>
-__device__ inline Pack<T, V> load_pack(const T* p, int n) {
-  Pack<T, V> r;
-  if (n >= V) {
-    const auto* at = reinterpret_cast<const typename Pack<T, V>::unaligned*>(p);
-    if constexpr (STREAM) r.v = __builtin_nontemporal_load(at);
-    else r.v = *at;
-    return r;
-  }
-#pragma unroll
-  for (int i = 0; i < V; ++i) r.v[i] = i < n ? p[i] : T(0);
-  return r;
-}
-template <class T, int V, bool STREAM = false>
-__device__ inline void store_pack(T* p, Pack<T, V> x, int n) {
-  if (n >= V) {
-    auto* at = reinterpret_cast<typename Pack<T, V>::unaligned*>(p);
-    if constexpr (STREAM) __builtin_nontemporal_store(x.v, at);
-    else *at = x.v;
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (i < n) p[i] = x.v[i];
-}
 
 // A workgroup of NT threads: L lanes of a wave lie along channels, V of them a
 // lane, and its 64 / L rows of lanes along time, R consecutive steps each.
@@ -145,31 +113,7 @@ struct Board {
 };
 constexpr int kCounterInts = 8;
 
-// ---------------------------------------------------------------- the gates
-__device__ inline float exp_full(float x) { return expf(x); }
-__device__ inline double exp_full(double x) { return exp(x); }
-__device__ inline float inverse(float x) { return __builtin_amdgcn_rcpf(x); }  // within 1 ulp
-__device__ inline double inverse(double x) { return 1.0 / x; }
-
-// s = 1 / (1 + exp(-a)) and q = 1 - s = 1 / (1 + exp(a)), each to full
-// relative precision down to the type's smallest normal value, and 0 and 1 are
-// reached. Behind a 16-bit value the exponential may be off by |a| units of
-// 2^-24.
-template <class T>
-__device__ inline void gates(Acc<T> a, Acc<T>* s, Acc<T>* q) {
-  typedef Acc<T> A;
-  if constexpr (sizeof(T) == 2) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * a);
-    *s = inverse(1.0f + e);
-    *q = e > 0x1p126f ? 1.0f : e * *s;  // beyond, 1 / e is no normal value; NaN stays
-  } else {  // with e = exp(-|a|) in [0, 1] nothing overflows, and 0 and 1 are reached
-    const A e = exp_full(-__builtin_elementwise_abs(a));
-    const A big = inverse(A(1) + e), small = e * big;
-    *s = __builtin_signbit(a) ? small : big;
-    *q = __builtin_signbit(a) ? big : small;
-  }
-}
-
+// -------------------------------------------------------------- registers
 // The compiler treats the values as new ones: it does not keep what it
 // derived from them before, which would take more registers than there are.
 template <class A, int R, int V>
@@ -189,12 +133,6 @@ __device__ inline void forget(Pack<T, V> (&x)[R]) {  // and unpacks again
       x[r].v = __builtin_bit_cast(typename Pack<T, V>::type, w);
     }
   }
-}
-
-__device__ inline int64_t row_length(const int32_t* lens, int64_t b, int64_t T) {
-  if (!lens) return T;
-  const int64_t n = lens[b];
-  return n < 0 ? 0 : n > T ? T : n;
 }
 
 // ------------------------------------------------------- maps along the time

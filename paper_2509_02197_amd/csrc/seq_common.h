@@ -1,5 +1,5 @@
-// Device helpers shared by the sequence operators' kernels (recurrence.hip,
-// layer_norm.hip, adamw.hip): element types and their accumulation type,
+// Device helpers shared by the kernels of the sequence and token operators:
+// element types and their accumulation type,
 // 16-byte vectors at any element's address, wave reductions.
 #pragma once
 
@@ -86,6 +86,36 @@ __device__ inline void store_part(T* p, Vec<T> v, int n) {
 
 __device__ inline float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
 __device__ inline double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
+
+__device__ inline float exp_full(float x) { return expf(x); }
+__device__ inline double exp_full(double x) { return exp(x); }
+__device__ inline float inverse(float x) { return __builtin_amdgcn_rcpf(x); }  // within 1 ulp
+__device__ inline double inverse(double x) { return 1.0 / x; }
+
+// s = 1 / (1 + exp(-a)) and q = 1 - s = 1 / (1 + exp(a)), each to full
+// relative precision down to the type's smallest normal value, and 0 and 1 are
+// reached. Behind a 16-bit value the exponential may be off by |a| units of
+// 2^-24.
+template <class T>
+__device__ inline void gates(Acc<T> a, Acc<T>* s, Acc<T>* q) {
+  typedef Acc<T> A;
+  if constexpr (sizeof(T) == 2) {
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * a);
+    *s = inverse(1.0f + e);
+    *q = e > 0x1p126f ? 1.0f : e * *s;  // beyond, 1 / e is no normal value; NaN stays
+  } else {  // with e = exp(-|a|) in [0, 1] nothing overflows, and 0 and 1 are reached
+    const A e = exp_full(-__builtin_elementwise_abs(a));
+    const A big = inverse(A(1) + e), small = e * big;
+    *s = __builtin_signbit(a) ? small : big;
+    *q = __builtin_signbit(a) ? big : small;
+  }
+}
+
+__device__ inline int64_t row_length(const int32_t* lens, int64_t b, int64_t T) {
+  if (!lens) return T;
+  const int64_t n = lens[b];
+  return n < 0 ? 0 : n > T ? T : n;
+}
 
 // Sum over groups of W consecutive lanes (16 or 64), in every lane, in an
 // order that is the same for all of them. Within a row of 16 lanes the values

@@ -116,56 +116,154 @@ __device__ inline int64_t work_id(int64_t n) {
   return n % 8 == 0 ? x % 8 * (n / 8) + x / 8 : x;
 }
 
-// The chunk's steps of one input, as a thread has them: E channels of step `row`.
-template <class S>
+// What a thread loads and stores of a chunk: E channels of step `row`. FULL: every slab has
+// all of its channels. Loads need no bounds: steps that are not there are read as the
+// first one, channels as the last one, and their values are not used.
+template <class S, bool FULL>
 struct Loader {
-  int row, c, n;  // n: channels that exist
+  int row, c, last, n;  // n: channels that exist
+  bool stores;
   __device__ Loader(const Place& p) {
-    row = threadIdx.x / S::kRowThreads;
+    row = threadIdx.x / S::kRowThreads % S::R;
     c = threadIdx.x % S::kRowThreads * S::E;
-    const int left = p.channels - c;
-    n = threadIdx.x < S::kLoaders && left > 0 ? (left < S::E ? left : S::E) : 0;
+    last = p.channels - 1;
+    n = FULL ? S::E : p.channels - c < S::E ? p.channels - c : S::E;
+    stores = threadIdx.x < S::kLoaders && (FULL || n > 0);
   }
   template <class T>
-  __device__ Pack<T, S::E> load(const void* from, int64_t at, bool there) const {
-    return load_pack<T, S::E>(static_cast<const T*>(from) + at, there ? n : 0);
+  __device__ Pack<T, S::E> load(const T* from) const {  // from: of the slab's first channel
+    Pack<T, S::E> v;
+    if constexpr (FULL) {
+      v = load_pack<T, S::E>(from + c, S::E);
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::E; ++i) v.v[i] = from[c + i < last ? c + i : last];
+    }
+    return v;
+  }
+  template <class T>
+  __device__ void store(T* to, const Pack<T, S::E>& v) const {
+    store_pack<T, S::E>(to + c, v, n);
   }
   template <class A>
   __device__ void constants(const void* from, int64_t d0, A (&to)[S::E]) const {
 #pragma unroll
     for (int i = 0; i < S::E; ++i)
-      to[i] = from && i < n ? static_cast<const A*>(from)[d0 + c + i] : A(0);
+      to[i] = from ? static_cast<const A*>(from)[d0 + (c + i < last ? c + i : last)] : A(0);
   }
 };
 
-// B and C of a chunk: [step][B or C][state] in LDS, zero where there is none.
-template <class T, class S>
-struct Coefficients {
-  typedef Acc<T> A;
-  T v[2][S::NB];
-  __device__ void load(const ScanArgs& a, const Place& p, int64_t t0, int rows, bool with_b) {
-    const T* const at[2] = {
-        static_cast<const T*>(a.Bm) + p.b * a.sb_b + t0 * a.sb_t + p.group * a.N,
-        static_cast<const T*>(a.Cm) + p.b * a.sc_b + t0 * a.sc_t + p.group * a.N};
-#pragma unroll
-    for (int i = 0; i < S::NB; ++i) {
-      const int k = threadIdx.x + i * S::NT, r = k / S::NP, n = k % S::NP;
-      const bool there = r < rows && n < a.N;
-      v[0][i] = there && with_b ? at[0][r * a.sb_t + n] : T(0);
-      v[1][i] = there ? at[1][r * a.sc_t + n] : T(0);
-    }
+// An input [batch][step][channel] as a thread goes through it, chunk after chunk.
+template <class T>
+struct Walk {
+  const T *first, *at;
+  int64_t by;
+  // of batch row b from step t0 on, for the thread's row; chunks of R steps forwards or back
+  __device__ Walk(const void* p, int64_t b, int64_t sb, int64_t st, int64_t t0, int64_t start,
+                  int row, int64_t d0, int step) {
+    const T* const base = p ? static_cast<const T*>(p) + b * sb + d0 : nullptr;
+    first = base + t0 * st;
+    at = base + (start + row) * st;
+    by = st * step;
   }
-  __device__ void put(A (&bc)[S::R][2][S::NP]) const {
+  __device__ const T* next(bool there) {
+    const T* const now = there ? at : first;
+    at += by;
+    return now;
+  }
+};
+
+// B and C of a chunk, {B, C} of a lane's states together in LDS.
+template <class S>
+struct Coefficients {
+  typedef typename S::A A;
+  struct alignas(2 * S::NS * sizeof(A)) Of {
+    A b[S::NS], c[S::NS];
+  };
+};
+template <class T, class S>
+struct CoefficientLoader {
+  Walk<T> b, c;
+  int row[S::NB], n[S::NB];
+  int64_t of_b[S::NB], of_c[S::NB];
+  __device__ CoefficientLoader(const ScanArgs& a, const Place& p, int64_t t0, int64_t start,
+                               int step)
+      : b(a.Bm, p.b, a.sb_b, a.sb_t, t0, start, 0, p.group * a.N, step),
+        c(a.Cm, p.b, a.sc_b, a.sc_t, t0, start, 0, p.group * a.N, step) {
 #pragma unroll
     for (int i = 0; i < S::NB; ++i) {
-      const int k = threadIdx.x + i * S::NT, r = k / S::NP, n = k % S::NP;
-      if (r < S::R) {
-        bc[r][0][n] = up(v[0][i]);
-        bc[r][1][n] = up(v[1][i]);
-      }
+      const int k = threadIdx.x + i * S::NT;
+      row[i] = k / S::NP;
+      n[i] = k % S::NP;
+      const int state = n[i] < a.N ? n[i] : 0;
+      of_b[i] = row[i] * a.sb_t + state;
+      of_c[i] = row[i] * a.sc_t + state;
     }
   }
 };
+
+// A chunk's inputs on their way.
+template <class T, class S>
+struct Inputs {
+  Pack<T, S::E> x, delta, z, dy;
+  T b[S::NB], c[S::NB];
+  typename S::A before[S::NS];
+  __device__ void request(CoefficientLoader<T, S>& l, int64_t left) {
+#pragma unroll
+    for (int i = 0; i < S::NB; ++i) {
+      const bool there = l.row[i] < left;
+      b[i] = there ? l.b.at[l.of_b[i]] : *l.b.first;
+      c[i] = there ? l.c.at[l.of_c[i]] : *l.c.first;
+    }
+    l.b.at += l.b.by;
+    l.c.at += l.c.by;
+  }
+  __device__ void put(const CoefficientLoader<T, S>& l, int states,
+                      typename Coefficients<S>::Of (&bc)[S::R][S::SG]) const {
+    typedef typename S::A A;
+#pragma unroll
+    for (int i = 0; i < S::NB; ++i)
+      if (S::R * S::NP % S::NT == 0 || l.row[i] < S::R) {
+        const bool there = l.n[i] < states;
+        bc[l.row[i]][l.n[i] / S::NS].b[l.n[i] % S::NS] = there ? up(b[i]) : A(0);
+        bc[l.row[i]][l.n[i] / S::NS].c[l.n[i] % S::NS] = there ? up(c[i]) : A(0);
+      }
+  }
+};
+
+// The sums of R values over the lanes that share a channel: first over a wave's two
+// halves, after which the lower one holds the chunk's first steps and the upper one the others.
+__device__ inline float add_halves(float first, float second) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, first),
+                                                  __builtin_bit_cast(uint32_t, second), false,
+                                                  false);
+  const uint32_t low = r[0], high = r[1];
+  return __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
+}
+__device__ inline double add_halves(double first, double second) {
+  const bool upper = threadIdx.x & 32;
+  return (upper ? second : first) + __shfl_xor(upper ? first : second, 32, 64);
+}
+template <class S>
+__device__ inline void leave(const typename S::A (&sums)[S::R],
+                             typename S::A (&part)[S::R][S::W][kSlab]) {
+  constexpr int H = S::R / 2;
+  const int wave = threadIdx.x / 64, c = threadIdx.x % kSlab, half = threadIdx.x / kSlab % 2 * H;
+#pragma unroll
+  for (int r = 0; r < H; ++r) part[half + r][wave][c] = add_halves(sums[r], sums[r + H]);
+}
+template <class S>
+__device__ inline void gather(const typename S::A (&part)[S::R][S::W][kSlab], int row, int c,
+                              typename S::A (&sums)[S::E]) {
+  typedef typename S::A A;
+  typedef A V __attribute__((ext_vector_type(S::E), aligned(sizeof(A) * (S::E < 4 ? S::E : 4))));
+#pragma unroll
+  for (int q = 0; q < S::W; ++q) {
+    const V v = *reinterpret_cast<const V*>(&part[row][q][c]);
+#pragma unroll
+    for (int i = 0; i < S::E; ++i) sums[i] = q == 0 ? (A)v[i] : sums[i] + (A)v[i];
+  }
+}
 
 // A lane's states: their channel, the first state and how many of them there are.
 struct Lane {
@@ -229,16 +327,16 @@ __device__ inline void through(const Maps<A>& m, const ScanArgs& a, const ScanGr
 template <class S>
 struct ForwardLds {
   typedef typename S::A A;
-  struct Two {
+  struct alignas(2 * sizeof(A)) Two {
     A s, sx;
   };
+  typename Coefficients<S>::Of bc[S::R][S::SG];
   Two in[S::R][kSlab];
-  A bc[S::R][2][S::NP];
-  A part[S::R][S::SG][kSlab];
+  A part[S::R][S::W][kSlab];
 };
 
 // MAP: the segment's map alone.
-template <class T, int NS, int W, bool MAP>
+template <class T, int NS, int W, bool MAP, bool FULL>
 __global__ __launch_bounds__(64 * W) void scan_fwd(ScanArgs a, ScanGrid g, void* ws) {
   typedef ScanShape<T, NS, W> S;
   typedef Acc<T> A;
@@ -250,7 +348,7 @@ __global__ __launch_bounds__(64 * W) void scan_fwd(ScanArgs a, ScanGrid g, void*
   const int64_t t1 = a.T - t0 < span ? a.T : t0 + span;
   if (MAP && len <= t1) return;  // no segment follows
   const int64_t live = len < t1 ? len : t1;
-  const Loader<S> at(p);
+  const Loader<S, FULL> at(p);
   const Lane l = lane_of<S>(a, p);
   const int64_t d = p.d0 + l.c;
   A rates[NS], h[NS], total = A(0);
@@ -266,74 +364,90 @@ __global__ __launch_bounds__(64 * W) void scan_fwd(ScanArgs a, ScanGrid g, void*
   A skip[E], bias[E];
   at.constants(a.D, p.d0, skip);
   at.constants(a.bias, p.d0, bias);
-  const int64_t from = p.d0 + at.c;
-  T* const y = static_cast<T*>(a.y);
-  Pack<T, E> x, delta, z;
-  Coefficients<T, S> bc;
-  const auto request = [&](int64_t t) {  // a chunk's inputs
+  T* y = a.y ? static_cast<T*>(a.y) + (p.b * a.T + t0 + at.row) * a.D_ + p.d0 : nullptr;
+  A* ck = static_cast<A*>(a.ck) + ((p.b * g.chunks + t0 / R) * a.N + l.first) * a.D_ + d;
+  Walk<T> xs(a.x, p.b, a.sx_b, a.sx_t, t0, t0, at.row, p.d0, R);
+  Walk<T> deltas(a.delta, p.b, a.sl_b, a.sl_t, t0, t0, at.row, p.d0, R);
+  Walk<T> zs(a.z, p.b, a.sz_b, a.sz_t, t0, t0, at.row, p.d0, R);
+  CoefficientLoader<T, S> coefficients(a, p, t0, t0, R);
+  const bool gated = !MAP && a.z;
+  const auto request = [&](Inputs<T, S>& in, int64_t t) {  // chunk after chunk
     const bool there = t + at.row < live;
-    x = at.template load<T>(a.x, p.b * a.sx_b + (t + at.row) * a.sx_t + from, there);
-    delta = at.template load<T>(a.delta, p.b * a.sl_b + (t + at.row) * a.sl_t + from, there);
-    if (!MAP && a.z)
-      z = at.template load<T>(a.z, p.b * a.sz_b + (t + at.row) * a.sz_t + from, there);
-    bc.load(a, p, t, (int)(live - t < R ? live - t : R), true);
+    in.x = at.load(xs.next(there));
+    in.delta = at.load(deltas.next(there));
+    if (gated) in.z = at.load(zs.next(there));
+    in.request(coefficients, live - t);
   };
-  if (t0 < live) request(t0);
-  for (int64_t t = t0; t < live; t += R) {
+  const auto chunk = [&](Inputs<T, S>& in, int64_t t) {
     const int rows = (int)(live - t < R ? live - t : R);
-    if (threadIdx.x < S::kLoaders) {
+    if (S::kLoaders == S::NT || threadIdx.x < S::kLoaders) {
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        A s = up((T)delta.v[i]) + bias[i];
+        A s = up((T)in.delta.v[i]) + bias[i];
         if (a.softplus) s = softplus(s);
-        lds.in[at.row][at.c + i] = {s, s * up((T)x.v[i])};
+        lds.in[at.row][at.c + i] = {s, s * up((T)in.x.v[i])};
       }
     }
-    bc.put(lds.bc);
+    in.put(coefficients, a.N, lds.bc);
+    const Pack<T, E> x = in.x, z = in.z;
     __syncthreads();
-    const Pack<T, E> old_x = x, old_z = z;
-    if (t + R < live) request(t + R);
+    request(in, t + 2 * R);
     if (!MAP && a.ck) {
-      A* const ck = static_cast<A*>(a.ck) + (p.b * g.chunks + t / R) * a.N * a.D_;
 #pragma unroll
       for (int i = 0; i < NS; ++i)
-        if (i < l.count) ck[(l.first + i) * a.D_ + d] = h[i];
+        if (i < l.count) ck[i * a.D_] = h[i];
+      ck += a.N * a.D_;
     }
-    const auto sweep = [&](auto steps) {
+    A sums[R];
+    const auto step = [&](int r) {
+      const auto now = lds.in[r][l.c];
+      const auto bc = lds.bc[r][l.group];
+      A sum = A(0);
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (!steps.has(r)) break;
-        const auto in = lds.in[r][l.c];
-        A sum = A(0);
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          h[i] = fma_(decay(in.s, rates[i]), h[i], in.sx * lds.bc[r][0][l.first + i]);
-          if (!MAP) sum = fma_(lds.bc[r][1][l.first + i], h[i], sum);
-        }
-        if (MAP) total += in.s;
-        else lds.part[r][l.group][l.c] = sum;
+      for (int i = 0; i < NS; ++i) {
+        h[i] = fma_(decay(now.s, rates[i]), h[i], now.sx * bc.b[i]);
+        if (!MAP) sum = fma_(bc.c[i], h[i], sum);
       }
+      if (MAP) total += now.s;
+      return sum;
     };
-    if (rows == R) sweep(Steps<true, R>{R});
-    else sweep(Steps<false, R>{rows});
+    if (rows == R) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) sums[r] = step(r);
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r) sums[r] = r < rows ? step(r) : A(0);
+    }
+    if (!MAP) leave<S>(sums, lds.part);
     __syncthreads();
-    if (!MAP && y && t + at.row < live && at.n > 0) {
-      Pack<T, E> out;
+    if (!MAP && y) {
+      if (at.stores && at.row < rows) {
+        A v[E];
+        gather<S>(lds.part, at.row, at.c, v);
+        Pack<T, E> out;
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        A v = lds.part[at.row][0][at.c + i];
-#pragma unroll
-        for (int q = 1; q < S::SG; ++q) v += lds.part[at.row][q][at.c + i];
-        v = fma_(skip[i], up((T)old_x.v[i]), v);
-        if (a.z) {
-          A f, rest;
-          const A zi = up((T)old_z.v[i]);
-          gates<T>(zi, &f, &rest);
-          v *= zi * f;
+        for (int i = 0; i < E; ++i) {
+          v[i] = fma_(skip[i], up((T)x.v[i]), v[i]);
+          if (a.z) {
+            A f, rest;
+            const A zi = up((T)z.v[i]);
+            gates<T>(zi, &f, &rest);
+            v[i] *= zi * f;
+          }
+          out.v[i] = down<T>(v[i]);
         }
-        out.v[i] = down<T>(v);
+        at.store(y, out);
       }
-      store_pack<T, E>(y + (p.b * a.T + t + at.row) * a.D_ + from, out, at.n);
+      y += R * a.D_;
+    }
+  };
+  if (t0 < live) {
+    Inputs<T, S> even, odd;
+    request(even, t0);
+    request(odd, t0 + R);
+    for (int64_t t = t0; t < live; t += 2 * R) {
+      chunk(even, t);
+      if (t + R < live) chunk(odd, t + R);
     }
   }
   if (MAP) {
@@ -350,12 +464,12 @@ __global__ __launch_bounds__(64 * W) void scan_fwd(ScanArgs a, ScanGrid g, void*
     for (int i = 0; i < NS; ++i)
       if (i < l.count)
         static_cast<A*>(a.hT)[(p.b * a.D_ + d) * a.N + l.first + i] = h[i];
-  if (y && at.n > 0) {
+  if (a.y && at.stores) {
     Pack<T, E> zero;
 #pragma unroll
     for (int i = 0; i < E; ++i) zero.v[i] = T(0);
     for (int64_t t = (live > t0 ? live : t0) + at.row; t < t1; t += R)
-      store_pack<T, E>(y + (p.b * a.T + t) * a.D_ + from, zero, at.n);
+      at.store(static_cast<T*>(a.y) + (p.b * a.T + t) * a.D_ + p.d0, zero);
   }
 }
 
@@ -409,12 +523,12 @@ __device__ inline void sum_channels(A (&x)[V]) {
 template <class S>
 struct ReverseLds {
   typedef typename S::A A;
-  struct Four {
+  struct alignas(4 * sizeof(A)) Four {
     A s, sx, dy, pad;
   };
+  typename Coefficients<S>::Of bc[S::R][S::SG];
   Four in[S::R][kSlab];
-  A bc[S::R][2][S::NP];
-  A part[3][S::R][S::SG][kSlab];  // of u, of sum A q, of y before skip and gate
+  A part[3][S::R][S::W][kSlab];  // of u, of sum A q, of y before skip and gate
 };
 
 // The partial sums that leave a workgroup.
@@ -432,7 +546,7 @@ struct Sums {
 };
 
 // MAP: the segment's map of G alone.
-template <class T, int NS, int W, bool MAP>
+template <class T, int NS, int W, bool MAP, bool FULL>
 __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void* ws, void* sums_ws) {
   typedef ScanShape<T, NS, W> S;
   typedef Acc<T> A;
@@ -442,10 +556,9 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
   const int64_t row = p.b;  // of workgroups: in the reverse sweep they take several batch rows
   const int64_t span = g.seg_chunks * R, t0 = p.segment * span;
   const int64_t t1 = a.T - t0 < span ? a.T : t0 + span;
-  const Loader<S> at(p);
+  const Loader<S, FULL> at(p);
   const Lane l = lane_of<S>(a, p);
   const int64_t d = p.d0 + l.c;
-  const int64_t from = p.d0 + at.c;
   A rates[NS], dA[NS];
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
@@ -470,106 +583,119 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
                  ? static_cast<const A*>(a.dhT)[(p.b * a.D_ + d) * a.N + l.first + i] : A(0);
     if (!MAP && p.segment + 1 < active)
       through(maps, a, g, p.b, active - 1, p.segment, -1, l, d, rates, G);
-    Pack<T, E> x, delta, z, dy;
-    Coefficients<T, S> bc;
-    A before[NS];
-    const auto request = [&](int64_t t) {
-      const bool there = t + at.row < live;
-      delta = at.template load<T>(a.delta, p.b * a.sl_b + (t + at.row) * a.sl_t + from, there);
-      dy = at.template load<T>(a.dy, p.b * a.sd_b + (t + at.row) * a.sd_t + from, there);
-      if (a.z) z = at.template load<T>(a.z, p.b * a.sz_b + (t + at.row) * a.sz_t + from, there);
-      if (!MAP) {
-        x = at.template load<T>(a.x, p.b * a.sx_b + (t + at.row) * a.sx_t + from, there);
-        const A* const ck = static_cast<const A*>(a.ck) + (p.b * g.chunks + t / R) * a.N * a.D_;
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-          before[i] = i < l.count ? ck[(l.first + i) * a.D_ + d] : A(0);
-      }
-      bc.load(a, p, t, (int)(live - t < R ? live - t : R), !MAP);
-    };
     const int64_t last = live > t0 ? t0 + (live - t0 - 1) / R * R : t0 - R;
-    if (last >= t0) request(last);
-    for (int64_t t = last; t >= t0; t -= R) {
+    Walk<T> xs(a.x, p.b, a.sx_b, a.sx_t, t0, last, at.row, p.d0, -R);
+    Walk<T> deltas(a.delta, p.b, a.sl_b, a.sl_t, t0, last, at.row, p.d0, -R);
+    Walk<T> zs(a.z, p.b, a.sz_b, a.sz_t, t0, last, at.row, p.d0, -R);
+    Walk<T> dys(a.dy, p.b, a.sd_b, a.sd_t, t0, last, at.row, p.d0, -R);
+    CoefficientLoader<T, S> coefficients(a, p, t0, last, -R);
+    const A* const ck0 =
+        static_cast<const A*>(a.ck) + (p.b * g.chunks + t0 / R) * a.N * a.D_;
+    const A* ck = ck0 + (last - t0) / R * a.N * a.D_;
+    // a lane's states in a checkpoint; lanes without them read the first
+    const int64_t of_ck = l.count > 0 ? l.first * a.D_ + d : 0;
+    const auto request = [&](Inputs<T, S>& in, int64_t t) {
+      const bool there = t >= t0 && t + at.row < live;
+      in.delta = at.load(deltas.next(there));
+      in.dy = at.load(dys.next(there));
+      if (a.z) in.z = at.load(zs.next(there));
+      if (!MAP) {
+        in.x = at.load(xs.next(there));
+        const A* const from = t >= t0 ? ck : ck0;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) in.before[i] = from[of_ck + (i < l.count ? i * a.D_ : 0)];
+        ck -= a.N * a.D_;
+      }
+      in.request(coefficients, t >= t0 ? live - t : 0);
+    };
+    const auto chunk = [&](Inputs<T, S>& in, int64_t t) {
       const int rows = (int)(live - t < R ? live - t : R);
       A s_[E], x_[E], dy_[E], gate[E], of_gate[E], slope[E];
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        const A raw = up((T)delta.v[i]) + bias[i];
+        const A raw = up((T)in.delta.v[i]) + bias[i];
         s_[i] = a.softplus ? softplus(raw) : raw;
         slope[i] = A(1);
         if (!MAP && a.softplus) {
           A rest;
           gates<T>(raw, &slope[i], &rest);
         }
-        x_[i] = MAP ? A(0) : up((T)x.v[i]);
-        dy_[i] = up((T)dy.v[i]);
+        x_[i] = MAP ? A(0) : up((T)in.x.v[i]);
+        dy_[i] = up((T)in.dy.v[i]);
         gate[i] = A(1);
         of_gate[i] = A(0);
         if (a.z) {
           A f, rest;
-          const A zi = up((T)z.v[i]);
+          const A zi = up((T)in.z.v[i]);
           gates<T>(zi, &f, &rest);
           gate[i] = zi * f;
           of_gate[i] = f * fma_(zi, rest, A(1));
         }
-        if (threadIdx.x < S::kLoaders)
-          lds.in[at.row][at.c + i] = {s_[i], s_[i] * x_[i], dy_[i] * gate[i], A(0)};
+        if (S::kLoaders == S::NT || threadIdx.x < S::kLoaders) {
+          // channels that are not there add nothing to the sums over channels
+          const bool there = FULL || at.c + i <= at.last;
+          lds.in[at.row][at.c + i] = {there ? s_[i] : A(0), there ? s_[i] * x_[i] : A(0),
+                                      there ? dy_[i] * gate[i] : A(0), A(0)};
+        }
       }
-      bc.put(lds.bc);
+      in.put(coefficients, a.N, lds.bc);
       A h[NS];
 #pragma unroll
-      for (int i = 0; i < NS; ++i) h[i] = MAP ? A(0) : before[i];
+      for (int i = 0; i < NS; ++i) h[i] = !MAP && i < l.count ? in.before[i] : A(0);
       __syncthreads();
-      if (t > t0) request(t - R);
+      request(in, t - 2 * R);
       const auto sweep = [&](auto steps) {
         if constexpr (MAP) {
 #pragma unroll
           for (int r = R - 1; r >= 0; --r) {
             if (!steps.has(r)) continue;
-            const auto in = lds.in[r][l.c];
-            total += in.s;
+            const auto now = lds.in[r][l.c];
+            const auto bc = lds.bc[r][l.group];
+            total += now.s;
 #pragma unroll
             for (int i = 0; i < NS; ++i)
-              G[i] = decay(in.s, rates[i]) * fma_(lds.bc[r][1][l.first + i], in.dy, G[i]);
+              G[i] = decay(now.s, rates[i]) * fma_(bc.c[i], now.dy, G[i]);
           }
         } else {
-          A e[R][NS], old[R][NS], ofB[V], ofC[V];
+          A e[R][NS], old[R][NS], ofB[V], ofC[V], u[R], aq[R], yp[R];
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            if (!steps.has(r)) break;
-            const auto in = lds.in[r][l.c];
-            A sum = A(0);
+            yp[r] = A(0);
+            if (!steps.has(r)) continue;
+            const auto now = lds.in[r][l.c];
+            const auto bc = lds.bc[r][l.group];
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
-              e[r][i] = decay(in.s, rates[i]);
+              e[r][i] = decay(now.s, rates[i]);
               old[r][i] = h[i];
-              h[i] = fma_(e[r][i], h[i], in.sx * lds.bc[r][0][l.first + i]);
-              sum = fma_(lds.bc[r][1][l.first + i], h[i], sum);
+              h[i] = fma_(e[r][i], h[i], now.sx * bc.b[i]);
+              yp[r] = fma_(bc.c[i], h[i], yp[r]);
             }
-            if (a.z) lds.part[2][r][l.group][l.c] = sum;
           }
+          if (a.z) leave<S>(yp, lds.part[2]);
 #pragma unroll
           for (int r = R - 1; r >= 0; --r) {
+            u[r] = aq[r] = A(0);
 #pragma unroll
             for (int i = 0; i < NS; ++i) ofB[r * NS + i] = ofC[r * NS + i] = A(0);
             if (!steps.has(r)) continue;
-            const auto in = lds.in[r][l.c];
-            A u = A(0), aq = A(0);
+            const auto now = lds.in[r][l.c];
+            const auto bc = lds.bc[r][l.group];
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
-              G[i] = fma_(lds.bc[r][1][l.first + i], in.dy, G[i]);
-              ofC[r * NS + i] = in.dy * h[i];
-              ofB[r * NS + i] = G[i] * in.sx;
-              u = fma_(G[i], lds.bc[r][0][l.first + i], u);
+              G[i] = fma_(bc.c[i], now.dy, G[i]);
+              ofC[r * NS + i] = now.dy * h[i];
+              ofB[r * NS + i] = G[i] * now.sx;
+              u[r] = fma_(G[i], bc.b[i], u[r]);
               G[i] *= e[r][i];
               h[i] = old[r][i];
               const A q = G[i] * h[i];
-              dA[i] = fma_(in.s, q, dA[i]);
-              aq = fma_(rates[i], q, aq);
+              dA[i] = fma_(now.s, q, dA[i]);
+              aq[r] = fma_(rates[i], q, aq[r]);
             }
-            lds.part[0][r][l.group][l.c] = u;
-            lds.part[1][r][l.group][l.c] = aq;
           }
+          leave<S>(u, lds.part[0]);
+          leave<S>(aq, lds.part[1]);
           sum_channels(ofB);
           sum_channels(ofC);
           A* const to = sums.bc + ((((p.slab * a.B + p.b) * g.chunks + t / R) * S::SG + l.group) * 2)
@@ -585,29 +711,35 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
       if (rows == R) sweep(Steps<true, R>{R});
       else sweep(Steps<false, R>{rows});
       __syncthreads();
-      if (!MAP && t + at.row < live && at.n > 0) {
+      if (!MAP && at.row < rows && at.stores) {
+        A u[E], aq[E], yp[E];
+        gather<S>(lds.part[0], at.row, at.c, u);
+        gather<S>(lds.part[1], at.row, at.c, aq);
+        if (a.z) gather<S>(lds.part[2], at.row, at.c, yp);
         Pack<T, E> ox, od, oz;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          A u = A(0), aq = A(0), yp = A(0);
-#pragma unroll
-          for (int q = 0; q < S::SG; ++q) {
-            u += lds.part[0][at.row][q][at.c + i];
-            aq += lds.part[1][at.row][q][at.c + i];
-            if (a.z) yp += lds.part[2][at.row][q][at.c + i];
-          }
           const A through_gate = dy_[i] * gate[i];
-          const A of_raw = fma_(u, x_[i], of_rate(aq)) * slope[i];
-          ox.v[i] = down<T>(fma_(s_[i], u, skip[i] * through_gate));
+          const A of_raw = fma_(u[i], x_[i], of_rate(aq[i])) * slope[i];
+          ox.v[i] = down<T>(fma_(s_[i], u[i], skip[i] * through_gate));
           od.v[i] = down<T>(of_raw);
-          oz.v[i] = down<T>(dy_[i] * fma_(skip[i], x_[i], yp) * of_gate[i]);
+          if (a.z) oz.v[i] = down<T>(dy_[i] * fma_(skip[i], x_[i], yp[i]) * of_gate[i]);
           dD[i] = fma_(through_gate, x_[i], dD[i]);
           dbias[i] += of_raw;
         }
-        const int64_t to = (p.b * a.T + t + at.row) * a.D_ + from;
-        store_pack<T, E>(static_cast<T*>(a.out.dx) + to, ox, at.n);
-        store_pack<T, E>(static_cast<T*>(a.out.ddelta) + to, od, at.n);
-        if (a.z) store_pack<T, E>(static_cast<T*>(a.out.dz) + to, oz, at.n);
+        const int64_t to = (p.b * a.T + t + at.row) * a.D_ + p.d0;
+        at.store(static_cast<T*>(a.out.dx) + to, ox);
+        at.store(static_cast<T*>(a.out.ddelta) + to, od);
+        if (a.z) at.store(static_cast<T*>(a.out.dz) + to, oz);
+      }
+    };
+    if (last >= t0) {
+      Inputs<T, S> even, odd;
+      request(even, last);
+      request(odd, last - R);
+      for (int64_t t = last; t >= t0; t -= 2 * R) {
+        chunk(even, t);
+        if (t - R >= t0) chunk(odd, t - R);
       }
     }
     if (MAP) {
@@ -623,15 +755,15 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
       for (int i = 0; i < NS; ++i)
         if (i < l.count)
           static_cast<A*>(a.out.dh0)[(p.b * a.D_ + d) * a.N + l.first + i] = G[i];
-    if (at.n > 0) {
+    if (at.stores) {
       Pack<T, E> zero;
 #pragma unroll
       for (int i = 0; i < E; ++i) zero.v[i] = T(0);
       for (int64_t t = (live > t0 ? live : t0) + at.row; t < t1; t += R) {
-        const int64_t to = (p.b * a.T + t) * a.D_ + from;
-        store_pack<T, E>(static_cast<T*>(a.out.dx) + to, zero, at.n);
-        store_pack<T, E>(static_cast<T*>(a.out.ddelta) + to, zero, at.n);
-        if (a.z) store_pack<T, E>(static_cast<T*>(a.out.dz) + to, zero, at.n);
+        const int64_t to = (p.b * a.T + t) * a.D_ + p.d0;
+        at.store(static_cast<T*>(a.out.dx) + to, zero);
+        at.store(static_cast<T*>(a.out.ddelta) + to, zero);
+        if (a.z) at.store(static_cast<T*>(a.out.dz) + to, zero);
       }
     }
   }
@@ -767,16 +899,23 @@ hipError_t by_shape(const ScanGrid& g, F f) {
   return hipErrorInvalidValue;
 }
 
+// Every slab has all of its channels, and rows of B and C exist.
+inline bool full_slabs(const ScanArgs& a) { return a.D_ / a.G % kSlab == 0; }
+
 template <class T>
 hipError_t forward_of(const ScanArgs& a, const ScanGrid& g, void* ws, hipStream_t st) {
   return by_shape<T>(g, [&](auto shape) {
     typedef decltype(shape) S;
+    constexpr int N = S::NS, W = S::W;
     const dim3 groups((unsigned)(g.slabs * g.segments * a.B));
+    const bool full = full_slabs(a);
     if (g.segments > 1) {
-      const hipError_t e = start(scan_fwd<T, S::NS, S::W, true>, groups, S::NT, st, a, g, ws);
+      const hipError_t e = start(full ? scan_fwd<T, N, W, true, true> : scan_fwd<T, N, W, true, false>,
+                                 groups, S::NT, st, a, g, ws);
       if (e != hipSuccess) return e;
     }
-    return start(scan_fwd<T, S::NS, S::W, false>, groups, S::NT, st, a, g, ws);
+    return start(full ? scan_fwd<T, N, W, false, true> : scan_fwd<T, N, W, false, false>, groups,
+                 S::NT, st, a, g, ws);
   });
 }
 
@@ -785,13 +924,15 @@ hipError_t vjp_of(const ScanArgs& a, const ScanGrid& g, void* ws, hipStream_t st
   void* const sums = static_cast<char*>(ws) + g.map_bytes;
   return by_shape<T>(g, [&](auto shape) {
     typedef decltype(shape) S;
+    constexpr int N = S::NS, W = S::W;
+    const bool full = full_slabs(a);
     if (g.segments > 1) {
-      const hipError_t e = start(scan_rev<T, S::NS, S::W, true>,
+      const hipError_t e = start(full ? scan_rev<T, N, W, true, true> : scan_rev<T, N, W, true, false>,
                                  dim3((unsigned)(g.slabs * g.segments * a.B)), S::NT, st, a, g, ws,
                                  sums);
       if (e != hipSuccess) return e;
     }
-    hipError_t e = start(scan_rev<T, S::NS, S::W, false>,
+    hipError_t e = start(full ? scan_rev<T, N, W, false, true> : scan_rev<T, N, W, false, false>,
                          dim3((unsigned)(g.slabs * g.segments * g.rows)), S::NT, st, a, g, ws, sums);
     if (e != hipSuccess) return e;
     const int64_t bc = a.B * g.chunks * g.chunk * 2 * S::NP * a.G;

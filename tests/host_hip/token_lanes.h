@@ -20,3 +20,5 @@ inline Pair rows_swap(uint32_t a, uint32_t b, int row) {
 
 #undef __builtin_amdgcn_permlane16_swap
 #define __builtin_amdgcn_permlane16_swap(a, b, x, y) host_hip::rows_swap(a, b, 16)
+#undef __builtin_amdgcn_permlane32_swap
+#define __builtin_amdgcn_permlane32_swap(a, b, x, y) host_hip::rows_swap(a, b, 32)

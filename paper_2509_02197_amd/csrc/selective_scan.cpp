@@ -16,9 +16,15 @@ constexpr int64_t kEnoughWaves = 768, kWaves = 2048, kLeastSegment = 128;
 ScanGrid scan_grid(int32_t dtype, int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
   ScanGrid g{};
   const int acc = dtype == ADST_F64 ? 8 : 4;
-  g.states = N <= 16 ? 2 : N <= 64 ? 4 : 8;
-  g.waves = N <= 4 ? 1 : N <= 8 ? 2 : N <= 32 ? 4 : 8;
-  g.chunk = dtype == ADST_F64 || g.states == 8 ? 8 : 16;
+  const bool wide = dtype == ADST_F64;
+  if (wide) {
+    g.states = N <= 16 ? 2 : 4;
+    g.waves = N <= 8 ? 2 : N <= 32 ? 4 : 8;
+  } else {
+    g.states = N <= 4 ? 1 : N <= 16 ? 2 : N <= 32 ? 4 : N <= 64 ? 8 : 16;
+    g.waves = N <= 8 ? 2 : 4;
+  }
+  g.chunk = (wide ? 16 : 32) / (g.states < 2 ? 2 : g.states);
   g.slab = 32;
   g.chunks = up_to(T, g.chunk);
   g.group_slabs = up_to(D / G, g.slab);

@@ -44,7 +44,8 @@ template <class T, int NS_, int W_>
 struct ScanShape {
   typedef Acc<T> A;
   static constexpr int NS = NS_, W = W_;
-  static constexpr int R = sizeof(T) == 8 || NS == 8 ? 8 : 16;  // steps of a chunk
+  // Steps of a chunk: their states' registers are what the reverse sweep has most of.
+  static constexpr int R = (sizeof(T) == 8 ? 16 : 32) / (NS < 2 ? 2 : NS);
   static constexpr int NT = 64 * W;
   static constexpr int SG = 2 * W;             // lanes that share a channel
   static constexpr int NP = SG * NS;           // states, those that are not there included
@@ -461,7 +462,7 @@ __global__ __launch_bounds__(64 * W) void scan_fwd(ScanArgs a, ScanGrid g, void*
     }
     in.put(coefficients, a.N, of_parity(bc0, bc1, P));
   };
-  Ahead<S, false, Two<A>, 4> ahead;
+  Ahead<S, false, Two<A>, R < 4 ? R : 4> ahead;
   const auto sweep = [&](auto steps, auto parity) {
     constexpr int P = decltype(parity)::p;
     A sums[R];
@@ -1059,13 +1060,17 @@ __global__ __launch_bounds__(256) void scan_one(ScanStep q, int lanes) {
 // f(shape) for the shape that the grid names.
 template <class T, class F>
 hipError_t by_shape(const ScanGrid& g, F f) {
-  if (g.states == 2 && g.waves == 1) return f(ScanShape<T, 2, 1>());
-  if (g.states == 2 && g.waves == 2) return f(ScanShape<T, 2, 2>());
-  if (g.states == 2 && g.waves == 4) return f(ScanShape<T, 2, 4>());
-  if (g.states == 4 && g.waves == 4) return f(ScanShape<T, 4, 4>());
-  if (g.states == 4 && g.waves == 8) return f(ScanShape<T, 4, 8>());
-  if constexpr (sizeof(T) < 8)
-    if (g.states == 8 && g.waves == 8) return f(ScanShape<T, 8, 8>());
+  switch (g.states * 16 + g.waves) {
+    case 32 + 2: return f(ScanShape<T, 2, 2>());
+    case 32 + 4: return f(ScanShape<T, 2, 4>());
+    case 64 + 4: return f(ScanShape<T, 4, 4>());
+    case 64 + 8: return f(ScanShape<T, 4, 8>());
+  }
+  if constexpr (sizeof(T) < 8) {
+    if (g.states == 1 && g.waves == 2) return f(ScanShape<T, 1, 2>());
+    if (g.states == 8 && g.waves == 4) return f(ScanShape<T, 8, 4>());
+    if (g.states == 16 && g.waves == 4) return f(ScanShape<T, 16, 4>());
+  }
   return hipErrorInvalidValue;
 }
 

@@ -14,12 +14,39 @@ int64_t up_to(int64_t n, int64_t by) { return parts(n, by) * by; }
 // 256 MB cache between the products.
 constexpr int64_t kPieceBytes = 128 << 20;
 
-// Parts of the long axis of an m x n product whose tiles leave CUs without work.
-int64_t splits_of(int64_t m, int64_t n, int64_t steps) {
-  const int64_t tiles = parts(m, 128) * parts(n, 128);
-  int64_t s = tiles >= 192 ? 1 : 256 / tiles;
-  if (s > steps / 8) s = steps / 8;
-  return s < 1 ? 1 : s;
+// The tiles of an m x n product, and the parts of its long axis (of `steps` steps) where it
+// may be split: what takes the least time by the work of the CU that has the most
+// tiles. The rates are those of large products measured here (F32 128, F64 55 TFLOP/s, and
+// 1050 of 16-bit types with 256 x 256 tiles); smaller tiles read more of LDS for each
+// product, and a CU with less than two waves a SIMD waits for its loads (999 x 515 x 10007 F32:
+// forward 135 us with 128 x 128 tiles, 3 on the fullest CU, and 115 with 128 x 64).
+XentPlan::Product product_of(int64_t e, int64_t m, int64_t n, int64_t steps, bool split) {
+  static const struct {
+    int64_t bm, bn, waves;
+    double speed;
+  } tiles[] = {{256, 256, 8, 1.0}, {128, 128, 4, 0.85}, {128, 64, 4, 0.7}, {64, 64, 4, 0.5}};
+  if (m <= 64 && !split) return {3, 1};
+  const double flops_per_us = (e == 2 ? 1050e6 : e == 4 ? 128e6 : 55e6) / 256;  // of a CU
+  XentPlan::Product best{1, 1};
+  double least = -1;
+  for (int k = e == 8 ? 1 : 0; k < 4; ++k) {
+    const auto& t = tiles[k];
+    const int64_t count = parts(m, t.bm) * parts(n, t.bn);
+    // (the matrix cores, not LDS, bound the wider types)
+    const double speed = e == 2 ? t.speed : 1 - (1 - t.speed) / 3;
+    const double step = 2.0 * t.bm * t.bn * (128 / e) / flops_per_us / speed;
+    for (int64_t s = 1; s == 1 || (split && s <= 64 && s <= steps / 8); ++s) {
+      const int64_t of_cu = parts(count * s, 256);
+      double us = (double)(of_cu * parts(steps, s)) * step;
+      if (of_cu * t.waves < 8) us *= 1.3;
+      if (s > 1) us += 4 + 2.0 * (double)(s * m * n * (e == 8 ? 8 : 4)) / 5e6;
+      if (least < 0 || us < least) {
+        least = us;
+        best = {k, s};
+      }
+    }
+  }
+  return best;
 }
 
 }  // namespace
@@ -35,6 +62,7 @@ XentPlan xent_plan(int32_t dtype, int64_t M, int64_t V, int64_t K, bool reverse)
     at += (uint64_t)up_to(bytes, 256);
     return here;
   };
+  p.logits = product_of(e, M, V, parts(K, step), false);
   if (!reverse) {
     p.stats = take(parts(V, 64) * M * 2 * acc);
     p.target = take(M * acc);
@@ -46,16 +74,17 @@ XentPlan xent_plan(int32_t dtype, int64_t M, int64_t V, int64_t K, bool reverse)
   p.pieces = parts(V, most);
   p.piece = up_to(parts(V, p.pieces), p.pieces > 1 ? 256 : step);
   p.pieces = parts(V, p.piece);
-  p.dx_splits = splits_of(M, K, p.piece / step);
-  p.dw_splits = splits_of(p.piece, K, p.m_pad / step);
-  p.dx_direct = p.pieces == 1 && p.dx_splits == 1;
+  p.logits = product_of(e, M, p.piece, parts(K, step), false);
+  p.dx = product_of(e, M, K, p.piece / step, true);
+  p.dw = product_of(e, p.piece, K, p.m_pad / step, true);
+  p.dx_direct = p.pieces == 1 && p.dx.splits == 1;
   p.scale = take(2 * 4);
   p.xt = take(K * p.m_pad * e);
   p.wt = take(K * p.piece * e);
   p.g = take(M * p.piece * e);
   p.gt = take(p.piece * p.m_pad * e);
-  p.dx_sums = take(p.dx_direct ? 0 : p.dx_splits * M * K * acc);
-  p.dw_sums = take(p.dw_splits > 1 ? p.dw_splits * p.piece * K * acc : 0);
+  p.dx_sums = take(p.dx_direct ? 0 : p.dx.splits * M * K * acc);
+  p.dw_sums = take(p.dw.splits > 1 ? p.dw.splits * p.piece * K * acc : 0);
   p.bytes = at;
   return p;
 }

@@ -137,17 +137,33 @@ __global__ __launch_bounds__(kJoinThreads) void xent_join(const void* stats, con
                                                           int64_t V, int64_t columns, void* loss,
                                                           void* lse) {
   typedef Acc<T> A;
+  constexpr int kAhead = 8;  // statistics whose loads are in flight together
   const int64_t m = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) / W;
   const int lane = threadIdx.x % W;
-  const Stat<A>* const from = static_cast<const Stat<A>*>(stats);
   const int64_t row = m < M ? m : M - 1;
-  A top = -__builtin_inf();
-  for (int64_t k = lane; k < columns; k += W) top = larger(from[k * M + row].top, top);
+  const Stat<A>* const from = static_cast<const Stat<A>*>(stats) + row;
+  Stat<A> all = {A(-__builtin_inf()), A(0)};
+  for (int64_t k = lane; k < columns; k += W * kAhead) {
+    Stat<A> some[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t at = k + i * W;
+      some[i] = from[(at < columns ? at : k) * M];
+      if (at >= columns) some[i].sum = A(0);  // of one that was there already
+    }
+    A top = all.top;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) top = larger(some[i].top, top);
+    A sum = relative_to(pivot(top), all);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) sum += relative_to(pivot(top), some[i]);
+    all = {top, sum};
+  }
+  A top = all.top;
 #pragma unroll
   for (int by = 1; by < W; by <<= 1) top = larger(top, __shfl_xor(top, by, 64));
   const A at = pivot(top);
-  A sum = A(0);
-  for (int64_t k = lane; k < columns; k += W) sum += relative_to(at, from[k * M + row]);
+  A sum = relative_to(at, all);
 #pragma unroll
   for (int by = 1; by < W; by <<= 1) sum += __shfl_xor(sum, by, 64);
   if (m >= M || lane > 0) return;
@@ -200,22 +216,30 @@ template <class T, bool KEEP>
 __global__ __launch_bounds__(256) void xent_turn(Rows from, int64_t cols, int64_t pad, void* to,
                                                  const int32_t* labels, const void* dloss,
                                                  int64_t V) {
-  __shared__ T tile[kTurn][kTurn + 16 / sizeof(T) / 2];
+  constexpr int N = Vec<T>::N, kAcross = kTurn / N;  // vectors of 16 bytes across a tile
+  __shared__ __attribute__((aligned(16))) T tile[kTurn][kTurn + N];  // [column][row]
   const int64_t across = (cols + kTurn - 1) / kTurn;
   const int64_t r0 = blockIdx.x / across * kTurn, c0 = blockIdx.x % across * kTurn;
-  const int c = threadIdx.x % kTurn, first = threadIdx.x / kTurn;
-#pragma unroll 4
-  for (int r = first; r < kTurn; r += 256 / kTurn) {
-    const int64_t row = r0 + r;
-    bool there = row < from.n && c0 + c < cols;
+#pragma unroll
+  for (int k = threadIdx.x; k < kTurn * kAcross; k += 256) {
+    const int r = k / kAcross, c = k % kAcross * N;
+    const int64_t row = r0 + r, left = cols - c0 - c;
+    bool there = row < from.n && left > 0;
     if (KEEP && there) there = row_weight<Acc<T>>(labels, dloss, row, V) != Acc<T>(0);
-    tile[r][c] = there ? static_cast<const T*>(from.p)[row * from.stride + c0 + c] : T(0);
+    const T* const at = static_cast<const T*>(from.p) + row * from.stride + c0 + c;
+    const Vec<T> v = load_part(at, there ? (int)(left < N ? left : N) : 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) tile[c + i][r] = v.v[i];
   }
   __syncthreads();
-#pragma unroll 4
-  for (int r = first; r < kTurn; r += 256 / kTurn)
-    if (c0 + r < cols && r0 + c < pad)
-      static_cast<T*>(to)[(c0 + r) * pad + r0 + c] = tile[c][r];
+#pragma unroll
+  for (int k = threadIdx.x; k < kTurn * kAcross; k += 256) {
+    const int c = k / kAcross, r = k % kAcross * N;
+    // (pad is whole steps of 128 bytes, and so whole vectors)
+    if (c0 + c < cols && r0 + r < pad)
+      *reinterpret_cast<U4*>(static_cast<T*>(to) + (c0 + c) * pad + r0 + r) =
+          *reinterpret_cast<const U4*>(&tile[c][r]);
+  }
 }
 
 // g of a piece of the vocabulary, whose first word is v0: [rows][piece] and, transposed,
@@ -321,26 +345,20 @@ __global__ __launch_bounds__(256) void xent_sum(const void* sums, int64_t n, int
 }
 
 // ------------------------------------------------------------------ launches
-template <class T>
-using Large = GemmShape<T, 2, 4, 8, 4, 2>;   // 256 x 256
-template <class T>
-using Middle = GemmShape<T, 2, 2, 4, 4, 2>;  // 128 x 128
-template <class T>
-using Few = GemmShape<T, 1, 4, 4, 1, 4>;     // 64 x 64: few rows
-
 inline int64_t parts(int64_t n, int64_t by) { return (n + by - 1) / by; }
 template <class S>
 Tiles tiles_of(int64_t m, int64_t n, int64_t K, int64_t splits) {
   return {parts(m, S::BM), parts(n, S::BN), K, parts(K, S::kStep), splits};
 }
 
-// f(shape): the largest tiles that fill the card's 256 CUs, the smallest where rows are few.
+// f(shape) for the tiles that the plan names.
 template <class T, class F>
-hipError_t by_size(int64_t m, int64_t n, F f) {
+hipError_t by_tiles(int tiles, F f) {
   if constexpr (sizeof(T) < 8)
-    if (parts(m, 256) * parts(n, 256) >= 200) return f(Large<T>());
-  if (m <= 64) return f(Few<T>());
-  return f(Middle<T>());
+    if (tiles == 0) return f(GemmShape<T, 2, 4, 8, 4, 2>());  // 256 x 256
+  if (tiles == 1) return f(GemmShape<T, 2, 2, 4, 4, 2>());    // 128 x 128
+  if (tiles == 2) return f(GemmShape<T, 2, 2, 4, 2, 2>());    // 128 x 64
+  return f(GemmShape<T, 1, 4, 4, 1, 4>());  // 64 x 64, three steps ahead: bound by loads
 }
 
 template <class T>
@@ -354,7 +372,7 @@ hipError_t forward_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_
   char* const at = static_cast<char*>(ws);
   const bool direct = whole_pieces<T>(a.x, a.sx, a.K) && whole_pieces<T>(a.w, a.sw, a.K);
   const Rows x{a.x, a.sx, a.M}, w{a.w, a.sw, a.V};
-  return by_size<T>(a.M, a.V, [&](auto shape) {
+  return by_tiles<T>(p.logits.tiles, [&](auto shape) {
     typedef decltype(shape) S;
     const Tiles t = tiles_of<S>(a.M, a.V, a.K, 1);
     hipError_t e = start(direct ? xent_stats<S, true> : xent_stats<S, false>,
@@ -365,7 +383,7 @@ hipError_t forward_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_
     if (a.M < 2048)
       return start(xent_join<T, 64>, dim3((unsigned)parts(a.M * 64, kJoinThreads)), kJoinThreads,
                    st, stats, target, a.labels, a.M, a.V, t.n, a.loss, a.lse);
-    return start(xent_join<T, 4>, dim3((unsigned)parts(a.M * 4, kJoinThreads)), kJoinThreads, st,
+    return start(xent_join<T, 8>, dim3((unsigned)parts(a.M * 8, kJoinThreads)), kJoinThreads, st,
                  stats, target, a.labels, a.M, a.V, t.n, a.loss, a.lse);
   });
 }
@@ -397,7 +415,7 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
     const bool direct = whole_pieces<T>(x.p, x.stride, a.K) && whole_pieces<T>(w.p, w.stride, a.K);
     const GArgs q{a.labels, a.lse, a.dloss, scale, v0, a.V, p.piece, p.m_pad, at + p.g, at + p.gt};
     // the products' long axes: this piece's words, and the rows, in whole steps
-    e = by_size<T>(a.M, words, [&](auto shape) {
+    e = by_tiles<T>(p.logits.tiles, [&](auto shape) {
       typedef decltype(shape) S;
       Tiles t = tiles_of<S>(p.m_pad, p.piece, a.K, 1);
       return start(direct ? xent_grad<S, true> : xent_grad<S, false>, dim3((unsigned)(t.m * t.n)),
@@ -407,17 +425,17 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
     if (a.dw) {
       const Rows gt{at + p.gt, p.m_pad, words}, xt{at + p.xt, p.m_pad, a.K};
       T* const out = static_cast<T*>(a.dw) + v0 * a.K;
-      const bool split = p.dw_splits > 1;
-      e = by_size<T>(words, a.K, [&](auto shape) {
+      const bool split = p.dw.splits > 1;
+      e = by_tiles<T>(p.dw.tiles, [&](auto shape) {
         typedef decltype(shape) S;
-        const Tiles t = tiles_of<S>(words, a.K, p.m_pad, p.dw_splits);
+        const Tiles t = tiles_of<S>(words, a.K, p.m_pad, p.dw.splits);
         return start(xent_product<S>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, gt,
                      xt, t, OutArgs{split ? nullptr : out, at + p.dw_sums, scale, false});
       });
       if (e != hipSuccess) return e;
       if (split) {
         e = start(xent_sum<T>, dim3((unsigned)parts(words * a.K, 256)), 256, st, at + p.dw_sums,
-                  words * a.K, p.dw_splits, scale, out);
+                  words * a.K, p.dw.splits, scale, out);
         if (e != hipSuccess) return e;
       }
     }
@@ -427,9 +445,9 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
                 p.piece, at + p.wt, a.labels, a.dloss, a.V);
       if (e != hipSuccess) return e;
       const Rows g{at + p.g, p.piece, a.M}, wt{at + p.wt, p.piece, a.K};
-      e = by_size<T>(a.M, a.K, [&](auto shape) {
+      e = by_tiles<T>(p.dx.tiles, [&](auto shape) {
         typedef decltype(shape) S;
-        const Tiles t = tiles_of<S>(a.M, a.K, p.piece, p.dx_splits);
+        const Tiles t = tiles_of<S>(a.M, a.K, p.piece, p.dx.splits);
         return start(xent_product<S>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, g,
                      wt, t, OutArgs{p.dx_direct ? a.dx : nullptr, at + p.dx_sums, scale, v0 > 0});
       });
@@ -438,7 +456,7 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
   }
   if (a.dx && !p.dx_direct)
     return start(xent_sum<T>, dim3((unsigned)parts(a.M * a.K, 256)), 256, st, at + p.dx_sums,
-                 a.M * a.K, p.dx_splits, scale, a.dx);
+                 a.M * a.K, p.dx.splits, scale, a.dx);
   return hipSuccess;
 }
 

@@ -1060,13 +1060,12 @@ __global__ __launch_bounds__(256) void scan_one(ScanStep q, int lanes) {
 // f(shape) for the shape that the grid names.
 template <class T, class F>
 hipError_t by_shape(const ScanGrid& g, F f) {
-  switch (g.states * 16 + g.waves) {
-    case 32 + 2: return f(ScanShape<T, 2, 2>());
-    case 32 + 4: return f(ScanShape<T, 2, 4>());
-    case 64 + 4: return f(ScanShape<T, 4, 4>());
-    case 64 + 8: return f(ScanShape<T, 4, 8>());
-  }
-  if constexpr (sizeof(T) < 8) {
+  if (g.states == 2 && g.waves == 2) return f(ScanShape<T, 2, 2>());
+  if (g.states == 2 && g.waves == 4) return f(ScanShape<T, 2, 4>());
+  if (g.states == 4 && g.waves == 4) return f(ScanShape<T, 4, 4>());
+  if constexpr (sizeof(T) == 8) {
+    if (g.states == 4 && g.waves == 8) return f(ScanShape<T, 4, 8>());
+  } else {
     if (g.states == 1 && g.waves == 2) return f(ScanShape<T, 1, 2>());
     if (g.states == 8 && g.waves == 4) return f(ScanShape<T, 8, 4>());
     if (g.states == 16 && g.waves == 4) return f(ScanShape<T, 16, 4>());

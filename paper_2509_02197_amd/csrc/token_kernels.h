@@ -134,7 +134,11 @@ struct XentArgs {
 struct XentPlan {
   int64_t piece, pieces;   // of the vocabulary: columns (padded) and their number
   int64_t m_pad;           // rows, padded
-  int64_t dx_splits, dw_splits;  // parts of the long axis that are summed afterwards
+  // each product's tiles, and the parts of its long axis that are summed afterwards
+  struct Product {
+    int tiles;  // 0: 256 x 256, 1: 128 x 128, 2: 128 x 64, 3: 64 x 64 for few rows
+    int64_t splits;
+  } logits, dx, dw;
   bool dx_direct;          // dx leaves its product in the element type
   uint64_t stats, target, scale, xt, wt, g, gt, dx_sums, dw_sums;
   uint64_t bytes;

@@ -22,7 +22,7 @@ typedef float F4 __attribute__((ext_vector_type(4)));
 typedef double D4 __attribute__((ext_vector_type(4)));
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
 
-// 16 x 16 of C from 16 rows' pieces of 16 bytes. at(lane, i): the row of a lane's
+// 16 x 16 of C from 16 rows' pieces of 16 bytes, in kParts instructions. at(lane, i): the row of a lane's
 // value i; its column is lane % 16.
 template <class T>
 struct Tile;
@@ -30,7 +30,8 @@ template <>
 struct Tile<bf16> {
   typedef F4 C;
   typedef bf16 V __attribute__((ext_vector_type(8)));
-  __device__ static C mul(U4 a, U4 b, C c) {
+  static constexpr int kParts = 1;
+  __device__ static C mul(U4 a, U4 b, C c, int) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a),
                                                    __builtin_bit_cast(V, b), c, 0, 0, 0);
   }
@@ -40,7 +41,8 @@ template <>
 struct Tile<f16> {
   typedef F4 C;
   typedef f16 V __attribute__((ext_vector_type(8)));
-  __device__ static C mul(U4 a, U4 b, C c) {
+  static constexpr int kParts = 1;
+  __device__ static C mul(U4 a, U4 b, C c, int) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a),
                                                   __builtin_bit_cast(V, b), c, 0, 0, 0);
   }
@@ -49,11 +51,10 @@ struct Tile<f16> {
 template <>
 struct Tile<float> {
   typedef F4 C;
-  __device__ static C mul(U4 a, U4 b, C c) {
+  static constexpr int kParts = 4;
+  __device__ static C mul(U4 a, U4 b, C c, int part) {
     const F4 x = __builtin_bit_cast(F4, a), y = __builtin_bit_cast(F4, b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
-    return c;
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(x[part], y[part], c, 0, 0, 0);
   }
   __device__ static int at(int lane, int i) { return lane / 16 * 4 + i; }
 };
@@ -61,11 +62,10 @@ template <>
 struct Tile<double> {
   typedef D4 C;
   typedef double V __attribute__((ext_vector_type(2)));
-  __device__ static C mul(U4 a, U4 b, C c) {
+  static constexpr int kParts = 2;
+  __device__ static C mul(U4 a, U4 b, C c, int part) {
     const V x = __builtin_bit_cast(V, a), y = __builtin_bit_cast(V, b);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) c = __builtin_amdgcn_mfma_f64_16x16x4f64(x[i], y[i], c, 0, 0, 0);
-    return c;
+    return __builtin_amdgcn_mfma_f64_16x16x4f64(x[part], y[part], c, 0, 0, 0);
   }
   __device__ static int at(int lane, int i) { return i * 4 + lane / 16; }
 };
@@ -158,10 +158,13 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
 #pragma unroll
       for (int i = 0; i < S::MT; ++i)
         a[i] = *reinterpret_cast<const U4*>(stage + read[h] + (wm * S::MT + i) * 16 * kStepBytes);
+      // (an instruction's result is ready some instructions later: no two in a row share one)
 #pragma unroll
-      for (int i = 0; i < S::MT; ++i)
+      for (int part = 0; part < C::kParts; ++part)
 #pragma unroll
-        for (int j = 0; j < S::NT; ++j) s.acc[i][j] = C::mul(a[i], b[j], s.acc[i][j]);
+        for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+          for (int j = 0; j < S::NT; ++j) s.acc[i][j] = C::mul(a[i], b[j], s.acc[i][j], part);
     }
   };
   if constexpr (DIRECT) {

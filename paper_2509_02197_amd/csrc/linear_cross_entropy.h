@@ -90,20 +90,25 @@ __global__ __launch_bounds__(S::kThreads) void xent_stats(Rows x, Rows w, Tiles 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
   Stat<A>(*const part)[S::WN] = reinterpret_cast<Stat<A>(*)[S::WN]>(lds);  // [row of the tile]
+  int* const label_of = reinterpret_cast<int*>(part + S::BM);  // a column of the tile, or -1
+  for (int row = threadIdx.x; row < S::BM; row += S::kThreads) {
+    const int64_t at = m0 + row < x.n ? labels[m0 + row] - n0 : -1;
+    label_of[row] = at >= 0 && at < S::BN && n0 + at < w.n ? (int)at : -1;
+  }
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < S::MT; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = (wm * S::MT + i) * 16 + C::at(lane, r);
-      const int64_t m = m0 + row;
-      const int64_t label = m < x.n ? labels[m] : -1;
+      const int label = label_of[row];
       A top = -__builtin_inf();
 #pragma unroll
       for (int j = 0; j < S::NT; ++j) {
-        const int64_t n = n0 + (wn * S::NT + j) * 16 + col;
+        const int n = (wn * S::NT + j) * 16 + col;
         const A v = s.acc[i][j][r];
-        if (n == label) static_cast<A*>(target)[m] = v;
-        if (n < w.n) top = larger(v, top);
+        if (n == label) static_cast<A*>(target)[m0 + row] = v;
+        if (n0 + n < w.n) top = larger(v, top);
       }
       top = row_top(top);
       const A from = pivot(top);
@@ -266,26 +271,59 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad(Rows x, Rows w, Tiles t
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
   const A scale = q.scale ? (A)q.scale[0] : A(1);
+  struct Row {
+    A lse, weight;
+    int label, pad;
+  };
+  Row* const row_of = reinterpret_cast<Row*>(lds);
+  for (int row = threadIdx.x; row < S::BM; row += S::kThreads) {
+    const int64_t m = m0 + row;
+    Row one = {A(0), A(0), -1, 0};
+    if (m < x.n) {
+      const int64_t at = q.labels[m] - q.v0 - n0;
+      one.weight = row_weight<A>(q.labels, q.dloss, m, q.V) * scale;
+      one.lse = static_cast<const A*>(q.lse)[m];
+      one.label = at >= 0 && at < S::BN ? (int)at : -1;
+    }
+    row_of[row] = one;
+  }
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < S::MT; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t m = m0 + (wm * S::MT + i) * 16 + C::at(lane, r);
-      const bool row = m < x.n;
-      const A weight = row ? row_weight<A>(q.labels, q.dloss, m, q.V) : A(0);
-      const A lse = row ? static_cast<const A*>(q.lse)[m] : A(0);
-      const int64_t label = row ? q.labels[m] - q.v0 : -1;
+      const Row row = row_of[(wm * S::MT + i) * 16 + C::at(lane, r)];
 #pragma unroll
       for (int j = 0; j < S::NT; ++j) {
-        const int64_t n = n0 + (wn * S::NT + j) * 16 + col;
+        const int n = (wn * S::NT + j) * 16 + col;
         A v = A(0);
-        if (weight != A(0) && n < w.n)
-          v = (exp_(s.acc[i][j][r] - lse) - (n == label ? A(1) : A(0))) * (weight * scale);
-        const T out = down<T>(v);
-        if (row && n < q.piece) static_cast<T*>(q.g)[m * q.piece + n] = out;
-        if (m < q.m_pad && n < q.piece) static_cast<T*>(q.gt)[n * q.m_pad + m] = out;
+        if (row.weight != A(0) && n0 + n < w.n)
+          v = (exp_(s.acc[i][j][r] - row.lse) - (n == row.label ? A(1) : A(0))) * row.weight;
+        s.acc[i][j][r] = v;
       }
     }
+  // transposed: a lane has four neighbouring rows of a column (every fourth, for F64)
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+      const int64_t n = n0 + (wn * S::NT + j) * 16 + col, m = m0 + (wm * S::MT + i) * 16;
+      if (m >= q.m_pad || n >= q.piece) continue;  // (both are multiples of 16)
+      T* const to = static_cast<T*>(q.gt) + n * q.m_pad + m;
+      if constexpr (sizeof(T) == 8) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[C::at(lane, r)] = down<T>(s.acc[i][j][r]);
+      } else {
+        typedef T Four __attribute__((ext_vector_type(4)));
+        Four v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = down<T>(s.acc[i][j][r]);
+        *reinterpret_cast<Four*>(to + C::at(lane, 0)) = v;
+      }
+    }
+  __syncthreads();
+  store_tile<S>(lds, static_cast<T*>(q.g) + m0 * q.piece + n0, q.piece, x.n - m0, q.piece - n0,
+                [&](int i, int r, int j) { return down<T>(s.acc[i][j][r]); });
 }
 
 // C [rows][n] from a product of whole steps: rounded to `out`, or added to (`add`: after
@@ -310,25 +348,33 @@ __global__ __launch_bounds__(S::kThreads) void xent_product(Rows a, Rows b, Tile
                     t.steps * (split + 1) / t.splits);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
-  const A back = q.out && q.scale ? (A)q.scale[1] : A(1);
+  if (q.out) {
+    const A back = q.scale ? (A)q.scale[1] : A(1);
+    store_tile<S>(lds, static_cast<T*>(q.out) + m0 * b.n + n0, b.n, a.n - m0, b.n - n0,
+                  [&](int i, int r, int j) { return down<T>(s.acc[i][j][r] * back); });
+    return;
+  }
+  A* const to = static_cast<A*>(q.sums) + (split * a.n + m0) * b.n + n0;
+  const int64_t rows = a.n - m0, columns = b.n - n0;
 #pragma unroll
-  for (int i = 0; i < S::MT; ++i)
+  for (int i = 0; i < S::MT; ++i) {
+    A old[4][S::NT];  // the loads of a row of tiles are in flight together
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t m = m0 + (wm * S::MT + i) * 16 + C::at(lane, r);
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int j = 0; j < S::NT; ++j) {
-        const int64_t n = n0 + (wn * S::NT + j) * 16 + col;
-        if (m >= a.n || n >= b.n) continue;
-        const A v = s.acc[i][j][r];
-        if (q.out) {
-          static_cast<T*>(q.out)[m * b.n + n] = down<T>(v * back);
-        } else {
-          A* const to = static_cast<A*>(q.sums) + (split * a.n + m) * b.n + n;
-          *to = q.add ? *to + v : v;
-        }
+        const int m = (wm * S::MT + i) * 16 + C::at(lane, r), n = (wn * S::NT + j) * 16 + col;
+        const bool there = m < rows && n < columns;
+        old[r][j] = q.add && there ? to[m * b.n + n] : A(0);
       }
-    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        const int m = (wm * S::MT + i) * 16 + C::at(lane, r), n = (wn * S::NT + j) * 16 + col;
+        if (m < rows && n < columns) to[m * b.n + n] = old[r][j] + s.acc[i][j][r];
+      }
+  }
 }
 
 // out = the splits' sums added in order, rounded.
@@ -364,7 +410,7 @@ hipError_t by_tiles(int tiles, F f) {
 template <class T>
 bool whole_pieces(const void* p, int64_t stride, int64_t K) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (int64_t)sizeof(T) % 16 == 0 &&
-         K * (int64_t)sizeof(T) % kStepBytes == 0;
+         K * (int64_t)sizeof(T) % kStepBytes == 0 && stride < (int64_t(1) << 28);
 }
 
 template <class T>

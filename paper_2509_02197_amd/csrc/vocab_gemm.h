@@ -3,13 +3,12 @@
 // tile of C before it leaves the registers (linear_cross_entropy.h).
 //
 // A workgroup computes BM x BN of C in steps of 128 bytes of k. A step's rows go
-// to LDS by loads that write it directly, 16 bytes a lane, one step ahead (ST - 1
-// steps); in LDS a row's eight pieces of 16 bytes are permuted by the row's number, so
-// that the reads of eight neighbouring rows fall into different banks. A wave's
-// lane reads 16 bytes of a row of A and of B for each matrix instruction (four for
-// F32, two for F64): lanes 16 q .. 16 q + 15 hold piece q of rows 0..15. The sum
-// over k does not ask in which order the pieces' elements are taken as long as A
-// and B agree.
+// to LDS by loads that write it directly, 16 bytes a lane, ST - 1 steps ahead; in LDS
+// a row's eight pieces of 16 bytes are permuted by the row's number, so that the reads
+// of eight neighbouring rows fall into different banks. A wave's lane reads 16 bytes of
+// a row of A and of B for each matrix instruction (four for F32, two for F64): lanes
+// 16 q .. 16 q + 15 hold piece q of rows 0..15. The sum over k does not ask in which
+// order the pieces' elements are taken as long as A and B agree.
 #pragma once
 
 #include "seq_common.h"
@@ -113,8 +112,24 @@ __device__ inline uint32_t lds_at(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
+// Of a lane's row from the first of eight, in bytes.
+template <bool DIRECT>
+struct Offset {
+  typedef int64_t type;
+};
+template <>
+struct Offset<true> {
+  typedef uint32_t type;
+};
+
+template <int N>
+struct Behind {
+  static constexpr int n = N;
+};
+
 // Steps first .. end of k into s.acc, for the tile whose first rows of A and B are m0, n0.
-// DIRECT: k is whole steps, rows and their starts are multiples of 16 bytes.
+// DIRECT: k is whole steps, rows and their starts are multiples of 16 bytes. Eight rows span
+// less than 2^32 bytes.
 template <class S, bool DIRECT>
 __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, int64_t K,
                                 int64_t m0, int64_t n0, int64_t first, int64_t end) {
@@ -130,71 +145,92 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
   if (first >= end) return;
 
   // A load of a wave fills 8 rows of a step: lane l row l / 8, piece l % 8 of LDS, which
-  // holds the row's piece (l % 8) ^ (l / 8).
+  // holds the row's piece (l % 8) ^ (l / 8). Rows beyond the matrix are read as its last
+  // one, and their results are not used.
+  constexpr int kWaves = S::kThreads / 64;
+  static_assert(S::BM % (kWaves * 8) == 0, "a load is of A or of B");
   const int row8 = lane >> 3, piece = (lane & 7) ^ row8;
-  const T* from[S::kLoads];
+  const char* from[S::kLoads];  // the first of the 8 rows, at step `first`
+  typename Offset<DIRECT>::type offset[S::kLoads];
 #pragma unroll
   for (int j = 0; j < S::kLoads; ++j) {
-    const int r = (j * (S::kThreads / 64) + wave) * 8 + row8;
-    const bool of_a = r < S::BM;
+    const bool of_a = j < S::BM / (kWaves * 8);
     const Rows& X = of_a ? A : B;
-    const int64_t want = of_a ? m0 + r : n0 + r - S::BM;
-    const int64_t row = want < X.n ? want : X.n - 1;  // beyond: any row, its results are not used
-    from[j] = static_cast<const T*>(X.p) + row * X.stride + piece * (16 / (int)sizeof(T));
+    const int64_t r0 = (of_a ? m0 : n0 - S::BM) + (j * kWaves + wave) * 8;
+    const int64_t row = r0 < X.n ? r0 : X.n - 1, left = X.n - 1 - row;
+    const int down_to = row8 < left ? row8 : (int)left;
+    from[j] = static_cast<const char*>(X.p) +
+              (row * X.stride + first * S::kStep) * (int64_t)sizeof(T);
+    offset[j] = (typename Offset<DIRECT>::type)(down_to * X.stride * (int64_t)sizeof(T) + piece * 16);
   }
   // What a lane reads: its row of 16 and, for each half of a step, the piece lane / 16.
-  uint32_t read[2];
+  uint32_t at[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h)
-    read[h] = (lane & 15) * kStepBytes + (((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
-  const auto compute = [&](const char* stage) {
+    at[h] = (lane & 15) * kStepBytes + (((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
+  U4 a[2][S::MT], b[2][S::NT];
+  const auto read = [&](const char* stage, int h) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      U4 a[S::MT], b[S::NT];
+    for (int j = 0; j < S::NT; ++j)
+      b[h][j] = *reinterpret_cast<const U4*>(stage + at[h] +
+                                             (S::BM + (wn * S::NT + j) * 16) * kStepBytes);
 #pragma unroll
-      for (int j = 0; j < S::NT; ++j)
-        b[j] = *reinterpret_cast<const U4*>(stage + read[h] +
-                                            (S::BM + (wn * S::NT + j) * 16) * kStepBytes);
+    for (int i = 0; i < S::MT; ++i)
+      a[h][i] = *reinterpret_cast<const U4*>(stage + at[h] + (wm * S::MT + i) * 16 * kStepBytes);
+  };
+  const auto compute = [&](int h) {
+    // (an instruction's result is ready some instructions later: no two in a row share one)
+#pragma unroll
+    for (int part = 0; part < C::kParts; ++part)
 #pragma unroll
       for (int i = 0; i < S::MT; ++i)
-        a[i] = *reinterpret_cast<const U4*>(stage + read[h] + (wm * S::MT + i) * 16 * kStepBytes);
-      // (an instruction's result is ready some instructions later: no two in a row share one)
 #pragma unroll
-      for (int part = 0; part < C::kParts; ++part)
-#pragma unroll
-        for (int i = 0; i < S::MT; ++i)
-#pragma unroll
-          for (int j = 0; j < S::NT; ++j) s.acc[i][j] = C::mul(a[i], b[j], s.acc[i][j], part);
-    }
+        for (int j = 0; j < S::NT; ++j) s.acc[i][j] = C::mul(a[h][i], b[h][j], s.acc[i][j], part);
   };
   if constexpr (DIRECT) {
+    // While a half of a step is multiplied the next half is read from LDS, across the
+    // barrier between steps too. (Read where they are used: 8192 x 8192 x 2048 bf16 254 us.)
     const uint32_t base = lds_at(lds);
-    const auto request = [&](int64_t k, int stage) {
+    const auto request = [&](int stage) {
 #pragma unroll
       for (int j = 0; j < S::kLoads; ++j) {
-        const uint32_t to = base + stage * S::kStageBytes + (j * (S::kThreads / 64) + wave) * 1024;
-        const T* const at = from[j] + k * S::kStep;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                     : : "s"(to), "v"(at) : "memory");
+        const uint32_t to = base + stage * S::kStageBytes + (j * kWaves + wave) * 1024;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     : : "s"(to), "v"(offset[j]), "s"(from[j]) : "memory");
+        from[j] += kStepBytes;
       }
     };
-    constexpr int kAhead = S::ST - 1;
-    for (int k = 0; k < kAhead; ++k)
-      if (first + k < end) request(first + k, k);
-    int stage = 0;
-    for (int64_t k = first; k < end; ++k) {
-      // the step's loads are done when no more than those of the steps behind it are under
-      // way; and this wave has read all of the step before, whose place is filled next
-      if (k + kAhead - 1 < end && kAhead > 1)
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((kAhead - 1) * S::kLoads) : "memory");
+    // A step is in LDS when no more loads than those of the `behind` steps after it are under
+    // way; and this wave has read all that it has asked LDS for.
+    const auto arrived = [&](bool behind, auto steps) {
+      if (behind)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(decltype(steps)::n * S::kLoads)
+                     : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" : : : "memory");
-      const int free_stage = stage == 0 ? S::ST - 1 : stage - 1;
-      if (k + kAhead < end) request(k + kAhead, free_stage);
-      compute(lds + stage * S::kStageBytes);
-      stage = stage + 1 == S::ST ? 0 : stage + 1;
+    };
+#pragma unroll
+    for (int k = 0; k < S::ST; ++k)
+      if (first + k < end) request(k);
+    arrived(first + S::ST <= end, Behind<S::ST - 1>());
+    read(lds, 0);
+    int stage = 0;
+    for (int64_t k = first; k < end; ++k) {
+      read(lds + stage * S::kStageBytes, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(0);
+      __builtin_amdgcn_sched_barrier(0);
+      const int next = stage + 1 == S::ST ? 0 : stage + 1;
+      if (k + 1 < end) {
+        arrived(k + S::ST <= end, Behind<S::ST - 2>());
+        if (k + S::ST < end) request(stage);  // every wave has read the step
+        read(lds + next * S::kStageBytes, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      compute(1);
+      stage = next;
     }
   } else {
     Vec<T> hold[S::kLoads];
@@ -202,14 +238,15 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
 #pragma unroll
       for (int j = 0; j < S::kLoads; ++j) {
         const int64_t left = K - k * S::kStep - piece * Vec<T>::N;
-        hold[j] = load_part(from[j] + k * S::kStep,
+        hold[j] = load_part(reinterpret_cast<const T*>(from[j] + offset[j]),
                             (int)(left < 0 ? 0 : left < Vec<T>::N ? left : Vec<T>::N));
+        from[j] += kStepBytes;
       }
     };
     const auto put = [&](char* stage) {
 #pragma unroll
       for (int j = 0; j < S::kLoads; ++j)
-        *reinterpret_cast<U4*>(stage + (j * (S::kThreads / 64) + wave) * 1024 + lane * 16) =
+        *reinterpret_cast<U4*>(stage + (j * kWaves + wave) * 1024 + lane * 16) =
             __builtin_bit_cast(U4, hold[j].v);
     };
     request(first);
@@ -218,11 +255,62 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
       const int stage = (int)((k - first) & 1);
       __syncthreads();
       if (k + 1 < end) request(k + 1);
-      compute(lds + stage * S::kStageBytes);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        read(lds + stage * S::kStageBytes, h);
+        compute(h);
+      }
       if (k + 1 < end) put(lds + (stage ^ 1) * S::kStageBytes);
     }
   }
   __syncthreads();  // LDS is free
+}
+
+// f(tile row i, value r, tile column j) of a wave's tiles as rows of T in global memory, through
+// LDS: to [row][column] from the workgroup's tile on, `rows` x `columns` of which exist, in whole
+// vectors where the rows allow it. All of the workgroup's threads.
+template <class S, class F>
+__device__ inline void store_tile(char* lds, typename S::T* to, int64_t stride, int64_t rows,
+                                  int64_t columns, F f) {
+  typedef typename S::T T;
+  typedef Tile<T> C;
+  constexpr int kAll = S::BM * S::BN * (int)sizeof(T), kHave = S::ST * S::kStageBytes;
+  constexpr int P = (kAll + kHave - 1) / kHave;  // parts of a wave's rows of tiles
+  static_assert(S::MT % P == 0, "");
+  constexpr int M = S::MT / P, N = Vec<T>::N, kPieces = S::BN / N;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / S::WN, wn = wave % S::WN;
+  // a row's pieces of 16 bytes are permuted by the number of its row of four
+  const auto place = [](int row, int piece) {
+    return (row * kPieces + (piece ^ (row / 4 % 4 * 2 % kPieces))) * 16;
+  };
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    if (p > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = (wm * M + i) * 16 + C::at(lane, r);
+          const int column = (wn * S::NT + j) * 16 + (lane & 15);
+          *reinterpret_cast<T*>(lds + place(row, column / N) + column % N * (int)sizeof(T)) =
+              f(p * M + i, r, j);
+        }
+    __syncthreads();
+    for (int k = threadIdx.x; k < S::BM / P * kPieces; k += S::kThreads) {
+      const int row = k / kPieces, piece = k % kPieces;
+      // the tile's row that this row of the part is
+      const int of = row / (M * 16) * S::MT * 16 + p * M * 16 + row % (M * 16);
+      const int64_t left = columns - piece * N;
+      if (of >= rows || left <= 0) continue;
+      Vec<T> v;
+      v.v = __builtin_bit_cast(typename Vec<T>::type,
+                               *reinterpret_cast<const U4*>(lds + place(row, piece)));
+      store_part(to + of * stride + piece * N, v, (int)(left < N ? left : N));
+    }
+  }
 }
 
 }  // namespace

@@ -4,8 +4,8 @@
 //
 // A workgroup computes BM x BN of C in steps of 128 bytes of k. A step's rows go
 // to LDS by loads that write it directly, 16 bytes a lane, ST - 1 steps ahead; in LDS
-// a row's eight pieces of 16 bytes are permuted by the row's number, so that the reads
-// of eight neighbouring rows fall into different banks. A wave's lane reads 16 bytes of
+// a row's eight pieces of 16 bytes are permuted by half the row's number, so that the
+// reads of 16 neighbouring rows fall into all 64 banks. A wave's lane reads 16 bytes of
 // a row of A and of B for each matrix instruction (four for F32, two for F64): lanes
 // 16 q .. 16 q + 15 hold piece q of rows 0..15. The sum over k does not ask in which
 // order the pieces' elements are taken as long as A and B agree.
@@ -145,11 +145,11 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
   if (first >= end) return;
 
   // A load of a wave fills 8 rows of a step: lane l row l / 8, piece l % 8 of LDS, which
-  // holds the row's piece (l % 8) ^ (l / 8). Rows beyond the matrix are read as its last
+  // holds the row's piece (l % 8) ^ (row / 2 % 8). Rows beyond the matrix are read as its last
   // one, and their results are not used.
   constexpr int kWaves = S::kThreads / 64;
-  static_assert(S::BM % (kWaves * 8) == 0, "a load is of A or of B");
-  const int row8 = lane >> 3, piece = (lane & 7) ^ row8;
+  static_assert(S::BM % (kWaves * 8) == 0 && kWaves % 2 == 0, "a load is of A or of B");
+  const int row8 = lane >> 3, piece = (lane & 7) ^ (row8 >> 1 | (wave & 1) << 2);
   const char* from[S::kLoads];  // the first of the 8 rows, at step `first`
   typename Offset<DIRECT>::type offset[S::kLoads];
 #pragma unroll
@@ -167,18 +167,24 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
   uint32_t at[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h)
-    at[h] = (lane & 15) * kStepBytes + (((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
-  U4 a[2][S::MT], b[2][S::NT];
-  const auto read = [&](const char* stage, int h) {
+    at[h] = (lane & 15) * kStepBytes + (((h * 4 + (lane >> 4)) ^ (lane >> 1 & 7)) * 16);
+  // Two halves' pieces in registers where an instruction takes 16 bytes; the wider types
+  // take 128 and 256 cycles for them, beside which a read is short.
+  constexpr bool kAcross = DIRECT && C::kParts == 1;
+  constexpr int kHalves = kAcross ? 2 : 1;
+  U4 a[kHalves][S::MT], b[kHalves][S::NT];
+  const auto read = [&](const char* stage, int half) {
+    const int h = half % kHalves;
+    stage += at[half];
 #pragma unroll
     for (int j = 0; j < S::NT; ++j)
-      b[h][j] = *reinterpret_cast<const U4*>(stage + at[h] +
-                                             (S::BM + (wn * S::NT + j) * 16) * kStepBytes);
+      b[h][j] = *reinterpret_cast<const U4*>(stage + (S::BM + (wn * S::NT + j) * 16) * kStepBytes);
 #pragma unroll
     for (int i = 0; i < S::MT; ++i)
-      a[h][i] = *reinterpret_cast<const U4*>(stage + at[h] + (wm * S::MT + i) * 16 * kStepBytes);
+      a[h][i] = *reinterpret_cast<const U4*>(stage + (wm * S::MT + i) * 16 * kStepBytes);
   };
-  const auto compute = [&](int h) {
+  const auto compute = [&](int half) {
+    const int h = half % kHalves;
     // (an instruction's result is ready some instructions later: no two in a row share one)
 #pragma unroll
     for (int part = 0; part < C::kParts; ++part)
@@ -215,21 +221,31 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
     for (int k = 0; k < S::ST; ++k)
       if (first + k < end) request(k);
     arrived(first + S::ST <= end, Behind<S::ST - 1>());
-    read(lds, 0);
+    if (kAcross) read(lds, 0);
     int stage = 0;
     for (int64_t k = first; k < end; ++k) {
-      read(lds + stage * S::kStageBytes, 1);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(0);
-      __builtin_amdgcn_sched_barrier(0);
+      const char* const here = lds + stage * S::kStageBytes;
       const int next = stage + 1 == S::ST ? 0 : stage + 1;
+      if constexpr (kAcross) {
+        read(here, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        compute(0);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        read(here, 0);
+        compute(0);
+        read(here, 1);
+        compute(1);
+      }
       if (k + 1 < end) {
         arrived(k + S::ST <= end, Behind<S::ST - 2>());
         if (k + S::ST < end) request(stage);  // every wave has read the step
-        read(lds + next * S::kStageBytes, 0);
+        if (kAcross) read(lds + next * S::kStageBytes, 0);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      compute(1);
+      if constexpr (kAcross) {
+        __builtin_amdgcn_sched_barrier(0);
+        compute(1);
+      }
       stage = next;
     }
   } else {

@@ -42,27 +42,39 @@ __device__ inline Acc<T> weight(const void* w, bool same, int64_t i) {
 template <class T, int K, int V>
 struct Taps {
   Acc<T> w[K][V], b[V];
-  __device__ void load(const ConvArgs& a, int64_t d0, int n) {
+  __device__ Taps(const ConvArgs& a, int64_t d0) {
     const bool same = a.wtype == a.dtype;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      b[i] = a.bias && i < n ? weight<T>(a.bias, same, d0 + i) : Acc<T>(0);
+      b[i] = a.bias ? weight<T>(a.bias, same, d0 + i) : Acc<T>(0);
 #pragma unroll
-      for (int k = 0; k < K; ++k)
-        w[k][i] = i < n ? weight<T>(a.w, same, k * a.D + d0 + i) : Acc<T>(0);
+      for (int k = 0; k < K; ++k) w[k][i] = weight<T>(a.w, same, k * a.D + d0 + i);
     }
   }
 };
 
+// A thread's first channel. V channels are there at every thread: the last one of a row
+// takes the row's last V, and computes what its neighbour does once more.
+template <int V>
+__device__ inline int64_t first_channel(int64_t c, int64_t D) {
+  return c * V + V <= D ? c * V : D - V;
+}
+template <class T, int V>
+__device__ inline Pack<T, V> zeros() {
+  Pack<T, V> z;
+#pragma unroll
+  for (int i = 0; i < V; ++i) z.v[i] = T(0);
+  return z;
+}
+
 // Input t of a row, those of the window before it where t < 0 (t >= 1 - K).
 template <class T, int V>
-__device__ inline Pack<T, V> input(const ConvArgs& a, int64_t b, int64_t t, int64_t d0, int n) {
-  if (t >= 0)
-    return load_pack<T, V>(static_cast<const T*>(a.x) + b * a.sx_b + t * a.sx_t + d0, n);
+__device__ inline Pack<T, V> input(const ConvArgs& a, int64_t b, int64_t t, int64_t d0) {
+  if (t >= 0) return load_pack<T, V>(static_cast<const T*>(a.x) + b * a.sx_b + t * a.sx_t + d0, V);
   if (a.x0)
     return load_pack<T, V>(
-        static_cast<const T*>(a.x0) + (b * (a.taps - 1) + t + a.taps - 1) * a.D + d0, n);
-  return load_pack<T, V>(static_cast<const T*>(nullptr), 0);
+        static_cast<const T*>(a.x0) + (b * (a.taps - 1) + t + a.taps - 1) * a.D + d0, V);
+  return zeros<T, V>();
 }
 
 // ------------------------------------------------------------------- forward
@@ -77,14 +89,13 @@ __global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, i
   const int64_t c = id % nvec, rest = id / nvec;
   const int64_t b = rest / (segments + 1), s = rest % (segments + 1);
   if (b >= a.B) return;
-  const int64_t d0 = c * V;
-  const int n = (int)(a.D - d0 < V ? a.D - d0 : V);
+  const int64_t d0 = first_channel<V>(c, a.D);
   const int64_t len = row_length(a.lens, b, a.T);
   if (s == segments) {
     if (a.xT)
       for (int j = 0; j < K - 1; ++j)
         store_pack<T, V>(static_cast<T*>(a.xT) + (b * (K - 1) + j) * a.D + d0,
-                         input<T, V>(a, b, len + j - (K - 1), d0, n), n);
+                         input<T, V>(a, b, len + j - (K - 1), d0), V);
     return;
   }
   if (!a.y) return;
@@ -92,17 +103,16 @@ __global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, i
   const int64_t end = first + all, live = len < end ? len : end;
   T* y = static_cast<T*>(a.y) + (b * a.T + first) * a.D + d0;
   if (first < live) {
-    Taps<T, K, V> taps;
-    taps.load(a, d0, n);
+    const Taps<T, K, V> taps(a, d0);
     Pack<T, V> seen[H];  // inputs t-K+1 .. t-1
 #pragma unroll
-    for (int k = 0; k < K - 1; ++k) seen[k] = input<T, V>(a, b, first - (K - 1) + k, d0, n);
+    for (int k = 0; k < K - 1; ++k) seen[k] = input<T, V>(a, b, first - (K - 1) + k, d0);
     const T* x = static_cast<const T*>(a.x) + b * a.sx_b + first * a.sx_t + d0;
     for (int64_t t = first; t < live; t += kBatch) {
-      Pack<T, V> in[kBatch];
+      Pack<T, V> in[kBatch];  // (of steps that are not there the batch's first)
 #pragma unroll
       for (int r = 0; r < kBatch; ++r)
-        in[r] = load_pack<T, V>(x + r * a.sx_t, t + r < live ? n : 0);
+        in[r] = load_pack<T, V>(x + (t + r < live ? r * a.sx_t : 0), V);
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
         Pack<T, V> out;
@@ -119,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, i
           }
           out.v[i] = down<T>(v);
         }
-        if (t + r < live) store_pack<T, V>(y + r * a.D, out, n);
+        if (t + r < live) store_pack<T, V>(y + r * a.D, out, V);
 #pragma unroll
         for (int k = 0; k + 1 < K - 1; ++k) seen[k] = seen[k + 1];
         if (K > 1) seen[H - 1] = in[r];
@@ -129,10 +139,8 @@ __global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, i
     }
   }
   y = static_cast<T*>(a.y) + b * a.T * a.D + d0;
-  Pack<T, V> zero;
-#pragma unroll
-  for (int i = 0; i < V; ++i) zero.v[i] = T(0);
-  for (int64_t t = live > first ? live : first; t < end; ++t) store_pack<T, V>(y + t * a.D, zero, n);
+  for (int64_t t = live > first ? live : first; t < end; ++t)
+    store_pack<T, V>(y + t * a.D, zeros<T, V>(), V);
 }
 
 // ------------------------------------------------------------------- reverse
@@ -142,9 +150,7 @@ struct Layout {
   int columns;
   int64_t slabs, workers, segments;
 };
-template <class T, int K>
-Layout layout_of(int64_t B, int64_t T_, int64_t D) {
-  constexpr int V = lanes_of<T, K>(true);
+Layout layout_of(int64_t B, int64_t T_, int64_t D, int V) {
   const int64_t nvec = (D + V - 1) / V;
   Layout l;
   l.columns = 1;
@@ -166,12 +172,9 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
   const int rows = kThreads / l.columns;
   const int column = threadIdx.x % l.columns, row = threadIdx.x / l.columns;
   const int64_t slab = blockIdx.x % l.slabs, worker = blockIdx.x / l.slabs;
-  const int64_t d0 = (slab * l.columns + column) * V;
-  const int n = (int)(a.D - d0 < V ? (a.D - d0 > 0 ? a.D - d0 : 0) : V);
-  const T* const x = static_cast<const T*>(a.x);
-  const T* const dy = static_cast<const T*>(a.dy);
-  Taps<T, K, V> taps;
-  if (n > 0) taps.load(a, d0, n);
+  const int64_t c = slab * l.columns + column, d0 = first_channel<V>(c, a.D);
+  const bool works = c * V < a.D;
+  const Taps<T, K, V> taps(a, d0);
   A dw[K][V], db[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -179,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
 #pragma unroll
     for (int k = 0; k < K; ++k) dw[k][i] = A(0);
   }
-  const int64_t all = n > 0 ? a.B * l.segments : 0;
+  const int64_t all = works ? a.B * l.segments : 0;
   for (int64_t item = worker * rows + row; item < all; item += l.workers * rows) {
     const int64_t b = item / l.segments, first = item % l.segments * kSegment;
     const int64_t end = a.T - first < kSegment ? a.T : first + kSegment;
@@ -188,38 +191,49 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
     const int64_t low = first > 0 ? first : -(K - 1);
     const int64_t most = end + K - 1 < len ? end + K - 1 : len;  // steps that are needed
     Pack<T, V> seen[H];
+    const bool any = first < most;
+    if (any) {
 #pragma unroll
-    for (int k = 0; k < K - 1; ++k) {
-      const bool have = first - (K - 1) + k < len;
-      seen[k] = input<T, V>(a, b, first - (K - 1) + k, d0, have ? n : 0);
+      for (int k = 0; k < K - 1; ++k) seen[k] = input<T, V>(a, b, first - (K - 1) + k, d0);
     }
     A acc[K][V];  // of the gradients of inputs t-K+1 .. t
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i) acc[k][i] = A(0);
-    const int64_t stop = end + K - 1;  // every gradient has left by then
-    for (int64_t t0 = first; t0 < stop; t0 += kBatch) {
-      Pack<T, V> in[kBatch], d[kBatch];
+    const T* x = static_cast<const T*>(a.x) + b * a.sx_b + first * a.sx_t + d0;
+    const T* dy = static_cast<const T*>(a.dy) + b * a.sd_b + first * a.sd_t + d0;
+    Pack<T, V> in[kBatch], d[kBatch];
+    const auto request = [&](int64_t t0) {  // (of steps that are not there the segment's first)
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
-        const int64_t t = t0 + r;
-        const int m = t < most ? n : 0;
-        in[r] = load_pack<T, V>(x + b * a.sx_b + t * a.sx_t + d0, m);
-        d[r] = load_pack<T, V>(dy + b * a.sd_b + t * a.sd_t + d0, m);
+        const int64_t t = t0 + r < most ? t0 + r - first : 0;
+        in[r] = load_pack<T, V>(x + t * a.sx_t, V);
+        d[r] = load_pack<T, V>(dy + t * a.sd_t, V);
       }
+    };
+    if (any) request(first);
+    const int64_t stop = end + K - 1;  // every gradient has left by then
+    for (int64_t t0 = first; t0 < stop; t0 += kBatch) {
+      Pack<T, V> now[kBatch], e[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        now[r] = in[r];
+        e[r] = d[r];
+      }
+      if (t0 + kBatch < most) request(t0 + kBatch);
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
         const int64_t t = t0 + r;
         if (t < most) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            A g = up((T)d[r].v[i]);
+            A g = up((T)e[r].v[i]);
             if (a.act == ADST_ACT_SILU) {
               A v = taps.b[i], s, q;
 #pragma unroll
               for (int k = 0; k < K - 1; ++k) v = fma_(taps.w[k][i], up((T)seen[k].v[i]), v);
-              v = fma_(taps.w[K - 1][i], up((T)in[r].v[i]), v);
+              v = fma_(taps.w[K - 1][i], up((T)now[r].v[i]), v);
               gates<T>(v, &s, &q);
               g *= s * fma_(v, q, A(1));
             }
@@ -229,7 +243,7 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
               db[i] += g;
 #pragma unroll
               for (int k = 0; k < K - 1; ++k) dw[k][i] = fma_(g, up((T)seen[k].v[i]), dw[k][i]);
-              dw[K - 1][i] = fma_(g, up((T)in[r].v[i]), dw[K - 1][i]);
+              dw[K - 1][i] = fma_(g, up((T)now[r].v[i]), dw[K - 1][i]);
             }
           }
         }
@@ -240,15 +254,15 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
           Pack<T, V> of;
           if (held)
             of = load_pack<T, V>(static_cast<const T*>(a.dxT) +
-                                     (b * (K - 1) + at + (K - 1) - len) * a.D + d0, n);
+                                     (b * (K - 1) + at + (K - 1) - len) * a.D + d0, V);
 #pragma unroll
           for (int i = 0; i < V; ++i)
             out.v[i] = down<T>(held ? acc[0][i] + up((T)of.v[i]) : acc[0][i]);
           if (at >= 0) {
-            if (a.dx) store_pack<T, V>(static_cast<T*>(a.dx) + (b * a.T + at) * a.D + d0, out, n);
+            if (a.dx) store_pack<T, V>(static_cast<T*>(a.dx) + (b * a.T + at) * a.D + d0, out, V);
           } else if (a.dx0) {
             store_pack<T, V>(static_cast<T*>(a.dx0) + (b * (K - 1) + at + (K - 1)) * a.D + d0, out,
-                             n);
+                             V);
           }
         }
 #pragma unroll
@@ -259,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
         for (int i = 0; i < V; ++i) acc[K - 1][i] = A(0);
 #pragma unroll
         for (int k = 0; k + 1 < K - 1; ++k) seen[k] = seen[k + 1];
-        if (K > 1) seen[H - 1] = in[r];
+        if (K > 1) seen[H - 1] = now[r];
       }
     }
   }
@@ -272,12 +286,12 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
 #pragma unroll
     for (int i = 0; i < V; ++i) part[threadIdx.x][i] = k < K ? dw[k < K ? k : 0][i] : db[i];
     __syncthreads();
-    if (row == 0)
+    if (row == 0 && works)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         A v = A(0);
         for (int r = 0; r < rows; ++r) v += part[r * l.columns + column][i];
-        if (i < n) out[k * a.D + d0 + i] = v;
+        out[k * a.D + d0 + i] = v;
       }
   }
 }
@@ -383,6 +397,12 @@ hipError_t by_taps(int taps, F f) {
   }
 }
 
+// f(the channels of a thread): one where a row has fewer than V.
+template <int V, class F>
+hipError_t by_lanes(int64_t D, F f) {
+  return D >= V ? f(Count<V>()) : f(Count<1>());
+}
+
 // Workgroups of one launch at most: its work-items are counted in 32 bits.
 constexpr int64_t kMostGroups = (int64_t(1) << 32) / kThreads - 1;
 
@@ -392,7 +412,9 @@ hipError_t conv_forward(const ConvArgs& q, hipStream_t st) {
   return by_type(q.dtype, [&](auto t) {
     return by_taps(q.taps, [&](auto k) {
       typedef decltype(t) T;
-      constexpr int K = decltype(k)::value, V = lanes_of<T, K>(false);
+      constexpr int K = decltype(k)::value;
+      return by_lanes<lanes_of<T, K>(false)>(q.D, [&](auto lanes) {
+      constexpr int V = decltype(lanes)::value;
       const int64_t nvec = (q.D + V - 1) / V;
       const int segment =
           nvec * q.B * ((q.T + kSegment - 1) / kSegment) >= kManyThreads ? kSegment : kFewSegment;
@@ -414,6 +436,7 @@ hipError_t conv_forward(const ConvArgs& q, hipStream_t st) {
         if (e != hipSuccess) return e;
       }
       return hipSuccess;
+      });
     });
   });
 }
@@ -424,8 +447,11 @@ uint64_t conv_workspace_bytes(int32_t dtype, int64_t B, int64_t T_, int64_t D, i
     return by_taps(taps, [&](auto k) {
       typedef decltype(t) T;
       constexpr int K = decltype(k)::value;
-      bytes = (uint64_t)layout_of<T, K>(B, T_, D).workers * (K + 1) * D * sizeof(Acc<T>);
-      return hipSuccess;
+      return by_lanes<lanes_of<T, K>(true)>(D, [&](auto lanes) {
+        bytes = (uint64_t)layout_of(B, T_, D, decltype(lanes)::value).workers * (K + 1) * D *
+                sizeof(Acc<T>);
+        return hipSuccess;
+      });
     });
   });
   return bytes;
@@ -435,8 +461,10 @@ hipError_t conv_vjp(const ConvArgs& q, void* ws, hipStream_t st) {
   return by_type(q.dtype, [&](auto t) {
     return by_taps(q.taps, [&](auto k) {
       typedef decltype(t) T;
-      constexpr int K = decltype(k)::value, V = lanes_of<T, K>(true);
-      const Layout l = layout_of<T, K>(q.B, q.T, q.D);
+      constexpr int K = decltype(k)::value;
+      return by_lanes<lanes_of<T, K>(true)>(q.D, [&](auto lanes) {
+      constexpr int V = decltype(lanes)::value;
+      const Layout l = layout_of(q.B, q.T, q.D, V);
       const bool sums = q.dw || q.dbias;
       const hipError_t e = start(conv_rev<T, K, V>, dim3((unsigned)(l.slabs * l.workers)), kThreads,
                                  st, q, l, sums ? ws : nullptr);
@@ -444,6 +472,7 @@ hipError_t conv_vjp(const ConvArgs& q, void* ws, hipStream_t st) {
       return start(conv_sum<T>, dim3((unsigned)(((K + 1) * q.D + 63) / 64)), kThreads, st,
                    static_cast<const Acc<T>*>(ws), l.workers, q.D, K, q.dw, q.dbias,
                    q.wtype == q.dtype);
+      });
     });
   });
 }

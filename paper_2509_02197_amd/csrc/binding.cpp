@@ -1,10 +1,10 @@
-// The ordinary calls of sequence.py, from tensors to the C call without Python
+// The ordinary calls of sequence.py and tokens.py, from tensors to the C call without Python
 // in between: a small call's time is the host's, and each attribute that
 // Python looks up is a good part of it (layer norm of 32 rows: 10.1 us through
 // Python, 6.7 from here, of which 3 are the launch; one step of AdamW over 121
 // tensors: 37 and 14). Each function returns None for anything that is not
 // ordinary (a wrong or unusual argument, tensors on another device than the
-// current one), before anything is launched; sequence.py then goes its own
+// current one), before anything is launched; the Python code then goes its own
 // way, which handles the unusual and raises the errors. A call that HIP fails
 // may have launched some of its work: it is never made again but raises
 // sequence.py's AdstError. Nothing else here throws into Python.
@@ -336,6 +336,321 @@ PyObject* recurrence_step(PyObject* module, Args x, Py_ssize_t n) {
   });
 }
 
+// --------------------------------------------------------- token operators
+const int32_t* ints(const at::Tensor& t) { return static_cast<const int32_t*>(at_of(t)); }
+void strides(const at::Tensor& t, int64_t (&to)[2]) {
+  to[0] = t.defined() ? t.stride(0) : 0;
+  to[1] = t.defined() && t.dim() > 2 ? t.stride(1) : 0;
+}
+
+// x [batch, steps, channels], or [batch, channels] of one step.
+adst_conv_problem conv_problem(const at::Tensor& x, const at::Tensor& w, const at::Tensor& b,
+                               int64_t act, const Here& h) {
+  same(x, x.sizes(), x.scalar_type(), h, false);
+  need(w.dim() == 2);
+  adst_conv_problem p{};
+  p.dtype = code_of(x);
+  p.weight_dtype = code_of(w);
+  p.act = (int32_t)act;
+  need(w.size(0) >= 1 && w.size(0) <= ADST_CONV_MAX_TAPS);
+  p.taps = (int32_t)w.size(0);
+  p.batch = x.size(0);
+  p.steps = x.dim() == 3 ? x.size(1) : 1;
+  p.channels = x.size(-1);
+  same(w, {p.taps, p.channels}, w.scalar_type(), h, true);
+  same(b, {p.channels}, w.scalar_type(), h, true);
+  strides(x, p.stride_x);
+  return p;
+}
+at::Tensor window(const adst_conv_problem& p, at::ScalarType type, const Here& h) {
+  return make({p.batch, p.taps - 1, p.channels}, type, h);
+}
+
+// (x, w, b, x0, lens, act, want_y)
+PyObject* causal_conv(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 7);
+    const at::Tensor x = tensor(a[0]), w = tensor(a[1]), b = maybe(a[2]), x0 = maybe(a[3]),
+                     lens = maybe(a[4]);
+    const Here h = here(x);
+    need(x.dim() == 3);
+    const adst_conv_problem p = conv_problem(x, w, b, whole(a[5]), h);
+    same(x0, {p.batch, p.taps - 1, p.channels}, x.scalar_type(), h, true);
+    same(lens, {p.batch}, at::kInt, h, true);
+    const at::Tensor none, y = truth(a[6]) ? like(x) : none, xT = window(p, x.scalar_type(), h);
+    Dict d;
+    d.put("y", y);
+    d.put("xT", xT);
+    run(adst_causal_conv_forward(&p, x.data_ptr(), w.data_ptr(), at_of(b), at_of(x0), ints(lens),
+                                 at_of(y), xT.data_ptr(), h.stream));
+    return d.take();
+  });
+}
+
+// (x, dy, w, b, x0, lens, dxT, act, want_dx, want_dw, want_db)
+PyObject* causal_conv_vjp(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 11);
+    const at::Tensor x = tensor(a[0]), dy = tensor(a[1]), w = tensor(a[2]), b = maybe(a[3]),
+                     x0 = maybe(a[4]), lens = maybe(a[5]), dxT = maybe(a[6]);
+    const Here h = here(x);
+    need(x.dim() == 3);
+    adst_conv_problem p = conv_problem(x, w, b, whole(a[7]), h);
+    same(dy, x.sizes(), x.scalar_type(), h, false);
+    strides(dy, p.stride_dy);
+    same(x0, {p.batch, p.taps - 1, p.channels}, x.scalar_type(), h, true);
+    same(dxT, {p.batch, p.taps - 1, p.channels}, x.scalar_type(), h, true);
+    same(lens, {p.batch}, at::kInt, h, true);
+    const bool dw_ = truth(a[9]), db_ = truth(a[10]);
+    const at::Tensor none, dx = truth(a[8]) ? like(x) : none, dw = dw_ ? like(w) : none,
+                     db = db_ ? make({p.channels}, w.scalar_type(), h) : none,
+                     dx0 = window(p, x.scalar_type(), h);
+    const uint64_t size = dw_ || db_ ? adst_causal_conv_workspace_bytes(&p) : 0;
+    const at::Tensor ws = bytes(size, h);
+    Dict d;
+    d.put("dx", dx);
+    d.put("dw", dw);
+    d.put("db", db);
+    d.put("dx0", dx0);
+    run(adst_causal_conv_vjp(&p, x.data_ptr(), dy.data_ptr(), w.data_ptr(), at_of(b), at_of(x0),
+                             ints(lens), at_of(dxT), at_of(dx), at_of(dw), at_of(db),
+                             dx0.data_ptr(), at_of(ws), size, h.stream));
+    return d.take();
+  });
+}
+
+// out, wrapped, of a call that writes `state` in place; call() makes it.
+template <class F>
+PyObject* in_place(const at::Tensor& out, const at::Tensor& state, F call) {
+  PyObject* const r = THPVariable_Wrap(out);
+  need(r);
+  const adst_status status = call();
+  if (status != ADST_OK) Py_DECREF(r);
+  if (status == ADST_OK || status == ADST_ERR_HIP) changed(state);
+  run(status);
+  return r;
+}
+
+// (x, w, window, b, slots, act)
+PyObject* causal_conv_step(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 6);
+    const at::Tensor x = tensor(a[0]), w = tensor(a[1]), pool = tensor(a[2]), b = maybe(a[3]),
+                     slots = maybe(a[4]);
+    const Here h = here(x);
+    need(x.dim() == 2 && pool.dim() == 3);
+    const adst_conv_problem p = conv_problem(x, w, b, whole(a[5]), h);
+    same(pool, {pool.size(0), p.taps - 1, p.channels}, x.scalar_type(), h, true);
+    same(slots, {p.batch}, at::kInt, h, true);
+    const at::Tensor y = like(x);
+    return in_place(y, pool, [&] {
+      return adst_causal_conv_step(&p, x.data_ptr(), w.data_ptr(), at_of(b), ints(slots),
+                                   pool.data_ptr(), pool.size(0), y.data_ptr(), h.stream);
+    });
+  });
+}
+
+// The scan's tensors: x, delta, z and dy [batch, steps, channels], B and C [batch, steps, groups,
+// states] or without the groups; of one step without the steps' axis.
+struct Scan {
+  adst_scan_problem p{};
+  adst_scan_inputs in{};
+  at::ScalarType acc;
+};
+Scan scan_problem(const at::Tensor& x, const at::Tensor& delta, const at::Tensor& A,
+                  const at::Tensor& B, const at::Tensor& C, const at::Tensor& D,
+                  const at::Tensor& z, const at::Tensor& bias, const at::Tensor& dy, bool softplus,
+                  bool one, const Here& h) {
+  Scan s;
+  adst_scan_problem& p = s.p;
+  const int dims = one ? 2 : 3;
+  const at::ScalarType type = x.scalar_type();
+  need(x.dim() == dims && A.dim() == 2);
+  for (const at::Tensor& t : {x, delta, z, dy}) same(t, x.sizes(), type, h, false);
+  p.dtype = code_of(x);
+  s.acc = acc_of(p.dtype);
+  p.softplus = softplus;
+  p.batch = x.size(0);
+  p.steps = one ? 1 : x.size(1);
+  p.channels = x.size(-1);
+  p.states = A.size(1);
+  same(A, {p.channels, p.states}, s.acc, h, true);
+  p.groups = B.dim() == dims + 1 ? B.size(dims - 1) : 1;
+  need(p.groups >= 1);
+  for (const at::Tensor& t : {B, C}) {
+    need((t.dim() == dims + 1 || (t.dim() == dims && p.groups == 1)) &&
+         t.scalar_type() == type && t.device() == h.device && t.size(0) == p.batch &&
+         (one || t.size(1) == p.steps) && t.size(-1) == p.states &&
+         (p.states < 2 || t.stride(-1) == 1));
+    if (t.dim() == dims + 1)
+      need(t.size(dims - 1) == p.groups && (p.groups < 2 || t.stride(dims - 1) == p.states));
+  }
+  same(D, {p.channels}, s.acc, h, true);
+  same(bias, {p.channels}, s.acc, h, true);
+  const auto set = [&](const at::Tensor& t, int64_t (&to)[2]) {
+    to[0] = t.defined() ? t.stride(0) : 0;
+    to[1] = t.defined() && !one ? t.stride(1) : 0;
+  };
+  set(x, p.stride_x);
+  set(delta, p.stride_delta);
+  set(B, p.stride_b);
+  set(C, p.stride_c);
+  set(z, p.stride_z);
+  set(dy, p.stride_dy);
+  s.in = {x.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(),
+          at_of(D),     at_of(z),         at_of(bias),  nullptr,      nullptr};
+  return s;
+}
+void scan_rows(Scan& s, const at::Tensor& h0, const at::Tensor& lens, const at::Tensor& dhT,
+               const Here& h) {
+  for (const at::Tensor& t : {h0, dhT})
+    same(t, {s.p.batch, s.p.channels, s.p.states}, s.acc, h, true);
+  same(lens, {s.p.batch}, at::kInt, h, true);
+  s.in.h0 = at_of(h0);
+  s.in.lens = ints(lens);
+}
+
+// (x, delta, A, B, C, D, z, delta_bias, h0, lens, softplus, want_y, want_ck)
+PyObject* selective_scan(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 13);
+    const at::Tensor x = tensor(a[0]), none;
+    const Here h = here(x);
+    const at::Tensor delta = tensor(a[1]), A = tensor(a[2]), B = tensor(a[3]), C = tensor(a[4]),
+                     D = maybe(a[5]), z = maybe(a[6]), bias = maybe(a[7]), h0 = maybe(a[8]),
+                     lens = maybe(a[9]);
+    Scan s = scan_problem(x, delta, A, B, C, D, z, bias, none, truth(a[10]), false, h);
+    scan_rows(s, h0, lens, none, h);
+    adst_scan_info info;
+    run(adst_selective_scan_plan(&s.p, &info));
+    const at::Tensor y = truth(a[11]) ? like(x) : none,
+                     hT = make({s.p.batch, s.p.channels, s.p.states}, s.acc, h),
+                     ck = truth(a[12]) ? bytes(info.ck_bytes, h) : none,
+                     ws = bytes(info.workspace_bytes, h);
+    Dict d;
+    d.put("y", y);
+    d.put("hT", hT);
+    d.put("ck", ck);
+    run(adst_selective_scan_forward(&s.p, &s.in, at_of(y), hT.data_ptr(), at_of(ck), at_of(ws),
+                                    info.workspace_bytes, h.stream));
+    return d.take();
+  });
+}
+
+// (x, delta, A, B, C, dy, D, z, delta_bias, h0, lens, dhT, ck, softplus)
+PyObject* selective_scan_vjp(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 14);
+    const at::Tensor x = tensor(a[0]);
+    const Here h = here(x);
+    const at::Tensor delta = tensor(a[1]), A = tensor(a[2]), B = tensor(a[3]), C = tensor(a[4]),
+                     dy = tensor(a[5]), D = maybe(a[6]), z = maybe(a[7]), bias = maybe(a[8]),
+                     h0 = maybe(a[9]), lens = maybe(a[10]), dhT = maybe(a[11]), ck = maybe(a[12]);
+    Scan s = scan_problem(x, delta, A, B, C, D, z, bias, dy, truth(a[13]), false, h);
+    scan_rows(s, h0, lens, dhT, h);
+    adst_scan_info info;
+    run(adst_selective_scan_plan(&s.p, &info));
+    same(ck, {(int64_t)info.ck_bytes}, at::kByte, h, true);
+    const uint64_t size = info.vjp_workspace_bytes + (ck.defined() ? 0 : info.ck_bytes);
+    const auto out = [](const at::Tensor& t) { return t.defined() ? like(t) : t; };
+    const at::Tensor dx = like(x), ddelta = like(x), dz = out(z), dB = like(B), dC = like(C),
+                     dA = like(A), dD = out(D), dbias = out(bias),
+                     dh0 = make({s.p.batch, s.p.channels, s.p.states}, s.acc, h),
+                     ws = bytes(size, h);
+    Dict d;
+    d.put("dx", dx);
+    d.put("ddelta", ddelta);
+    d.put("dz", dz);
+    d.put("dB", dB);
+    d.put("dC", dC);
+    d.put("dA", dA);
+    d.put("dD", dD);
+    d.put("ddelta_bias", dbias);
+    d.put("dh0", dh0);
+    const adst_scan_gradients g{dx.data_ptr(), ddelta.data_ptr(), at_of(dz),
+                                dB.data_ptr(), dC.data_ptr(),     dA.data_ptr(),
+                                at_of(dD),     at_of(dbias),      dh0.data_ptr()};
+    run(adst_selective_scan_vjp(&s.p, &s.in, at_of(ck), dy.data_ptr(), at_of(dhT), &g, at_of(ws),
+                                size, h.stream));
+    return d.take();
+  });
+}
+
+// (x, delta, A, B, C, state, D, z, delta_bias, slots, softplus)
+PyObject* selective_scan_step(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 11);
+    const at::Tensor x = tensor(a[0]), none;
+    const Here h = here(x);
+    const at::Tensor delta = tensor(a[1]), A = tensor(a[2]), B = tensor(a[3]), C = tensor(a[4]),
+                     state = tensor(a[5]), D = maybe(a[6]), z = maybe(a[7]), bias = maybe(a[8]),
+                     slots = maybe(a[9]);
+    const Scan s = scan_problem(x, delta, A, B, C, D, z, bias, none, truth(a[10]), true, h);
+    need(state.dim() == 3);
+    same(state, {state.size(0), s.p.channels, s.p.states}, s.acc, h, true);
+    same(slots, {s.p.batch}, at::kInt, h, true);
+    const at::Tensor y = like(x);
+    return in_place(y, state, [&] {
+      return adst_selective_scan_step(&s.p, &s.in, ints(slots), state.data_ptr(), state.size(0),
+                                      y.data_ptr(), h.stream);
+    });
+  });
+}
+
+adst_xent_problem xent_problem(const at::Tensor& x, const at::Tensor& w, const at::Tensor& labels,
+                               const Here& h) {
+  need(x.dim() == 2 && w.dim() == 2 && x.size(1) >= 1 && w.size(0) >= 1);
+  same(x, x.sizes(), x.scalar_type(), h, false);
+  same(w, {w.size(0), x.size(1)}, x.scalar_type(), h, false);
+  same(labels, {x.size(0)}, at::kInt, h, true);
+  return {code_of(x), 0, x.size(0), x.size(1), w.size(0), x.stride(0), w.stride(0)};
+}
+
+// (x, w, labels)
+PyObject* linear_cross_entropy(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 3);
+    const at::Tensor x = tensor(a[0]), w = tensor(a[1]), labels = tensor(a[2]);
+    const Here h = here(x);
+    const adst_xent_problem p = xent_problem(x, w, labels, h);
+    adst_xent_info info;
+    run(adst_linear_cross_entropy_plan(&p, &info));
+    const at::Tensor loss = make({p.rows}, acc_of(p.dtype), h),
+                     lse = make({p.rows}, acc_of(p.dtype), h), ws = bytes(info.workspace_bytes, h);
+    Dict d;
+    d.put("loss", loss);
+    d.put("lse", lse);
+    run(adst_linear_cross_entropy_forward(&p, x.data_ptr(), w.data_ptr(), ints(labels),
+                                          loss.data_ptr(), lse.data_ptr(), at_of(ws),
+                                          info.workspace_bytes, h.stream));
+    return d.take();
+  });
+}
+
+// (x, w, labels, lse, dloss, want_dx, want_dw)
+PyObject* linear_cross_entropy_vjp(PyObject* module, Args a, Py_ssize_t n) {
+  return ordinary(module, [&] {
+    need(n == 7);
+    const at::Tensor x = tensor(a[0]), w = tensor(a[1]), labels = tensor(a[2]), lse = tensor(a[3]),
+                     dloss = maybe(a[4]);
+    const Here h = here(x);
+    const adst_xent_problem p = xent_problem(x, w, labels, h);
+    same(lse, {p.rows}, acc_of(p.dtype), h, true);
+    same(dloss, {p.rows}, acc_of(p.dtype), h, true);
+    adst_xent_info info;
+    run(adst_linear_cross_entropy_plan(&p, &info));
+    const at::Tensor none, dx = truth(a[5]) ? like(x) : none, dw = truth(a[6]) ? like(w) : none,
+                     ws = bytes(info.vjp_workspace_bytes, h);
+    Dict d;
+    d.put("dx", dx);
+    d.put("dw", dw);
+    run(adst_linear_cross_entropy_vjp(&p, x.data_ptr(), w.data_ptr(), ints(labels), lse.data_ptr(),
+                                      at_of(dloss), at_of(dx), at_of(dw), at_of(ws),
+                                      info.vjp_workspace_bytes, h.stream));
+    return d.take();
+  });
+}
+
 // --------------------------------------------------------------------- AdamW
 // (problem's address, descriptors' address, their number, params, states,
 // grads, copies or None, grad_scale or None, t), states the tuple of m and v,
@@ -418,8 +733,20 @@ PyObject* adamw_step(PyObject* module, Args a, Py_ssize_t n) {
 
 #define CALL(name) \
   { #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr }
-PyMethodDef kMethods[] = {CALL(layer_norm),     CALL(layer_norm_vjp),  CALL(recurrence),
-                          CALL(recurrence_vjp), CALL(recurrence_step), CALL(adamw_step),
+PyMethodDef kMethods[] = {CALL(layer_norm),
+                          CALL(layer_norm_vjp),
+                          CALL(recurrence),
+                          CALL(recurrence_vjp),
+                          CALL(recurrence_step),
+                          CALL(adamw_step),
+                          CALL(causal_conv),
+                          CALL(causal_conv_vjp),
+                          CALL(causal_conv_step),
+                          CALL(selective_scan),
+                          CALL(selective_scan_vjp),
+                          CALL(selective_scan_step),
+                          CALL(linear_cross_entropy),
+                          CALL(linear_cross_entropy_vjp),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods};
 

@@ -25,11 +25,16 @@ constexpr int kSegment = 32;   // steps of a thread, where there are enough thre
 constexpr int kFewSegment = 8;
 constexpr int64_t kManyThreads = 1 << 17;  // 8 waves a CU
 
-// Channels of a thread: 16 bytes, and half of that where the taps' weights and
-// sums would not leave registers for two waves a SIMD.
+template <int K>
+struct Count {
+  static constexpr int value = K;
+};
+
+// Channels of a thread: as many as leave registers for three waves a SIMD (8 x 4096 x 2048
+// bf16 forward 64 us with 4 channels of 2 bytes, 67 with 8).
 template <class T, int K>
 constexpr int lanes_of(bool reverse) {
-  return sizeof(T) == 2 ? (K > 4 || reverse ? 4 : 8) : sizeof(T) == 4 ? (reverse && K > 4 ? 2 : 4) : 2;
+  return sizeof(T) == 8 || (sizeof(T) == 4 && reverse && K > 4) ? 2 : 4;
 }
 
 // A weight: of T, or of float beside 16-bit T.
@@ -80,7 +85,7 @@ __device__ inline Pack<T, V> input(const ConvArgs& a, int64_t b, int64_t t, int6
 // ------------------------------------------------------------------- forward
 // A thread: V channels of one segment of a row; the last segment's index copies
 // the window that follows the row.
-template <class T, int K, int V>
+template <class T, int K, int V, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, int64_t segments,
                                                      int segment) {
   typedef Acc<T> A;
@@ -108,11 +113,17 @@ __global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, i
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) seen[k] = input<T, V>(a, b, first - (K - 1) + k, d0);
     const T* x = static_cast<const T*>(a.x) + b * a.sx_b + first * a.sx_t + d0;
-    for (int64_t t = first; t < live; t += kBatch) {
-      Pack<T, V> in[kBatch];  // (of steps that are not there the batch's first)
+    Pack<T, V> in[kBatch];
+    const auto request = [&](int64_t t) {  // (of steps that are not there the segment's first)
 #pragma unroll
       for (int r = 0; r < kBatch; ++r)
-        in[r] = load_pack<T, V>(x + (t + r < live ? r * a.sx_t : 0), V);
+        in[r] = load_pack<T, V>(x + (t + r < live ? t + r - first : 0) * a.sx_t, V);
+    };
+    const auto batch = [&](int64_t t, auto whole) {
+      Pack<T, V> now[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) now[r] = in[r];
+      request(t + kBatch);
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
         Pack<T, V> out;
@@ -121,22 +132,25 @@ __global__ __launch_bounds__(kThreads) void conv_fwd(ConvArgs a, int64_t nvec, i
           A v = taps.b[i];
 #pragma unroll
           for (int k = 0; k < K - 1; ++k) v = fma_(taps.w[k][i], up((T)seen[k].v[i]), v);
-          v = fma_(taps.w[K - 1][i], up((T)in[r].v[i]), v);
-          if (a.act == ADST_ACT_SILU) {
+          v = fma_(taps.w[K - 1][i], up((T)now[r].v[i]), v);
+          if (SILU) {
             A g, q;
             gates<T>(v, &g, &q);
             v *= g;
           }
           out.v[i] = down<T>(v);
         }
-        if (t + r < live) store_pack<T, V>(y + r * a.D, out, V);
+        if (decltype(whole)::value || t + r < live) store_pack<T, V>(y + r * a.D, out, V);
 #pragma unroll
         for (int k = 0; k + 1 < K - 1; ++k) seen[k] = seen[k + 1];
-        if (K > 1) seen[H - 1] = in[r];
+        if (K > 1) seen[H - 1] = now[r];
       }
-      x += kBatch * a.sx_t;
       y += kBatch * a.D;
-    }
+    };
+    request(first);
+    int64_t t = first;
+    for (; t + kBatch <= live; t += kBatch) batch(t, Count<1>());
+    if (t < live) batch(t, Count<0>());
   }
   y = static_cast<T*>(a.y) + b * a.T * a.D + d0;
   for (int64_t t = live > first ? live : first; t < end; ++t)
@@ -164,7 +178,7 @@ Layout layout_of(int64_t B, int64_t T_, int64_t D, int V) {
   return l;
 }
 
-template <class T, int K, int V>
+template <class T, int K, int V, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void* sums) {
   typedef Acc<T> A;
   constexpr int H = K > 1 ? K - 1 : 1;
@@ -213,69 +227,88 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
       }
     };
     if (any) request(first);
-    const int64_t stop = end + K - 1;  // every gradient has left by then
-    for (int64_t t0 = first; t0 < stop; t0 += kBatch) {
+    // one step: WHOLE: it is there; OWN: one of the segment's, whose dw and db it adds to, 0 where
+    // that is to be asked
+    const auto step = [&](int r, int64_t t, const Pack<T, V>& now, const Pack<T, V>& e, auto whole,
+                          auto own) {
+      constexpr bool kWhole = decltype(whole)::value, kOwn = decltype(own)::value;
+      if (kWhole || t < most) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          A g = up((T)e.v[i]);
+          if (SILU) {
+            A v = taps.b[i], s, q;
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k) v = fma_(taps.w[k][i], up((T)seen[k].v[i]), v);
+            v = fma_(taps.w[K - 1][i], up((T)now.v[i]), v);
+            gates<T>(v, &s, &q);
+            g *= s * fma_(v, q, A(1));
+          }
+#pragma unroll
+          for (int k = 0; k < K; ++k) acc[k][i] = fma_(taps.w[k][i], g, acc[k][i]);
+          if (kOwn || (!kWhole && t < end)) {
+            db[i] += g;
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k) dw[k][i] = fma_(g, up((T)seen[k].v[i]), dw[k][i]);
+            dw[K - 1][i] = fma_(g, up((T)now.v[i]), dw[K - 1][i]);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k + 1 < K - 1; ++k) seen[k] = seen[k + 1];
+      if (K > 1) seen[H - 1] = now;
+    };
+    // the gradient of input t - (K - 1) is whole
+    const auto leave = [&](int64_t t, auto inside) {
+      const int64_t at = t - (K - 1);
+      if (decltype(inside)::value || (at >= low && at < end)) {
+        Pack<T, V> out, of;
+        const bool held =
+            !decltype(inside)::value && a.dxT && at >= len - (K - 1) && at < len;
+        if (held)
+          of = load_pack<T, V>(static_cast<const T*>(a.dxT) +
+                                   (b * (K - 1) + at + (K - 1) - len) * a.D + d0, V);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          out.v[i] = down<T>(held ? acc[0][i] + up((T)of.v[i]) : acc[0][i]);
+        if (decltype(inside)::value || at >= 0) {
+          if (a.dx) store_pack<T, V, true>(static_cast<T*>(a.dx) + (b * a.T + at) * a.D + d0, out, V);
+        } else if (a.dx0) {
+          store_pack<T, V>(static_cast<T*>(a.dx0) + (b * (K - 1) + at + (K - 1)) * a.D + d0, out, V);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k + 1 < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[k][i] = acc[k + 1][i];
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[K - 1][i] = A(0);
+    };
+    const auto batch = [&](int64_t t0, auto whole, auto own, auto inside) {
       Pack<T, V> now[kBatch], e[kBatch];
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
         now[r] = in[r];
         e[r] = d[r];
       }
-      if (t0 + kBatch < most) request(t0 + kBatch);
+      if (any) request(t0 + kBatch);
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
-        const int64_t t = t0 + r;
-        if (t < most) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            A g = up((T)e[r].v[i]);
-            if (a.act == ADST_ACT_SILU) {
-              A v = taps.b[i], s, q;
-#pragma unroll
-              for (int k = 0; k < K - 1; ++k) v = fma_(taps.w[k][i], up((T)seen[k].v[i]), v);
-              v = fma_(taps.w[K - 1][i], up((T)now[r].v[i]), v);
-              gates<T>(v, &s, &q);
-              g *= s * fma_(v, q, A(1));
-            }
-#pragma unroll
-            for (int k = 0; k < K; ++k) acc[k][i] = fma_(taps.w[k][i], g, acc[k][i]);
-            if (t < end) {
-              db[i] += g;
-#pragma unroll
-              for (int k = 0; k < K - 1; ++k) dw[k][i] = fma_(g, up((T)seen[k].v[i]), dw[k][i]);
-              dw[K - 1][i] = fma_(g, up((T)now[r].v[i]), dw[K - 1][i]);
-            }
-          }
-        }
-        const int64_t at = t - (K - 1);  // the input whose gradient is whole now
-        if (at >= low && at < end) {
-          Pack<T, V> out;
-          const bool held = a.dxT && at >= len - (K - 1) && at < len;
-          Pack<T, V> of;
-          if (held)
-            of = load_pack<T, V>(static_cast<const T*>(a.dxT) +
-                                     (b * (K - 1) + at + (K - 1) - len) * a.D + d0, V);
-#pragma unroll
-          for (int i = 0; i < V; ++i)
-            out.v[i] = down<T>(held ? acc[0][i] + up((T)of.v[i]) : acc[0][i]);
-          if (at >= 0) {
-            if (a.dx) store_pack<T, V>(static_cast<T*>(a.dx) + (b * a.T + at) * a.D + d0, out, V);
-          } else if (a.dx0) {
-            store_pack<T, V>(static_cast<T*>(a.dx0) + (b * (K - 1) + at + (K - 1)) * a.D + d0, out,
-                             V);
-          }
-        }
-#pragma unroll
-        for (int k = 0; k + 1 < K; ++k)
-#pragma unroll
-          for (int i = 0; i < V; ++i) acc[k][i] = acc[k + 1][i];
-#pragma unroll
-        for (int i = 0; i < V; ++i) acc[K - 1][i] = A(0);
-#pragma unroll
-        for (int k = 0; k + 1 < K - 1; ++k) seen[k] = seen[k + 1];
-        if (K > 1) seen[H - 1] = now[r];
+        step(r, t0 + r, now[r], e[r], whole, own);
+        leave(t0 + r, inside);
       }
+    };
+    const int64_t stop = end + K - 1;  // every gradient has left by then
+    int64_t t0 = first;
+    typedef Count<1> Yes;
+    typedef Count<0> No;
+    if (first + kSegment + K - 1 <= len) {  // nothing of the segment or after it is missing
+      constexpr int kLead = (K - 1 + kBatch - 1) / kBatch;  // batches whose gradients start before
+#pragma unroll
+      for (int k = 0; k < kLead; ++k, t0 += kBatch) batch(t0, Yes(), Yes(), No());
+      for (; t0 < end; t0 += kBatch) batch(t0, Yes(), Yes(), Yes());
     }
+    for (; t0 < stop; t0 += kBatch) batch(t0, No(), No(), No());
   }
   if (!sums) return;
   // [worker][K + 1][D]: over the workgroup's rows in turn
@@ -323,11 +356,10 @@ __global__ __launch_bounds__(kThreads) void conv_sum(const Acc<T>* sums, int64_t
 
 // ------------------------------------------------------------------ one step
 template <class T, int V>
-__global__ __launch_bounds__(kThreads) void conv_one(ConvStep a, int64_t nvec) {
+__global__ __launch_bounds__(kThreads) void conv_one(ConvStep a, int64_t first) {
   typedef Acc<T> A;
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t b = id / nvec, d0 = id % nvec * V;
-  if (b >= a.B) return;
+  const int64_t b = first + blockIdx.y, d0 = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * V;
+  if (d0 >= a.D) return;
   const int n = (int)(a.D - d0 < V ? a.D - d0 : V), K = a.taps;
   const bool same = a.wtype == a.dtype;
   const int64_t slot = a.slots ? a.slots[b] : b;
@@ -340,25 +372,37 @@ __global__ __launch_bounds__(kThreads) void conv_one(ConvStep a, int64_t nvec) {
   }
   T* const window = static_cast<T*>(a.window) + slot * (K - 1) * a.D + d0;
   Pack<T, V> seen[ADST_CONV_MAX_TAPS];
+  A w[ADST_CONV_MAX_TAPS][V], v[V];
+  const auto weights = [&](const void* from, int64_t at, A (&to)[V]) {
+    if (same) {
+      const Pack<T, V> p = load_pack<T, V>(static_cast<const T*>(from) + at, n);
 #pragma unroll
-  for (int k = 0; k < ADST_CONV_MAX_TAPS - 1; ++k)
-    if (k < K - 1) seen[k] = load_pack<T, V>(window + k * a.D, n);
-  const Pack<T, V> in = load_pack<T, V>(static_cast<const T*>(a.x) + b * a.sx + d0, n);
-  A v[V];
+      for (int i = 0; i < V; ++i) to[i] = up((T)p.v[i]);
+    } else {
+      const Pack<float, V> p = load_pack<float, V>(static_cast<const float*>(from) + at, n);
 #pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = a.bias && i < n ? weight<T>(a.bias, same, d0 + i) : A(0);
+      for (int i = 0; i < V; ++i) to[i] = (A)p.v[i];
+    }
+  };
 #pragma unroll
-  for (int k = 0; k < ADST_CONV_MAX_TAPS - 1; ++k)
-    if (k < K - 1) {
+  for (int k = 0; k < ADST_CONV_MAX_TAPS; ++k)
+    if (k < K) {
+      seen[k] = load_pack<T, V>(k < K - 1 ? window + k * a.D
+                                          : static_cast<const T*>(a.x) + b * a.sx + d0, n);
+      weights(a.w, k * a.D + d0, w[k]);
+    }
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < n) v[i] = fma_(weight<T>(a.w, same, k * a.D + d0 + i), up((T)seen[k].v[i]), v[i]);
+  for (int i = 0; i < V; ++i) v[i] = A(0);
+  if (a.bias) weights(a.bias, d0, v);
+#pragma unroll
+  for (int k = 0; k < ADST_CONV_MAX_TAPS; ++k)
+    if (k < K) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = fma_(w[k][i], up((T)seen[k].v[i]), v[i]);
       if (k > 0) store_pack<T, V>(window + (k - 1) * a.D, seen[k], n);
     }
-  if (K > 1) store_pack<T, V>(window + (K - 2) * a.D, in, n);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    if (i < n) v[i] = fma_(weight<T>(a.w, same, (K - 1) * a.D + d0 + i), up((T)in.v[i]), v[i]);
     if (a.act == ADST_ACT_SILU) {
       A g, q;
       gates<T>(v[i], &g, &q);
@@ -379,10 +423,6 @@ hipError_t by_type(int32_t dtype, F f) {
     default: return f(f16());
   }
 }
-template <int K>
-struct Count {
-  static constexpr int value = K;
-};
 template <class F>
 hipError_t by_taps(int taps, F f) {
   switch (taps) {
@@ -405,6 +445,7 @@ hipError_t by_lanes(int64_t D, F f) {
 
 // Workgroups of one launch at most: its work-items are counted in 32 bits.
 constexpr int64_t kMostGroups = (int64_t(1) << 32) / kThreads - 1;
+constexpr int64_t kMostRows = 65535;  // of a launch's second axis
 
 }  // namespace
 
@@ -431,8 +472,9 @@ hipError_t conv_forward(const ConvArgs& q, hipStream_t st) {
         a.y = q.y ? static_cast<T*>(q.y) + b * q.T * q.D : nullptr;
         a.xT = q.xT ? static_cast<T*>(q.xT) + b * (K - 1) * q.D : nullptr;
         const unsigned groups = (unsigned)((a.B * row + kThreads - 1) / kThreads);
-        const hipError_t e = start(conv_fwd<T, K, V>, dim3(groups), kThreads, st, a, nvec,
-                                   segments, segment);
+        const hipError_t e = start(a.act == ADST_ACT_SILU ? conv_fwd<T, K, V, true>
+                                                          : conv_fwd<T, K, V, false>,
+                                   dim3(groups), kThreads, st, a, nvec, segments, segment);
         if (e != hipSuccess) return e;
       }
       return hipSuccess;
@@ -466,8 +508,10 @@ hipError_t conv_vjp(const ConvArgs& q, void* ws, hipStream_t st) {
       constexpr int V = decltype(lanes)::value;
       const Layout l = layout_of(q.B, q.T, q.D, V);
       const bool sums = q.dw || q.dbias;
-      const hipError_t e = start(conv_rev<T, K, V>, dim3((unsigned)(l.slabs * l.workers)), kThreads,
-                                 st, q, l, sums ? ws : nullptr);
+      const hipError_t e = start(q.act == ADST_ACT_SILU ? conv_rev<T, K, V, true>
+                                                        : conv_rev<T, K, V, false>,
+                                 dim3((unsigned)(l.slabs * l.workers)), kThreads, st, q, l,
+                                 sums ? ws : nullptr);
       if (e != hipSuccess || !sums) return e;
       return start(conv_sum<T>, dim3((unsigned)(((K + 1) * q.D + 63) / 64)), kThreads, st,
                    static_cast<const Acc<T>*>(ws), l.workers, q.D, K, q.dw, q.dbias,
@@ -481,8 +525,14 @@ hipError_t conv_step(const ConvStep& q, hipStream_t st) {
   return by_type(q.dtype, [&](auto t) {
     typedef decltype(t) T;
     constexpr int V = sizeof(T) == 8 ? 1 : sizeof(T) == 4 ? 2 : 4;
-    const int64_t nvec = (q.D + V - 1) / V, groups = (q.B * nvec + kThreads - 1) / kThreads;
-    return start(conv_one<T, V>, dim3((unsigned)groups), kThreads, st, q, nvec);
+    const int64_t nvec = (q.D + V - 1) / V, groups = (nvec + kThreads - 1) / kThreads;
+    for (int64_t b = 0; b < q.B; b += kMostRows) {
+      const int64_t rows = q.B - b < kMostRows ? q.B - b : kMostRows;
+      const hipError_t e = start(conv_one<T, V>, dim3((unsigned)groups, (unsigned)rows), kThreads,
+                                 st, q, b);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   });
 }
 

@@ -486,7 +486,10 @@ __global__ __launch_bounds__(64 * W) void scan_fwd(ScanArgs a, ScanGrid g, void*
       A v[E];
       gather<S>(of_parity(part0, part1, P), at.row, at.c, v);
 #pragma unroll
-      for (int i = 0; i < E; ++i) out.v[i] = down<T>(fma_(skip[i], x[P][i], v[i]) * gate[P][i]);
+      for (int i = 0; i < E; ++i) {
+        const A all = a.D ? fma_(skip[i], x[P][i], v[i]) : v[i];  // (0 x is not 0 for every x)
+        out.v[i] = down<T>(all * gate[P][i]);
+      }
     }
     return out;
   };
@@ -837,7 +840,8 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
           const A of_raw = fma_(u[i], x_[P][i], of_rate(aq[i])) * slope[P][i];
           o.dx.v[i] = down<T>(fma_(s_[P][i], u[i], skip[i] * through_gate));
           o.ddelta.v[i] = down<T>(of_raw);
-          o.dz.v[i] = down<T>(dy * fma_(skip[i], x_[P][i], yp[i]) * of_gate[P][i]);
+          const A all = a.D ? fma_(skip[i], x_[P][i], yp[i]) : yp[i];
+          o.dz.v[i] = down<T>(dy * all * of_gate[P][i]);
           dD[i] = there ? fma_(through_gate, x_[P][i], dD[i]) : dD[i];
           dbias[i] = there ? dbias[i] + of_raw : dbias[i];
         }
@@ -1007,53 +1011,83 @@ __global__ __launch_bounds__(kSumThreads) void scan_sum_a(ScanArgs a, ScanGrid g
 }
 
 // ------------------------------------------------------------------ one step
-// A lane: four neighbouring states of a channel; `lanes` lanes, a power of two, share
-// a channel.
-template <class T>
-__global__ __launch_bounds__(256) void scan_one(ScanStep q, int lanes) {
+// A lane: four neighbouring states of a channel; LANES lanes, a power of two, share a
+// channel. A workgroup's row of the batch is its second index.
+template <int LANES, class A>
+__device__ inline A sum_lanes(A v) {
+  if constexpr (sizeof(A) == 4) {
+    if (LANES > 1) v += permuted<0xb1>(v);
+    if (LANES > 2) v += permuted<0x4e>(v);
+    if (LANES > 4) v += permuted<0x141>(v);
+    if (LANES > 8) v += permuted<0x140>(v);
+    if (LANES > 16) v += __shfl_xor(v, 16, 64);
+  } else {
+#pragma unroll
+    for (int by = 1; by < LANES; by <<= 1) v += __shfl_xor(v, by, 64);
+  }
+  return v;
+}
+// Rows of the batch that a lane takes, whose loads are in flight together.
+constexpr int kStepRows = 2;
+template <class T, int LANES>
+__global__ __launch_bounds__(256) void scan_one(ScanStep q, int64_t row) {
   typedef Acc<T> A;
   const ScanArgs& a = q.a;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int first = (int)(id % lanes) * 4;
-  const int64_t channel = id / lanes, b = channel / a.D_, d = channel % a.D_;
-  const int64_t slot = b < a.B ? (q.slots ? q.slots[b] : b) : -1;
-  const bool on = slot >= 0 && slot < q.nstates;
-  A sum = A(0), x = A(0);
-  if (on) {
-    const int left = a.N - first, n = left < 0 ? 0 : left < 4 ? left : 4;
-    x = up(static_cast<const T*>(a.x)[b * a.sx_b + d]);
-    A s = up(static_cast<const T*>(a.delta)[b * a.sl_b + d]);
-    if (a.bias) s += static_cast<const A*>(a.bias)[d];
-    if (a.softplus) s = softplus(s);
-    const int64_t group = d / (a.D_ / a.G);
-    A* const state = static_cast<A*>(q.state) + (slot * a.D_ + d) * a.N + first;
-    Pack<A, 4> h = load_pack<A, 4>(state, n);
-    const Pack<A, 4> r = load_pack<A, 4>(static_cast<const A*>(a.A) + d * a.N + first, n);
-    const Pack<T, 4> B = load_pack<T, 4>(
-        static_cast<const T*>(a.Bm) + b * a.sb_b + group * a.N + first, n);
-    const Pack<T, 4> C = load_pack<T, 4>(
-        static_cast<const T*>(a.Cm) + b * a.sc_b + group * a.N + first, n);
+  const int first = (int)(threadIdx.x % LANES) * 4;
+  const int64_t d = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const bool channel = d < a.D_;
+  const int left = channel ? a.N - first : 0, n = left < 0 ? 0 : left < 4 ? left : 4;
+  const int64_t c = channel ? d : 0;  // (loads of lanes that have no channel are of the first)
+  const int64_t group = (uint32_t)c / (uint32_t)(a.D_ / a.G);
+  const Pack<A, 4> r = load_pack<A, 4>(static_cast<const A*>(a.A) + c * a.N + first, n);
+  const A bias = a.bias ? static_cast<const A*>(a.bias)[c] : A(0);
+  const A skip = a.D ? static_cast<const A*>(a.D)[c] : A(0);
+  Pack<A, 4> h[kStepRows];
+  Pack<T, 4> B[kStepRows], C[kStepRows];
+  A x[kStepRows], s[kStepRows], z[kStepRows];
+  A* state[kStepRows];
+  bool on[kStepRows];
+  const int64_t b0 = row + (int64_t)blockIdx.y * kStepRows;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) {
-        h.v[i] = fma_(decay(s, rate((A)r.v[i])), (A)h.v[i], s * x * up((T)B.v[i]));
-        sum = fma_(up((T)C.v[i]), (A)h.v[i], sum);
-      }
-    store_pack<A, 4>(state, h, n);
+  for (int k = 0; k < kStepRows; ++k) {
+    const int64_t b = b0 + k < a.B ? b0 + k : b0;
+    const int64_t slot = q.slots ? q.slots[b] : b;
+    on[k] = b0 + k < a.B && slot >= 0 && slot < q.nstates;
+    state[k] = static_cast<A*>(q.state) + ((on[k] ? slot : 0) * a.D_ + c) * a.N + first;
+    const int m = on[k] ? n : 0;
+    h[k] = load_pack<A, 4>(state[k], m);
+    B[k] = load_pack<T, 4>(static_cast<const T*>(a.Bm) + b * a.sb_b + group * a.N + first, m);
+    C[k] = load_pack<T, 4>(static_cast<const T*>(a.Cm) + b * a.sc_b + group * a.N + first, m);
+    x[k] = up(static_cast<const T*>(a.x)[b * a.sx_b + c]);
+    s[k] = up(static_cast<const T*>(a.delta)[b * a.sl_b + c]) + bias;
+    z[k] = a.z ? up(static_cast<const T*>(a.z)[b * a.sz_b + c]) : A(0);
   }
-  for (int by = 1; by < lanes; by <<= 1) sum += __shfl_xor(sum, by, 64);
-  if (first > 0 || b >= a.B || !a.y) return;
-  A v = A(0);
-  if (on) {
-    v = a.D ? fma_(static_cast<const A*>(a.D)[d], x, sum) : sum;
-    if (a.z) {
-      A f, rest;
-      const A z = up(static_cast<const T*>(a.z)[b * a.sz_b + d]);
-      gates<T>(z, &f, &rest);
-      v *= z * f;
+#pragma unroll
+  for (int k = 0; k < kStepRows; ++k) {
+    if (a.softplus) s[k] = softplus(s[k]);
+    A sum = A(0);
+    if (on[k]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < n) {
+          h[k].v[i] = fma_(decay(s[k], rate((A)r.v[i])), (A)h[k].v[i], s[k] * x[k] * up((T)B[k].v[i]));
+          sum = fma_(up((T)C[k].v[i]), (A)h[k].v[i], sum);
+        }
+      store_pack<A, 4>(state[k], h[k], n);
     }
+    sum = sum_lanes<LANES>(sum);
+    if (first > 0 || !channel || b0 + k >= a.B || !a.y) continue;
+    A v = A(0);
+    if (on[k]) {
+      v = a.D ? fma_(skip, x[k], sum) : sum;
+      if (a.z) {
+        A f, rest;
+        gates<T>(z[k], &f, &rest);
+        v *= z[k] * f;
+      }
+    }
+    static_cast<T*>(a.y)[(b0 + k) * a.D_ + d] = down<T>(v);
   }
-  static_cast<T*>(a.y)[b * a.D_ + d] = down<T>(v);
 }
 
 // ------------------------------------------------------------------ launches
@@ -1121,12 +1155,28 @@ hipError_t vjp_of(const ScanArgs& a, const ScanGrid& g, void* ws, hipStream_t st
   });
 }
 
+template <class T, int LANES>
+hipError_t step_with(const ScanStep& q, hipStream_t st) {
+  constexpr int64_t kMostRows = 65535 * kStepRows;  // of a launch's second axis
+  const int64_t of_group = 256 / LANES, groups = (q.a.D_ + of_group - 1) / of_group;
+  for (int64_t b = 0; b < q.a.B; b += kMostRows) {
+    const int64_t rows = q.a.B - b < kMostRows ? q.a.B - b : kMostRows;
+    const dim3 grid((unsigned)groups, (unsigned)((rows + kStepRows - 1) / kStepRows));
+    const hipError_t e = start(scan_one<T, LANES>, grid, 256, st, q, b);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <class T>
 hipError_t step_of(const ScanStep& q, hipStream_t st) {
-  int lanes = 1;
-  while (lanes * 4 < q.a.N) lanes *= 2;
-  const int64_t groups = (q.a.B * q.a.D_ * lanes + 255) / 256;
-  return start(scan_one<T>, dim3((unsigned)groups), 256, st, q, lanes);
+  const int N = q.a.N;
+  if (N <= 4) return step_with<T, 1>(q, st);
+  if (N <= 8) return step_with<T, 2>(q, st);
+  if (N <= 16) return step_with<T, 4>(q, st);
+  if (N <= 32) return step_with<T, 8>(q, st);
+  if (N <= 64) return step_with<T, 16>(q, st);
+  return step_with<T, 32>(q, st);
 }
 
 }  // namespace

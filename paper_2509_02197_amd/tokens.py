@@ -13,7 +13,7 @@ import ctypes
 from . import (ADST_ACT_NONE, ADST_BF16, ADST_CONV_MAX_TAPS, ADST_F16, ADST_F32, _check, _ptr,
                _stream, adst_conv_problem, adst_scan_gradients, adst_scan_info, adst_scan_inputs,
                adst_scan_problem, adst_xent_info, adst_xent_problem, lib)
-from .sequence import (_acc, _at, _bytes, _call, _channels_contiguous, _check_in_place, _code, _codes,
+from .sequence import (_acc, _at, _binding, _bytes, _call, _channels_contiguous, _check_in_place, _code, _codes,
                        _expect, _require)
 
 
@@ -148,6 +148,10 @@ def causal_conv(x, w, b=None, x0=None, lens=None, act=ADST_ACT_NONE, want_y=True
     lens [batch] int32: the steps of each row. x may have any strides with contiguous channels.
     Returns a dict: y (None unless want_y; 0 beyond lens) and xT, the window that follows each
     row: x0 of the next piece of it, or its state for causal_conv_step."""
+    if stream is None:
+        done = _binding().causal_conv(x, w, b, x0, lens, act, want_y)
+        if done is not None:
+            return done
     import torch
     prob = _conv_problem(x, w, b, x0, lens, act)
     B, T, D = x.shape
@@ -166,6 +170,11 @@ def causal_conv_vjp(x, dy, w, b=None, x0=None, lens=None, dxT=None, act=ADST_ACT
                     want_dx=True, want_dw=True, want_db=True, stream=None):
     """The VJP of causal_conv: dy = dL/dy, dxT = dL/dxT (optional). Returns a dict: dx, dw and db
     (in w's dtype), each None unless wanted, and dx0."""
+    if stream is None:
+        done = _binding().causal_conv_vjp(x, dy, w, b, x0, lens, dxT, act, want_dx, want_dw,
+                                          want_db)
+        if done is not None:
+            return done
     import torch
     prob = _conv_problem(x, w, b, x0, lens, act, _given("dy", dy), dxT)
     B, T, D = x.shape
@@ -195,6 +204,10 @@ def causal_conv_step(x, w, window, b=None, slots=None, act=ADST_ACT_NONE, stream
     [nstates, taps - 1, channels] of x's dtype, updated in place. slots [batch] int32: each row's
     window, no two the same; None: row b's is window[b]. Rows whose slot is outside the pool are
     idle: their y is 0. Returns y [batch, channels]."""
+    if stream is None:
+        y = _binding().causal_conv_step(x, w, window, b, slots, act)
+        if y is not None:
+            return y
     import torch
     code = _code("x", x)
     if x.dim() != 2:
@@ -282,6 +295,11 @@ def selective_scan(x, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None, 
     each row. x, delta, z, B and C may have any strides with contiguous channels (groups and
     states). Returns a dict: y (None unless want_y; 0 beyond lens), hT the last states, and ck
     (None unless want_ck) the checkpoints with which selective_scan_vjp recomputes the states."""
+    if stream is None:
+        done = _binding().selective_scan(x, delta, A, B, C, D, z, delta_bias, h0, lens, softplus,
+                                         want_y, want_ck)
+        if done is not None:
+            return done
     import torch
     prob, inputs = _scan_problem(x, delta, A, B, C, D, z, delta_bias, softplus)
     _scan_rows(prob, inputs, x, h0, lens)
@@ -304,6 +322,11 @@ def selective_scan_vjp(x, delta, A, B, C, dy, D=None, z=None, delta_bias=None, h
     """The VJP of selective_scan: dy = dL/dy, dhT = dL/dhT (optional). ck: the checkpoints that
     selective_scan gave for the same inputs; None recomputes them. Returns a dict: dx, ddelta, dz,
     dB, dC, dA, dD, ddelta_bias (each like its input, None without it) and dh0."""
+    if stream is None:
+        done = _binding().selective_scan_vjp(x, delta, A, B, C, dy, D, z, delta_bias, h0, lens, dhT,
+                                             ck, softplus)
+        if done is not None:
+            return done
     import torch
     prob, inputs = _scan_problem(x, delta, A, B, C, D, z, delta_bias, softplus, _given("dy", dy))
     _scan_rows(prob, inputs, x, h0, lens, dhT)
@@ -338,6 +361,11 @@ def selective_scan_step(x, delta, A, B, C, state, D=None, z=None, delta_bias=Non
     float64 inputs), updated in place. slots [batch] int32: each row's state, no two the same;
     None: row b's is state[b]. Rows whose slot is outside the pool are idle: their y is 0. Returns
     y [batch, channels]."""
+    if stream is None:
+        y = _binding().selective_scan_step(x, delta, A, B, C, state, D, z, delta_bias, slots,
+                                           softplus)
+        if y is not None:
+            return y
     import torch
     _code("x", x)
     if x.dim() != 2:
@@ -394,6 +422,10 @@ def linear_cross_entropy(x, w, labels, stream=None):
     loss = lse - logits[label]. labels [rows] int32; a row whose label is outside [0, vocab) (as
     -1 is) has loss 0. The logits are not held. x and w may have any strides between rows. Returns
     a dict: loss and lse [rows], in float32 (float64 for float64 inputs)."""
+    if stream is None:
+        done = _binding().linear_cross_entropy(x, w, labels)
+        if done is not None:
+            return done
     import torch
     prob = _xent_problem(x, w, labels)
     info = adst_linear_cross_entropy_plan(prob)
@@ -417,6 +449,10 @@ def linear_cross_entropy_vjp(x, w, labels, lse, dloss=None, want_dx=True, want_d
     if None). Returns a dict: dx and dw like x and w (contiguous), each None unless wanted. A row
     without a label, or whose dloss is 0, adds nothing to dw, whatever it holds. The logits are
     computed again, for a piece of the vocabulary at a time."""
+    if stream is None:
+        done = _binding().linear_cross_entropy_vjp(x, w, labels, lse, dloss, want_dx, want_dw)
+        if done is not None:
+            return done
     import torch
     prob = _xent_problem(x, w, labels)
     acc = _acc(prob.dtype)

@@ -1,6 +1,7 @@
 /* adst.h — reverse-mode gradients of time-iterated stencil programs under a
  * checkpoint-memory budget, on AMD MI355X (gfx950); and the time loop of a
- * sequence layer with its gradients (the section "Sequence operators").
+ * sequence layer with its gradients (the sections "Sequence operators" and
+ * "Token operators").
  *
  * The operation (DaCe AD, arXiv 2509.02197): given an unmodified time loop
  *     x_t = F(x_{t-1}; K),  t = 1..T,
@@ -670,7 +671,7 @@ typedef struct {
  * those of x0 among them where the row is shorter. lens: as in
  * adst_recurrence_forward; y beyond is 0. Errors: ADST_ERR_ARG (NULL problem, x or
  * w, bad types, extents or strides, overlapping ranges), ADST_ERR_UNSUPPORTED
- * (an extent >= 2^31 - 2^16), ADST_ERR_HIP. */
+ * (batch or steps >= 2^31 - 2^16, channels >= 2^26), ADST_ERR_HIP. */
 adst_status adst_causal_conv_forward(const adst_conv_problem* prob, const void* x, const void* w,
                                      const void* bias, const void* x0, const int32_t* lens,
                                      void* y, void* xT, hipStream_t stream);
@@ -690,7 +691,8 @@ adst_status adst_causal_conv_vjp(const adst_conv_problem* prob, const void* x, c
 
 /* One step of each batch row (prob->steps must be 1) on a pool of windows
  * [nstates][taps-1][channels], updated in place; y [batch][channels] (optional).
- * slots and idle rows: as in adst_recurrence_step. Errors: as the forward. */
+ * slots and idle rows: as in adst_recurrence_step. Errors: as the forward;
+ * ADST_ERR_UNSUPPORTED for batch * channels >= 2^31. */
 adst_status adst_causal_conv_step(const adst_conv_problem* prob, const void* x, const void* w,
                                   const void* bias, const int32_t* slots, void* window,
                                   int64_t nstates, void* y, hipStream_t stream);
@@ -744,7 +746,8 @@ typedef struct {
 } adst_scan_gradients;
 
 typedef struct {
-  int64_t span;                 /* steps between checkpoints */
+  int64_t span;                 /* steps between checkpoints: 16 with up to 16 states, 8 with up
+                                   to 32, 4 with up to 64, 2 beyond (half of that for F64) */
   uint64_t ck_bytes;            /* checkpoints: the states at the start of each span */
   uint64_t workspace_bytes;     /* ws of adst_selective_scan_forward */
   uint64_t vjp_workspace_bytes; /* ws of adst_selective_scan_vjp given checkpoints; ck_bytes
@@ -753,8 +756,9 @@ typedef struct {
 
 /* Sizes of a problem's buffers (host only). They depend on the sizes alone, as
  * the order of all sums does. Errors: ADST_ERR_ARG (NULL, unknown dtype, a bad extent or
- * stride), ADST_ERR_UNSUPPORTED (an extent >= 2^31 - 2^16, more states than
- * above, or more channels and rows than a launch holds). */
+ * stride), ADST_ERR_UNSUPPORTED (batch or steps >= 2^31 - 2^16, channels >=
+ * 2^26, more states than above, or more than a launch holds: about
+ * 2^32 / 16 of batch * channels, and 2^31 of batch * steps * groups * states). */
 adst_status adst_selective_scan_plan(const adst_scan_problem* prob, adst_scan_info* out);
 
 /* y [batch][steps][channels] (contiguous, optional; 0 beyond lens[b]), the last states hT
@@ -778,7 +782,8 @@ adst_status adst_selective_scan_vjp(const adst_scan_problem* prob, const adst_sc
 /* One step of each batch row (prob->steps must be 1; h0 and lens NULL) on a
  * pool of states [nstates][channels][states] in the accumulation type, updated
  * in place; y [batch][channels] (optional). slots and idle rows: as in
- * adst_recurrence_step. Errors: as the forward, without ADST_ERR_WORKSPACE. */
+ * adst_recurrence_step. Errors: as the forward, without ADST_ERR_WORKSPACE;
+ * ADST_ERR_UNSUPPORTED for batch * channels >= 2^26. */
 adst_status adst_selective_scan_step(const adst_scan_problem* prob, const adst_scan_inputs* in,
                                      const int32_t* slots, void* state, int64_t nstates, void* y,
                                      hipStream_t stream);
@@ -805,7 +810,8 @@ typedef struct {
 } adst_xent_info;
 
 /* Host only. Errors: ADST_ERR_ARG (NULL, unknown dtype, a bad extent or
- * stride), ADST_ERR_UNSUPPORTED (an extent >= 2^31 - 2^16). */
+ * stride), ADST_ERR_UNSUPPORTED (rows or vocab times width + 64 >= 2^31, or
+ * rows * vocab >= 2^35). */
 adst_status adst_linear_cross_entropy_plan(const adst_xent_problem* prob, adst_xent_info* out);
 
 /* loss and lse [rows] in the accumulation type (each optional). Errors: as the
@@ -820,8 +826,8 @@ adst_status adst_linear_cross_entropy_forward(const adst_xent_problem* prob, con
  * a row: dx = sum_v g_v * w[v], dw[v] = sum over rows of g_v * x (each
  * optional). lse: the forward call's. dloss: dL/dloss [rows] in the accumulation
  * type (1 if NULL). The logits are computed again; g is held in 16 bits beside 16-bit
- * inputs, scaled by a power of two so that the largest dloss is at the top of
- * the type's range. A row whose dloss is 0, or that has no label, gets a dx of
+ * inputs, scaled so that the largest |dloss| is a power of two (2^14 in F16,
+ * whose least values would be lost otherwise). A row whose dloss is 0, or that has no label, gets a dx of
  * 0. Errors: as the forward. */
 adst_status adst_linear_cross_entropy_vjp(const adst_xent_problem* prob, const void* x,
                                           const void* w, const int32_t* labels, const void* lse,

@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
     if (any) request(first);
     // one step: WHOLE: it is there; OWN: one of the segment's, whose dw and db it adds to, 0 where
     // that is to be asked
-    const auto step = [&](int r, int64_t t, const Pack<T, V>& now, const Pack<T, V>& e, auto whole,
+    const auto step = [&](int64_t t, const Pack<T, V>& now, const Pack<T, V>& e, auto whole,
                           auto own) {
       constexpr bool kWhole = decltype(whole)::value, kOwn = decltype(own)::value;
       if (kWhole || t < most) {
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
       if (any) request(t0 + kBatch);
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
-        step(r, t0 + r, now[r], e[r], whole, own);
+        step(t0 + r, now[r], e[r], whole, own);
         leave(t0 + r, inside);
       }
     };
@@ -455,29 +455,29 @@ hipError_t conv_forward(const ConvArgs& q, hipStream_t st) {
       typedef decltype(t) T;
       constexpr int K = decltype(k)::value;
       return by_lanes<lanes_of<T, K>(false)>(q.D, [&](auto lanes) {
-      constexpr int V = decltype(lanes)::value;
-      const int64_t nvec = (q.D + V - 1) / V;
-      const int segment =
-          nvec * q.B * ((q.T + kSegment - 1) / kSegment) >= kManyThreads ? kSegment : kFewSegment;
-      const int64_t segments = q.y ? (q.T + segment - 1) / segment : 0;
-      // rows of the batch in several launches where one does not hold them
-      const int64_t row = nvec * (segments + 1), rows = kMostGroups * kThreads / row;
-      if (rows < 1) return hipErrorInvalidValue;
-      for (int64_t b = 0; b < q.B; b += rows) {
-        ConvArgs a = q;
-        a.B = q.B - b < rows ? q.B - b : rows;
-        a.x = q.x ? static_cast<const T*>(q.x) + b * q.sx_b : nullptr;
-        a.x0 = q.x0 ? static_cast<const T*>(q.x0) + b * (K - 1) * q.D : nullptr;
-        a.lens = q.lens ? q.lens + b : nullptr;
-        a.y = q.y ? static_cast<T*>(q.y) + b * q.T * q.D : nullptr;
-        a.xT = q.xT ? static_cast<T*>(q.xT) + b * (K - 1) * q.D : nullptr;
-        const unsigned groups = (unsigned)((a.B * row + kThreads - 1) / kThreads);
-        const hipError_t e = start(a.act == ADST_ACT_SILU ? conv_fwd<T, K, V, true>
-                                                          : conv_fwd<T, K, V, false>,
-                                   dim3(groups), kThreads, st, a, nvec, segments, segment);
-        if (e != hipSuccess) return e;
-      }
-      return hipSuccess;
+        constexpr int V = decltype(lanes)::value;
+        const int64_t nvec = (q.D + V - 1) / V;
+        const int segment =
+            nvec * q.B * ((q.T + kSegment - 1) / kSegment) >= kManyThreads ? kSegment : kFewSegment;
+        const int64_t segments = q.y ? (q.T + segment - 1) / segment : 0;
+        // rows of the batch in several launches where one does not hold them
+        const int64_t row = nvec * (segments + 1), rows = kMostGroups * kThreads / row;
+        if (rows < 1) return hipErrorInvalidValue;
+        for (int64_t b = 0; b < q.B; b += rows) {
+          ConvArgs a = q;
+          a.B = q.B - b < rows ? q.B - b : rows;
+          a.x = q.x ? static_cast<const T*>(q.x) + b * q.sx_b : nullptr;
+          a.x0 = q.x0 ? static_cast<const T*>(q.x0) + b * (K - 1) * q.D : nullptr;
+          a.lens = q.lens ? q.lens + b : nullptr;
+          a.y = q.y ? static_cast<T*>(q.y) + b * q.T * q.D : nullptr;
+          a.xT = q.xT ? static_cast<T*>(q.xT) + b * (K - 1) * q.D : nullptr;
+          const unsigned groups = (unsigned)((a.B * row + kThreads - 1) / kThreads);
+          const hipError_t e = start(a.act == ADST_ACT_SILU ? conv_fwd<T, K, V, true>
+                                                            : conv_fwd<T, K, V, false>,
+                                     dim3(groups), kThreads, st, a, nvec, segments, segment);
+          if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
       });
     });
   });
@@ -505,17 +505,17 @@ hipError_t conv_vjp(const ConvArgs& q, void* ws, hipStream_t st) {
       typedef decltype(t) T;
       constexpr int K = decltype(k)::value;
       return by_lanes<lanes_of<T, K>(true)>(q.D, [&](auto lanes) {
-      constexpr int V = decltype(lanes)::value;
-      const Layout l = layout_of(q.B, q.T, q.D, V);
-      const bool sums = q.dw || q.dbias;
-      const hipError_t e = start(q.act == ADST_ACT_SILU ? conv_rev<T, K, V, true>
-                                                        : conv_rev<T, K, V, false>,
-                                 dim3((unsigned)(l.slabs * l.workers)), kThreads, st, q, l,
-                                 sums ? ws : nullptr);
-      if (e != hipSuccess || !sums) return e;
-      return start(conv_sum<T>, dim3((unsigned)(((K + 1) * q.D + 63) / 64)), kThreads, st,
-                   static_cast<const Acc<T>*>(ws), l.workers, q.D, K, q.dw, q.dbias,
-                   q.wtype == q.dtype);
+        constexpr int V = decltype(lanes)::value;
+        const Layout l = layout_of(q.B, q.T, q.D, V);
+        const bool sums = q.dw || q.dbias;
+        const hipError_t e = start(q.act == ADST_ACT_SILU ? conv_rev<T, K, V, true>
+                                                          : conv_rev<T, K, V, false>,
+                                   dim3((unsigned)(l.slabs * l.workers)), kThreads, st, q, l,
+                                   sums ? ws : nullptr);
+        if (e != hipSuccess || !sums) return e;
+        return start(conv_sum<T>, dim3((unsigned)(((K + 1) * q.D + 63) / 64)), kThreads, st,
+                     static_cast<const Acc<T>*>(ws), l.workers, q.D, K, q.dw, q.dbias,
+                     q.wtype == q.dtype);
       });
     });
   });

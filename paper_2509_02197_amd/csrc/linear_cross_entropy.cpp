@@ -18,8 +18,8 @@ constexpr int64_t kPieceBytes = 128 << 20;
 // may be split: what takes the least time by the work of the CU that has the most
 // tiles. The rates are those of large products measured here (F32 128, F64 55 TFLOP/s, and
 // 1050 of 16-bit types with 256 x 256 tiles); smaller tiles read more of LDS for each
-// product, and a CU with less than two waves a SIMD waits for its loads (999 x 515 x 10007 F32:
-// forward 135 us with 128 x 128 tiles, 3 on the fullest CU, and 115 with 128 x 64).
+// product, and a CU with less than two waves a SIMD waits for its loads. (999 x 515 x 10007 F32:
+// the whole step 590 us with 128 x 128 tiles everywhere, 555 with the ones chosen here.)
 XentPlan::Product product_of(int64_t e, int64_t m, int64_t n, int64_t steps, bool split) {
   static const struct {
     int64_t bm, bn, waves;

@@ -410,7 +410,8 @@ hipError_t by_tiles(int tiles, F f) {
 template <class T>
 bool whole_pieces(const void* p, int64_t stride, int64_t K) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (int64_t)sizeof(T) % 16 == 0 &&
-         K * (int64_t)sizeof(T) % kStepBytes == 0 && stride < (int64_t(1) << 28);
+         K * (int64_t)sizeof(T) % kStepBytes == 0 &&
+         stride < (int64_t(1) << 29) / (int64_t)sizeof(T);  // offsets of 7 rows in 32 bits
 }
 
 template <class T>

@@ -8,7 +8,8 @@ namespace {
 
 int64_t up_to(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
-// Waves that fill the card's 1024 SIMDs, and segments at least this long in steps.
+// Segments are cut below kEnoughWaves of the card's 1024 SIMDs, into kWaves, and are at least
+// kLeastSegment steps long.
 constexpr int64_t kEnoughWaves = 768, kWaves = 2048, kLeastSegment = 128;
 
 }  // namespace
@@ -29,8 +30,10 @@ ScanGrid scan_grid(int32_t dtype, int64_t B, int64_t T, int64_t D, int64_t N, in
   g.chunks = up_to(T, g.chunk);
   g.group_slabs = up_to(D / G, g.slab);
   g.slabs = g.group_slabs * G;
-  // Segments only where the batch's rows and channels leave SIMDs without work: a
-  // segment's map is a second sweep over its inputs.
+  // Segments only where the batch's rows and channels leave SIMDs without work: a segment's
+  // map is a second sweep over its inputs. 6 x 777 x 1000 F16 of 16 states, 768 waves: 63 us
+  // in one segment, 52 + 29 (map) in two, 37 + 29 in four. 1 x 16384 x 2048 bf16, 256 waves:
+  // 152 + 211 in eight; a wave of one segment has four times the steps of 4 x 4096 x 2048's 301.
   const int64_t waves = g.slabs * B * g.waves;
   int64_t segments = 1;
   if (waves > 0 && waves < kEnoughWaves) {

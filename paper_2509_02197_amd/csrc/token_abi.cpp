@@ -100,13 +100,8 @@ adst_status check_scan(const adst_scan_problem* p, ScanGrid* grid) {
   if (p->channels % p->groups != 0) return fail(ADST_ERR_ARG, "groups must divide channels");
   if (Wide(p->batch) * p->channels * (p->steps + 16) * p->states > (Wide(1) << 52))
     return fail(ADST_ERR_UNSUPPORTED, "more values than the address space");
-  if (p->channels > 0) {
-    *grid = scan_grid(p->dtype, p->batch, p->steps, p->channels, p->states, p->groups);
-    if (!grid->fits) return fail(ADST_ERR_UNSUPPORTED, "more rows and channels than a launch holds");
-  } else {
-    *grid = ScanGrid{};
-    grid->chunk = 16;
-  }
+  *grid = scan_grid(p->dtype, p->batch, p->steps, p->channels, p->states, p->groups);
+  if (!grid->fits) return fail(ADST_ERR_UNSUPPORTED, "more rows and channels than a launch holds");
   return ADST_OK;
 }
 
@@ -380,8 +375,10 @@ adst_status adst_selective_scan_vjp(const adst_scan_problem* prob, const adst_sc
   Ranges rs;
   CHECK(scan_inputs(prob, in, &rs));
   const bool some = p.batch > 0 && p.steps > 0 && p.channels > 0;
-  if (some && (!dy || !out->dx || !out->ddelta || !out->dB || !out->dC))
-    return fail(ADST_ERR_ARG, "dy, dx, ddelta, dB and dC are required");
+  if (some && (!dy || !out->dx || !out->ddelta))
+    return fail(ADST_ERR_ARG, "dy, dx and ddelta are required");
+  if (p.batch > 0 && p.steps > 0 && (!out->dB || !out->dC))
+    return fail(ADST_ERR_ARG, "dB and dC are required");
   if (p.channels > 0 && (!in->A || !out->dA)) return fail(ADST_ERR_ARG, "A and dA are required");
   if (some && in->z && !out->dz) return fail(ADST_ERR_ARG, "dz is required with z");
   if (!in->z && out->dz) return fail(ADST_ERR_ARG, "dz without z");
@@ -420,7 +417,8 @@ adst_status adst_selective_scan_vjp(const adst_scan_problem* prob, const adst_sc
   if (need) CHECK(check_aligned("ws", ws, 16));
   if (need) rs.out("ws", ws, need);
   CHECK(rs.check());
-  if (p.channels == 0) return report_ok();
+  // without channels dB and dC, sums over them, are still to be cleared
+  if (p.channels == 0 && (p.batch == 0 || p.steps == 0)) return report_ok();
   ScanArgs a = scan_args(prob, in);
   if (!ck) {  // the checkpoints again
     a.ck = static_cast<char*>(ws) + given;

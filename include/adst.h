@@ -828,7 +828,7 @@ adst_status adst_linear_cross_entropy_forward(const adst_xent_problem* prob, con
  * type (1 if NULL). The logits are computed again; g is held in 16 bits beside 16-bit
  * inputs, scaled so that the largest |dloss| is a power of two (2^14 in F16,
  * whose least values would be lost otherwise). A row whose dloss is 0, or that has no label, gets a dx of
- * 0. Errors: as the forward. */
+ * 0 (of a finite w), whatever it holds. Errors: as the forward. */
 adst_status adst_linear_cross_entropy_vjp(const adst_xent_problem* prob, const void* x,
                                           const void* w, const int32_t* labels, const void* lse,
                                           const void* dloss, void* dx, void* dw, void* ws,

@@ -411,7 +411,7 @@ template <class T>
 bool whole_pieces(const void* p, int64_t stride, int64_t K) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (int64_t)sizeof(T) % 16 == 0 &&
          K * (int64_t)sizeof(T) % kStepBytes == 0 &&
-         stride < (int64_t(1) << 29) / (int64_t)sizeof(T);  // offsets of 7 rows in 32 bits
+         stride < (int64_t(1) << 28) / (int64_t)sizeof(T);  // offsets of 7 rows in 31 bits
 }
 
 template <class T>
@@ -427,6 +427,7 @@ hipError_t forward_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_
                          at + p.stats, at + p.target);
     if (e != hipSuccess) return e;
     const void *stats = at + p.stats, *target = at + p.target;
+    // (few rows: a wave for each, whose lanes take the tiles' statistics at once)
     if (a.M < 2048)
       return start(xent_join<T, 64>, dim3((unsigned)parts(a.M * 64, kJoinThreads)), kJoinThreads,
                    st, stats, target, a.labels, a.M, a.V, t.n, a.loss, a.lse);

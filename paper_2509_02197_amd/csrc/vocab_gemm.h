@@ -128,8 +128,8 @@ struct Behind {
 };
 
 // Steps first .. end of k into s.acc, for the tile whose first rows of A and B are m0, n0.
-// DIRECT: k is whole steps, rows and their starts are multiples of 16 bytes. Eight rows span
-// less than 2^32 bytes.
+// DIRECT: k is whole steps, rows and their starts are multiples of 16 bytes, rows less than
+// 2^28 bytes apart.
 template <class S, bool DIRECT>
 __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, int64_t K,
                                 int64_t m0, int64_t n0, int64_t first, int64_t end) {
@@ -195,8 +195,8 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
   };
   if constexpr (DIRECT) {
     // While a half of a step is multiplied the next half is read from LDS, across the
-    // barrier between steps too. (8192 x 8192 x 2048 bf16: 232 us, 254
-    // read where they are used.)
+    // barrier between steps too. (8192 x 8192 x 2048 bf16: 232 us, and 254
+    // where they are read as they are used.)
     const uint32_t base = lds_at(lds);
     const auto request = [&](int stage) {
 #pragma unroll

@@ -331,8 +331,7 @@ def selective_scan_vjp(x, delta, A, B, C, dy, D=None, z=None, delta_bias=None, h
     prob, inputs = _scan_problem(x, delta, A, B, C, D, z, delta_bias, softplus, _given("dy", dy))
     _scan_rows(prob, inputs, x, h0, lens, dhT)
     info = adst_selective_scan_plan(prob)
-    if ck is not None or info.ck_bytes == 0:
-        _expect("ck", ck, (info.ck_bytes,), torch.uint8, x.device)
+    _expect("ck", ck, (info.ck_bytes,), torch.uint8, x.device)
     need = info.vjp_workspace_bytes + (0 if ck is not None else info.ck_bytes)
 
     def body(handle):

@@ -155,10 +155,13 @@ def test_strides(how, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_rows_gigabytes_apart(dtype):
-    """Offsets of neighbouring rows that pass 32 bits, within a wave's eight rows too."""
+@pytest.mark.parametrize("bits", [28, 27, 26])
+def test_rows_gigabytes_apart(bits, dtype):
+    """Offsets of neighbouring rows that pass 32 bits, within a wave's eight rows too; strides on
+    both sides of 2^28 bytes."""
     s = make(9, 64, 11, dtype)
-    for k, stride in (("x", 1 << 28), ("w", (1 << 28) - 64)):
+    for k, stride in (("x", 1 << bits), ("w", 1 << bits)) if bits > 27 else \
+            (("x", (1 << bits) - 64), ("w", (1 << bits) - 128)):
         rows = s[k].shape[0]
         flat = torch.empty((rows - 1) * stride + 64, dtype=dtype, device="cuda")
         far = flat.as_strided((rows, 64), (stride, 1))

@@ -324,7 +324,7 @@ __device__ inline void through(const Maps<A>& m, const ScanArgs& a, const ScanGr
 // In LDS a chunk's prepared inputs and sums have a place for each parity of the chunk's
 // number: while a chunk is swept the next one is prepared and the one before is finished,
 // in one stretch of independent instructions between two barriers. (4 x 4096 x 2048 bf16
-// of 16 states: 301 us forward and 833 in reverse, 323 and 930 with a barrier after each of the
+// of 16 states: 301 us forward and 852 in reverse, 323 and 949 with a barrier after each of the
 // three: a SIMD has one wave there, so what a wave waits for nothing hides.) The arrays are variables of
 // their own, so that the compiler knows that they do not overlap.
 //
@@ -651,17 +651,33 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
   const Loader<S, FULL> at(p);
   const Lane l = lane_of<S>(a, p);
   const int64_t d = p.d0 + l.c;
-  A rates[NS], dA[NS];
+  A rates[NS];
 #pragma unroll
-  for (int i = 0; i < NS; ++i) {
+  for (int i = 0; i < NS; ++i)
     rates[i] = i < l.count ? rate(static_cast<const A*>(a.A)[d * a.N + l.first + i]) : A(0);
-    dA[i] = A(0);
-  }
-  A skip[E], bias[E], dD[E], dbias[E];
+  A skip[E], bias[E];
   at.constants(a.D, p.d0, skip);
   at.constants(a.bias, p.d0, bias);
+  // Sums over steps, a few chunks' at a time: one sum over thousands of steps is 1.5 times as
+  // far off (dA of 4 x 4096 x 2048 bf16: 2.7e-6 of it, two levels 1.9e-6; 852 us, not 833).
+  A dA[NS], dD[E], dbias[E], all_dA[NS], all_dD[E], all_dbias[E];
 #pragma unroll
-  for (int i = 0; i < E; ++i) dD[i] = dbias[i] = A(0);
+  for (int i = 0; i < NS; ++i) dA[i] = all_dA[i] = A(0);
+#pragma unroll
+  for (int i = 0; i < E; ++i) dD[i] = dbias[i] = all_dD[i] = all_dbias[i] = A(0);
+  const auto keep_sums = [&] {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      all_dA[i] += dA[i];
+      dA[i] = A(0);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      all_dD[i] += dD[i];
+      all_dbias[i] += dbias[i];
+      dD[i] = dbias[i] = A(0);
+    }
+  };
   const Maps<A> maps(ws, a, g);
   const Sums<A> sums(sums_ws, a.B, a.D_, a.N, g);
   for (p.b = row; p.b < a.B; p.b += MAP ? a.B : g.rows) {
@@ -908,6 +924,7 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
       for (t -= 2 * R; t > t0; t -= 2 * R) {
         turn(odd, Parity<0>(), false, t);
         turn(even, Parity<1>(), false, t - R);
+        if (!MAP && (t - t0) / R % 8 == 1) keep_sums();
       }
       store(finish(Parity<1>(), true), t0, true);
       __syncthreads();  // the next row's chunks take its place
@@ -920,6 +937,7 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
       if (l.channel && l.group == 0) maps.s[(p.b * g.segments + p.segment) * a.D_ + d] = total;
       return;
     }
+    keep_sums();
     if (p.segment == 0 && a.out.dh0)
 #pragma unroll
       for (int i = 0; i < NS; ++i)
@@ -940,15 +958,15 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
   const int64_t part = row * g.segments + p.segment;
 #pragma unroll
   for (int i = 0; i < NS; ++i)
-    if (i < l.count) sums.a[(part * a.N + l.first + i) * a.D_ + d] = dA[i];
+    if (i < l.count) sums.a[(part * a.N + l.first + i) * a.D_ + d] = all_dA[i];
   // the loaders' sums of a channel, step after step of the chunk
   A(*const rows_of)[2][kSlab] = reinterpret_cast<A(*)[2][kSlab]>(&part0[0][0][0][0]);
   __syncthreads();
   if (threadIdx.x < S::kLoaders)
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      rows_of[at.row][0][at.c + i] = dD[i];
-      rows_of[at.row][1][at.c + i] = dbias[i];
+      rows_of[at.row][0][at.c + i] = all_dD[i];
+      rows_of[at.row][1][at.c + i] = all_dbias[i];
     }
   __syncthreads();
   if (threadIdx.x < 2 * kSlab && (int)threadIdx.x % kSlab < p.channels) {

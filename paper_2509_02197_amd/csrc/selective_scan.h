@@ -325,8 +325,8 @@ __device__ inline void through(const Maps<A>& m, const ScanArgs& a, const ScanGr
 // number: while a chunk is swept the next one is prepared and the one before is finished,
 // in one stretch of independent instructions between two barriers. (4 x 4096 x 2048 bf16
 // of 16 states: 301 us forward and 852 in reverse, 323 and 949 with a barrier after each of the
-// three: a SIMD has one wave there, so what a wave waits for nothing hides.) The arrays are variables of
-// their own, so that the compiler knows that they do not overlap.
+// three: a SIMD has one wave there, so what a wave waits for nothing hides.) The arrays are
+// variables of their own, so that the compiler knows that they do not overlap.
 //
 // A sweep's LDS reads go a batch of steps ahead of its arithmetic, held there by
 // scheduling barriers.

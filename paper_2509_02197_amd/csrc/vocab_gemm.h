@@ -21,8 +21,8 @@ typedef float F4 __attribute__((ext_vector_type(4)));
 typedef double D4 __attribute__((ext_vector_type(4)));
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
 
-// 16 x 16 of C from 16 rows' pieces of 16 bytes, in kParts instructions. at(lane, i): the row of a lane's
-// value i; its column is lane % 16.
+// 16 x 16 of C from 16 rows' pieces of 16 bytes, in kParts instructions. at(lane, i): the row of
+// a lane's value i; its column is lane % 16.
 template <class T>
 struct Tile;
 template <>
@@ -89,6 +89,8 @@ struct GemmShape {
   static constexpr int kStep = kStepBytes / (int)sizeof(T);  // elements of k
   static constexpr int kStageBytes = (BM + BN) * kStepBytes;
   static constexpr int kLoads = kStageBytes / 16 / kThreads;  // of a thread, per step
+  // Steps that are on their way in registers where they cannot go to LDS directly.
+  static constexpr int kHold = BM * BN <= 64 * 64 ? 3 : BM * BN <= 128 * 128 ? 2 : 1;
   static_assert(kStageBytes % (16 * kThreads) == 0 && BM % 8 == 0, "");
   typename Tile<T>::C acc[MT][NT];
 };
@@ -250,35 +252,42 @@ __device__ inline void multiply(S& s, char* lds, const Rows& A, const Rows& B, i
       stage = next;
     }
   } else {
-    Vec<T> hold[S::kLoads];
-    const auto request = [&](int64_t k) {
+    // Through registers, kHold steps ahead; two stages of LDS are in use.
+    constexpr int D = S::kHold;
+    Vec<T> hold[D][S::kLoads];
+    const auto request = [&](Vec<T>(&to)[S::kLoads], int64_t k) {
 #pragma unroll
       for (int j = 0; j < S::kLoads; ++j) {
         const int64_t left = K - k * S::kStep - piece * Vec<T>::N;
-        hold[j] = load_part(reinterpret_cast<const T*>(from[j] + offset[j]),
-                            (int)(left < 0 ? 0 : left < Vec<T>::N ? left : Vec<T>::N));
+        to[j] = load_part(reinterpret_cast<const T*>(from[j] + offset[j]),
+                          (int)(left < 0 ? 0 : left < Vec<T>::N ? left : Vec<T>::N));
         from[j] += kStepBytes;
       }
     };
-    const auto put = [&](char* stage) {
 #pragma unroll
-      for (int j = 0; j < S::kLoads; ++j)
-        *reinterpret_cast<U4*>(stage + (j * kWaves + wave) * 1024 + lane * 16) =
-            __builtin_bit_cast(U4, hold[j].v);
-    };
-    request(first);
-    put(lds);
-    for (int64_t k = first; k < end; ++k) {
-      const int stage = (int)((k - first) & 1);
-      __syncthreads();
-      if (k + 1 < end) request(k + 1);
+    for (int d = 0; d < D; ++d)
+      if (first + d < end) request(hold[d], first + d);
+    char *here = lds, *other = lds + S::kStageBytes;
+    for (int64_t k0 = first; k0 < end; k0 += D)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        read(lds + stage * S::kStageBytes, h);
-        compute(h);
+      for (int d = 0; d < D; ++d) {
+        const int64_t k = k0 + d;
+        if (k >= end) break;
+#pragma unroll
+        for (int j = 0; j < S::kLoads; ++j)
+          *reinterpret_cast<U4*>(here + (j * kWaves + wave) * 1024 + lane * 16) =
+              __builtin_bit_cast(U4, hold[d][j].v);
+        if (k + D < end) request(hold[d], k + D);
+        __syncthreads();  // and every wave has read the step before, whose stage is next
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          read(here, h);
+          compute(h);
+        }
+        char* const next = other;
+        other = here;
+        here = next;
       }
-      if (k + 1 < end) put(lds + (stage ^ 1) * S::kStageBytes);
-    }
   }
   __syncthreads();  // LDS is free
 }

@@ -13,8 +13,8 @@ import ctypes
 from . import (ADST_ACT_NONE, ADST_BF16, ADST_CONV_MAX_TAPS, ADST_F16, ADST_F32, _check, _ptr,
                _stream, adst_conv_problem, adst_scan_gradients, adst_scan_info, adst_scan_inputs,
                adst_scan_problem, adst_xent_info, adst_xent_problem, lib)
-from .sequence import (_acc, _at, _binding, _bytes, _call, _channels_contiguous, _check_in_place, _code, _codes,
-                       _expect, _require)
+from .sequence import (_acc, _at, _binding, _bytes, _call, _channels_contiguous, _check_in_place,
+                       _code, _codes, _expect, _require)
 
 
 # ------------------------------------------------------------ the C calls

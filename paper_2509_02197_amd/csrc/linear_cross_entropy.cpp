@@ -49,6 +49,16 @@ XentPlan::Product product_of(int64_t e, int64_t m, int64_t n, int64_t steps, boo
   return best;
 }
 
+// The logits' product: split, into tiles of 64 x 64, where those are fewer than a quarter of the
+// CUs and have at least 16 steps each, which one after another take longer than the two
+// launches more.
+XentPlan::Product logits_of(int64_t e, int64_t M, int64_t V, int64_t steps) {
+  const int64_t count = parts(M, 64) * parts(V, 64);
+  if (count > 64 || steps < 16) return product_of(e, M, V, steps, false);
+  const int64_t fill = 256 / count;
+  return {3, fill < steps / 4 ? fill : steps / 4};
+}
+
 }  // namespace
 
 XentPlan xent_plan(int32_t dtype, int64_t M, int64_t V, int64_t K, bool reverse) {
@@ -62,8 +72,13 @@ XentPlan xent_plan(int32_t dtype, int64_t M, int64_t V, int64_t K, bool reverse)
     at += (uint64_t)up_to(bytes, 256);
     return here;
   };
-  p.logits = product_of(e, M, V, parts(K, step), false);
+  p.logits = logits_of(e, M, V, parts(K, step));
+  if (p.logits.splits > 1) p.few = take(p.logits.splits * M * V * acc);
   if (!reverse) {
+    if (p.logits.splits > 1) {
+      p.bytes = at;
+      return p;
+    }
     p.stats = take(parts(V, 64) * M * 2 * acc);
     p.target = take(M * acc);
     p.bytes = at;
@@ -74,7 +89,8 @@ XentPlan xent_plan(int32_t dtype, int64_t M, int64_t V, int64_t K, bool reverse)
   p.pieces = parts(V, most);
   p.piece = up_to(parts(V, p.pieces), p.pieces > 1 ? 256 : step);
   p.pieces = parts(V, p.piece);
-  p.logits = product_of(e, M, p.piece, parts(K, step), false);
+  // (few logits are one piece)
+  if (p.logits.splits == 1) p.logits = product_of(e, M, p.piece, parts(K, step), false);
   p.dx = product_of(e, M, K, p.piece / step, true);
   p.dw = product_of(e, p.piece, K, p.m_pad / step, true);
   p.dx_direct = p.pieces == 1 && p.dx.splits == 1;

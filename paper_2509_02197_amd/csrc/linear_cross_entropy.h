@@ -326,7 +326,7 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad(Rows x, Rows w, Tiles t
                 [&](int i, int r, int j) { return down<T>(s.acc[i][j][r]); });
 }
 
-// C [rows][n] from a product of whole steps: rounded to `out`, or added to (`add`: after
+// C [rows][n] from a product (DIRECT: of whole steps): rounded to `out`, or added to (`add`: after
 // earlier pieces) its split's sums [split][rows][n].
 struct OutArgs {
   void* out;
@@ -334,7 +334,7 @@ struct OutArgs {
   const float* scale;
   bool add;
 };
-template <class S>
+template <class S, bool DIRECT>
 __global__ __launch_bounds__(S::kThreads) void xent_product(Rows a, Rows b, Tiles t, OutArgs q) {
   typedef typename S::T T;
   typedef Acc<T> A;
@@ -344,8 +344,8 @@ __global__ __launch_bounds__(S::kThreads) void xent_product(Rows a, Rows b, Tile
   const TileAt tile = tile_at(t.m, t.n, blockIdx.x / t.splits);
   const int64_t m0 = tile.m * S::BM, n0 = tile.n * S::BN;
   S s;
-  multiply<S, true>(s, lds, a, b, t.K, m0, n0, t.steps * split / t.splits,
-                    t.steps * (split + 1) / t.splits);
+  multiply<S, DIRECT>(s, lds, a, b, t.K, m0, n0, t.steps * split / t.splits,
+                      t.steps * (split + 1) / t.splits);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
   if (q.out) {
@@ -390,6 +390,89 @@ __global__ __launch_bounds__(256) void xent_sum(const void* sums, int64_t n, int
   static_cast<T*>(out)[i] = down<T>(scale ? v * (A)scale[1] : v);
 }
 
+// --------------------------------------------------------------- few logits
+// Where the tiles of the logits are fewer than the CUs and the rows long, the product is
+// split along them, into sums in memory [split][row][word], and what follows a product is a
+// kernel of its own (5 x 4014 over 728 words F32, 12 tiles of 126 steps: 107 us in one part).
+template <class A>
+__device__ inline A few_logit(const A* sums, int64_t splits, int64_t all, int64_t at) {
+  A v = A(0);
+#pragma unroll 8
+  for (int64_t k = 0; k < splits; ++k) v += sums[k * all + at];
+  return v;
+}
+
+// loss and lse: NT threads a row.
+template <class T, int NT>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void xent_few_stats(
+    const void* sums, int64_t splits, const int32_t* labels, int64_t M, int64_t V, void* loss,
+    void* lse) {
+  typedef Acc<T> A;
+  constexpr int kRows = NT < 256 ? 256 / NT : 1, kWaves = NT / 64;
+  __shared__ Stat<A> part[kWaves];
+  __shared__ A part_target[kWaves];
+  const int lane = threadIdx.x % NT;
+  const int64_t m = (int64_t)blockIdx.x * kRows + threadIdx.x / NT, row = m < M ? m : M - 1;
+  const int64_t label = labels[row];
+  const A* const from = static_cast<const A*>(sums) + row * V;
+  Stat<A> all = {A(-__builtin_inf()), A(0)};
+  A target = A(0);
+  for (int64_t n = lane; n < V; n += NT) {
+    const A v = few_logit(from, splits, M * V, n);
+    if (n == label) target = v;
+    const A top = larger(v, all.top);
+    all = {top, relative_to(pivot(top), all) + exp_(v - pivot(top))};
+  }
+  const auto join = [&](Stat<A> other) {
+    const A top = larger(other.top, all.top), at = pivot(top);
+    all = {top, relative_to(at, all) + relative_to(at, other)};
+  };
+#pragma unroll
+  for (int by = 1; by < 64; by <<= 1) {
+    join({__shfl_xor(all.top, by, 64), __shfl_xor(all.sum, by, 64)});
+    target += __shfl_xor(target, by, 64);
+  }
+  if constexpr (kWaves > 1) {
+    if (lane % 64 == 0) {
+      part[lane / 64] = all;
+      part_target[lane / 64] = target;
+    }
+    __syncthreads();
+    if (lane > 0) return;
+    all = part[0];
+    target = part_target[0];
+    for (int k = 1; k < kWaves; ++k) {
+      join(part[k]);
+      target += part_target[k];
+    }
+  }
+  if (m >= M || lane > 0) return;
+  const A v = pivot(all.top) + log_(all.sum);
+  if (lse) static_cast<A*>(lse)[m] = v;
+  if (loss) static_cast<A*>(loss)[m] = label >= 0 && label < V ? v - target : A(0);
+}
+
+// g of the whole vocabulary in both orders, as xent_grad leaves it. A thread: one value.
+template <class T>
+__global__ __launch_bounds__(256) void xent_few_grad(const void* sums, int64_t splits, int64_t M,
+                                                     GArgs q) {
+  typedef Acc<T> A;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= q.m_pad * q.piece) return;
+  const int64_t m = id / q.piece, n = id % q.piece;
+  A v = A(0);
+  if (m < M && n < q.V) {
+    const A weight = row_weight<A>(q.labels, q.dloss, m, q.V) * (q.scale ? (A)q.scale[0] : A(1));
+    if (weight != A(0)) {
+      const A logit = few_logit(static_cast<const A*>(sums), splits, M * q.V, m * q.V + n);
+      v = (exp_(logit - static_cast<const A*>(q.lse)[m]) - (n == q.labels[m] ? A(1) : A(0))) *
+          weight;
+    }
+  }
+  if (m < M) static_cast<T*>(q.g)[m * q.piece + n] = down<T>(v);
+  static_cast<T*>(q.gt)[n * q.m_pad + m] = down<T>(v);
+}
+
 // ------------------------------------------------------------------ launches
 inline int64_t parts(int64_t n, int64_t by) { return (n + by - 1) / by; }
 template <class S>
@@ -414,11 +497,34 @@ bool whole_pieces(const void* p, int64_t stride, int64_t K) {
          stride < (int64_t(1) << 28) / (int64_t)sizeof(T);  // offsets of 7 rows in 31 bits
 }
 
+// The logits' sums of a plan with few of them.
+template <class T>
+hipError_t few_logits(const XentArgs& a, const XentPlan& p, const Rows& x, const Rows& w,
+                      bool direct, void* sums, hipStream_t st) {
+  return by_tiles<T>(p.logits.tiles, [&](auto shape) {
+    typedef decltype(shape) S;
+    const Tiles t = tiles_of<S>(a.M, a.V, a.K, p.logits.splits);
+    return start(direct ? xent_product<S, true> : xent_product<S, false>,
+                 dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, x, w, t,
+                 OutArgs{nullptr, sums, nullptr, false});
+  });
+}
+
 template <class T>
 hipError_t forward_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st) {
   char* const at = static_cast<char*>(ws);
   const bool direct = whole_pieces<T>(a.x, a.sx, a.K) && whole_pieces<T>(a.w, a.sw, a.K);
   const Rows x{a.x, a.sx, a.M}, w{a.w, a.sw, a.V};
+  if (p.logits.splits > 1) {
+    const hipError_t e = few_logits<T>(a, p, x, w, direct, at + p.few, st);
+    if (e != hipSuccess) return e;
+    const void* const sums = at + p.few;
+    if (a.V <= 256)
+      return start(xent_few_stats<T, 64>, dim3((unsigned)parts(a.M, 4)), 256, st, sums,
+                   p.logits.splits, a.labels, a.M, a.V, a.loss, a.lse);
+    return start(xent_few_stats<T, 1024>, dim3((unsigned)a.M), 1024, st, sums, p.logits.splits,
+                 a.labels, a.M, a.V, a.loss, a.lse);
+  }
   return by_tiles<T>(p.logits.tiles, [&](auto shape) {
     typedef decltype(shape) S;
     const Tiles t = tiles_of<S>(a.M, a.V, a.K, 1);
@@ -463,12 +569,20 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
     const bool direct = whole_pieces<T>(x.p, x.stride, a.K) && whole_pieces<T>(w.p, w.stride, a.K);
     const GArgs q{a.labels, a.lse, a.dloss, scale, v0, a.V, p.piece, p.m_pad, at + p.g, at + p.gt};
     // the products' long axes: this piece's words, and the rows, in whole steps
-    e = by_tiles<T>(p.logits.tiles, [&](auto shape) {
-      typedef decltype(shape) S;
-      Tiles t = tiles_of<S>(p.m_pad, p.piece, a.K, 1);
-      return start(direct ? xent_grad<S, true> : xent_grad<S, false>, dim3((unsigned)(t.m * t.n)),
-                   S::kThreads, st, x, w, t, q);
-    });
+    if (p.logits.splits > 1) {
+      e = few_logits<T>(a, p, x, w, direct, at + p.few, st);
+      if (e != hipSuccess) return e;
+      const void* const logits = at + p.few;
+      e = start(xent_few_grad<T>, dim3((unsigned)parts(p.m_pad * p.piece, 256)), 256, st, logits,
+                p.logits.splits, a.M, q);
+    } else {
+      e = by_tiles<T>(p.logits.tiles, [&](auto shape) {
+        typedef decltype(shape) S;
+        const Tiles t = tiles_of<S>(p.m_pad, p.piece, a.K, 1);
+        return start(direct ? xent_grad<S, true> : xent_grad<S, false>,
+                     dim3((unsigned)(t.m * t.n)), S::kThreads, st, x, w, t, q);
+      });
+    }
     if (e != hipSuccess) return e;
     if (a.dw) {
       const Rows gt{at + p.gt, p.m_pad, words}, xt{at + p.xt, p.m_pad, a.K};
@@ -477,7 +591,7 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
       e = by_tiles<T>(p.dw.tiles, [&](auto shape) {
         typedef decltype(shape) S;
         const Tiles t = tiles_of<S>(words, a.K, p.m_pad, p.dw.splits);
-        return start(xent_product<S>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, gt,
+        return start(xent_product<S, true>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, gt,
                      xt, t, OutArgs{split ? nullptr : out, at + p.dw_sums, scale, false});
       });
       if (e != hipSuccess) return e;
@@ -496,7 +610,7 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
       e = by_tiles<T>(p.dx.tiles, [&](auto shape) {
         typedef decltype(shape) S;
         const Tiles t = tiles_of<S>(a.M, a.K, p.piece, p.dx.splits);
-        return start(xent_product<S>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, g,
+        return start(xent_product<S, true>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, g,
                      wt, t, OutArgs{p.dx_direct ? a.dx : nullptr, at + p.dx_sums, scale, v0 > 0});
       });
       if (e != hipSuccess) return e;

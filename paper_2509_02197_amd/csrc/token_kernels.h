@@ -141,6 +141,7 @@ struct XentPlan {
   } logits, dx, dw;
   bool dx_direct;          // dx leaves its product in the element type
   uint64_t stats, target, scale, xt, wt, g, gt, dx_sums, dw_sums;
+  uint64_t few;            // the logits' sums, where their product is split
   uint64_t bytes;
 };
 XentPlan xent_plan(int32_t dtype, int64_t M, int64_t V, int64_t K, bool reverse);

@@ -88,6 +88,49 @@ def test_several_pieces_of_the_vocabulary(dtype):
     ref.within(got["dw"], (g.T @ x).cpu(), bound, dtype)
 
 
+# few logits from long rows, whose product is split along them
+FEW = [(1, 2048, 300), (5, 4014, 728), (157, 1100, 19), (1044, 1918, 9), (64, 1024, 4096),
+       (4000, 1030, 64), (65, 2100, 257), (3, 1024, 1)]
+
+
+@pytest.mark.parametrize("dtype", seq_util.TYPES)
+@pytest.mark.parametrize("M,K,V", FEW)
+def test_few_logits(M, K, V, dtype):
+    s = make(M, K, V, dtype, seed=M + K + V, mean=False)
+    one = check(s)
+    two = run(s)
+    assert all(torch.equal(one[k], two[k]) for k in one)
+
+
+def test_few_logits_of_rows_that_take_no_part():
+    s = make(200, 2070, 300, torch.bfloat16, ignored=0.3, mean=False)
+    off = (s["labels"] < 0) | (s["labels"] >= 300)
+    clean = run(s)
+    s["x"][off] = float("nan")
+    s["dloss"][off] = float("inf")
+    got = run(s)
+    assert bool((got["loss"][off] == 0).all()) and bool((got["dx"][off] == 0).all())
+    assert torch.equal(got["dw"], clean["dw"]) and torch.equal(got["dx"], clean["dx"])
+    assert torch.equal(got["loss"][~off], clean["loss"][~off])
+
+
+@pytest.mark.parametrize("V", [3, 700])
+def test_few_logits_that_are_infinite(V):
+    """Rows of 1024: +inf, -inf alone, and -inf beside finite ones."""
+    x, w = torch.zeros(3, 1024, device="cuda"), torch.zeros(V, 1024, device="cuda")
+    w[:, 0] = 3e38
+    x[0, 0], x[1, 0] = 3.0, -3.0
+    w[0, 2], w[1:, 1] = -3e38, 2.0
+    x[2, 2], x[2, 1] = 3.0, 1.0
+    labels = torch.tensor([0, 0, 1], dtype=torch.int32, device="cuda")
+    f = adst.linear_cross_entropy(x, w, labels)
+    want = torch.tensor([float("inf"), float("-inf"),
+                         2.0 + torch.log(torch.tensor(V - 1.0))], device="cuda")
+    assert torch.equal(torch.isinf(f["lse"]), torch.isinf(want))
+    assert bool((f["lse"][:2] == want[:2]).all()) and abs(float(f["lse"][2] - want[2])) < 1e-5
+    assert abs(float(f["loss"][2]) - float(want[2] - 2)) < 1e-5
+
+
 def test_rows_without_a_label_take_no_part_whatever_they_hold():
     s = make(200, 70, 300, torch.bfloat16, ignored=0.3, mean=False)
     off = (s["labels"] < 0) | (s["labels"] >= 300)

@@ -19,17 +19,19 @@ constexpr int64_t kPieceBytes = 128 << 20;
 // tiles. The rates are those of large products measured here (F32 128, F64 55 TFLOP/s, and
 // 1050 of 16-bit types with 256 x 256 tiles); smaller tiles read more of LDS for each
 // product, and a CU with less than two waves a SIMD waits for its loads. (999 x 515 x 10007 F32:
-// the whole step 590 us with 128 x 128 tiles everywhere, 555 with the ones chosen here.)
+// the whole step 590 us with 128 x 128 tiles everywhere, 555 with the ones chosen here. Up to 16
+// rows have tiles of their own: 7 x 2383 over 52952 words F32 forward 120 us, 219 with 64 x 64.)
 XentPlan::Product product_of(int64_t e, int64_t m, int64_t n, int64_t steps, bool split) {
   static const struct {
     int64_t bm, bn, waves;
     double speed;
-  } tiles[] = {{256, 256, 8, 1.0}, {128, 128, 4, 0.85}, {128, 64, 4, 0.7}, {64, 64, 4, 0.5}};
-  if (m <= 64 && !split) return {3, 1};
+  } tiles[] = {{256, 256, 8, 1.0}, {128, 128, 4, 0.85}, {128, 64, 4, 0.7}, {64, 64, 4, 0.5},
+               {16, 128, 2, 0.3}};
+  if (m <= 64 && !split) return {m <= 16 ? 4 : 3, 1};
   const double flops_per_us = (e == 2 ? 1050e6 : e == 4 ? 128e6 : 55e6) / 256;  // of a CU
   XentPlan::Product best{1, 1};
   double least = -1;
-  for (int k = e == 8 ? 1 : 0; k < 4; ++k) {
+  for (int k = e == 8 ? 1 : 0; k < (m <= 16 ? 5 : 4); ++k) {
     const auto& t = tiles[k];
     const int64_t count = parts(m, t.bm) * parts(n, t.bn);
     // (the matrix cores, not LDS, bound the wider types)
@@ -91,7 +93,7 @@ XentPlan xent_plan(int32_t dtype, int64_t M, int64_t V, int64_t K, bool reverse)
   p.piece = up_to(parts(V, p.pieces), p.pieces > 1 ? 256 : step);
   p.pieces = parts(V, p.piece);
   // (few logits are one piece)
-  if (p.logits.splits == 1) p.logits = product_of(e, M, p.piece, parts(K, step), false);
+  if (p.logits.splits == 1) p.logits = product_of(e, p.m_pad, p.piece, parts(K, step), false);
   p.dx = product_of(e, M, K, p.piece / step, true);
   p.dw = product_of(e, p.piece, K, p.m_pad / step, true);
   p.dx_direct = p.pieces == 1 && p.dx.splits == 1;

@@ -488,7 +488,8 @@ hipError_t by_tiles(int tiles, F f) {
     if (tiles == 0) return f(GemmShape<T, 2, 4, 8, 4, 2>());  // 256 x 256
   if (tiles == 1) return f(GemmShape<T, 2, 2, 4, 4, 2>());    // 128 x 128
   if (tiles == 2) return f(GemmShape<T, 2, 2, 4, 2, 2>());    // 128 x 64
-  return f(GemmShape<T, 1, 4, 4, 1, 4>());  // 64 x 64, three steps ahead: bound by loads
+  if (tiles == 3) return f(GemmShape<T, 1, 4, 4, 1, 4>());  // 64 x 64, three steps ahead
+  return f(GemmShape<T, 1, 2, 1, 4, 4>());  // 16 x 128
 }
 
 template <class T>

@@ -136,7 +136,7 @@ struct XentPlan {
   int64_t m_pad;           // rows, padded
   // each product's tiles, and the parts of its long axis that are summed afterwards
   struct Product {
-    int tiles;  // 0: 256 x 256, 1: 128 x 128, 2: 128 x 64, 3: 64 x 64 for few rows
+    int tiles;  // 0: 256 x 256, 1: 128 x 128, 2: 128 x 64; for few rows 3: 64 x 64, 4: 16 x 128
     int64_t splits;
   } logits, dx, dw;
   bool dx_direct;          // dx leaves its product in the element type

@@ -88,6 +88,15 @@ def test_several_pieces_of_the_vocabulary(dtype):
     ref.within(got["dw"], (g.T @ x).cpu(), bound, dtype)
 
 
+@pytest.mark.parametrize("dtype", seq_util.TYPES)
+@pytest.mark.parametrize("M,K,V", [(1, 64, 9000), (7, 131, 12000), (16, 128, 8200), (17, 96, 8200)])
+def test_few_rows_of_many_words(M, K, V, dtype):
+    s = make(M, K, V, dtype, seed=M + K, mean=False)
+    one = check(s)
+    two = run(s)
+    assert all(torch.equal(one[k], two[k]) for k in one)
+
+
 # few logits from long rows, whose product is split along them
 FEW = [(1, 2048, 300), (5, 4014, 728), (157, 1100, 19), (1044, 1918, 9), (64, 1536, 4096),
        (4000, 1030, 64), (65, 2100, 257), (3, 1024, 1)]

@@ -57,7 +57,7 @@ XentPlan::Product product_of(int64_t e, int64_t m, int64_t n, int64_t steps, boo
 // bf16 of 16 18 and 15, of 32 18 and 21).
 XentPlan::Product logits_of(int64_t e, int64_t M, int64_t V, int64_t steps) {
   const int64_t count = parts(M, 64) * parts(V, 64);
-  if (count > 64 || steps < (e == 2 ? 24 : 16)) return product_of(e, M, V, steps, false);
+  if (count < 1 || count > 64 || steps < (e == 2 ? 24 : 16)) return product_of(e, M, V, steps, false);
   const int64_t fill = 256 / count;
   return {3, fill < steps / 4 ? fill : steps / 4};
 }

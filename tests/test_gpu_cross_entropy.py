@@ -270,3 +270,12 @@ def test_gradients_against_differences():
                 L.append(loss())
             flat[i] = keep
             assert abs((L[0] - L[1]) / 2e-6 - float(got["d" + name].view(-1)[i])) < 1e-7, (name, i)
+
+
+@pytest.mark.parametrize("dtype", seq_util.TYPES)
+@pytest.mark.parametrize("K", [1, 8, 255, 256, 512, 1535, 1536, 2048])
+def test_no_rows_at_any_width(K, dtype):
+    """Widths on both sides of where the logits' product is split, which without rows has no tiles."""
+    got = run(make(0, K, 20, dtype))
+    assert got["loss"].shape == got["lse"].shape == (0,) and got["dx"].shape == (0, K)
+    assert got["dw"].shape == (20, K) and bool((got["dw"] == 0).all())

@@ -259,6 +259,8 @@ adst_status adst_causal_conv_vjp(const adst_conv_problem* prob, const void* x, c
   const int e = size_of(p.dtype), we = size_of(p.weight_dtype);
   if (p.batch > 0 && p.steps > 0 && p.channels > 0 && (!x || !w || !dy))
     return fail(ADST_ERR_ARG, "x, dy and w are required");
+  const bool launches = p.channels > 0 && (dx || dw || dbias || dx0);
+  if (launches && !w) return fail(ADST_ERR_ARG, "w is required");  // it is read before any step
   Ranges rs;
   CHECK(conv_inputs(prob, x, w, bias, x0, lens, &rs));
   CHECK(check_aligned("dy", dy, e));
@@ -281,7 +283,7 @@ adst_status adst_causal_conv_vjp(const adst_conv_problem* prob, const void* x, c
   rs.out("dbias", dbias, Wide(p.channels) * we);
   if (need) rs.out("ws", ws, need);
   CHECK(rs.check());
-  if (p.channels == 0 || (!dx && !dw && !dbias && !dx0)) return report_ok();
+  if (!launches) return report_ok();
   ConvArgs a = conv_args(prob, x, w, bias, x0, lens);
   a.dy = dy;
   a.dxT = dxT;

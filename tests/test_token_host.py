@@ -277,3 +277,12 @@ def test_xent_arrays():
     fails(SMALL, adst.adst_linear_cross_entropy_forward, *xent_fwd(n=i.workspace_bytes - 1))
     fails(SMALL, adst.adst_linear_cross_entropy_vjp, *xent_rev(n=i.vjp_workspace_bytes - 1))
     fails(SMALL, adst.adst_linear_cross_entropy_vjp, *xent_rev(ws=None))
+
+
+# ------------------------------------------- arrays that a call without steps reads
+@pytest.mark.parametrize("over", [dict(steps=0), dict(batch=0), dict(steps=0, batch=0)])
+@pytest.mark.parametrize("out", ["dx", "dw", "db", "dx0"])
+def test_conv_vjp_needs_its_weights_without_steps_too(over, out):
+    """The kernel that writes an output loads the taps first, whatever the extents."""
+    none = {k: None for k in ("dx", "dw", "db", "dx0") if k != out}
+    fails(BAD, adst.adst_causal_conv_vjp, *conv_rev(conv(**over), x=None, dy=None, w=None, **none))

@@ -357,7 +357,7 @@ adst_status adst_selective_scan_forward(const adst_scan_problem* prob, const ads
   if (g.map_bytes) rs.out("ws", ws, g.map_bytes);
   CHECK(rs.check());
   if (p.batch == 0 || p.channels == 0 || (!y && !hT && !ck)) return report_ok();
-  if (hT && !in->A) return fail(ADST_ERR_ARG, "A is required");
+  if (!in->A) return fail(ADST_ERR_ARG, "A is required");  // it is read before any step
   ScanArgs a = scan_args(prob, in);
   a.y = y;
   a.hT = hT;

@@ -286,3 +286,11 @@ def test_conv_vjp_needs_its_weights_without_steps_too(over, out):
     """The kernel that writes an output loads the taps first, whatever the extents."""
     none = {k: None for k in ("dx", "dw", "db", "dx0") if k != out}
     fails(BAD, adst.adst_causal_conv_vjp, *conv_rev(conv(**over), x=None, dy=None, w=None, **none))
+
+
+@pytest.mark.parametrize("out", ["y", "hT", "ck"])
+def test_scan_forward_needs_its_rates_without_steps_too(out):
+    """The kernel that writes an output loads A first, whatever the steps."""
+    none = {k: None for k in ("y", "hT", "ck") if k != out}
+    kw = dict(x=None, delta=None, A=None, B=None, C=None, **none)
+    fails(BAD, adst.adst_selective_scan_forward, *scan_fwd(scan(steps=0), **kw))

@@ -98,7 +98,10 @@ adst_status check_scan(const adst_scan_problem* p, ScanGrid* grid) {
     return fail(ADST_ERR_UNSUPPORTED, "at most %lld states", (long long)most);
   CHECK(check_extents(p->batch, p->steps, p->channels));
   if (p->channels % p->groups != 0) return fail(ADST_ERR_ARG, "groups must divide channels");
-  if (Wide(p->batch) * p->channels * (p->steps + 16) * p->states > (Wide(1) << 52))
+  // (without channels nothing else bounds the groups, whose B and C are still read and cleared)
+  if (Wide(p->batch) * p->channels * (p->steps + 16) * p->states > (Wide(1) << 52) ||
+      p->groups >= (int64_t(1) << 26) ||
+      Wide(p->batch) * (p->steps + 16) * p->groups * p->states > (Wide(1) << 52))
     return fail(ADST_ERR_UNSUPPORTED, "more values than the address space");
   *grid = scan_grid(p->dtype, p->batch, p->steps, p->channels, p->states, p->groups);
   if (!grid->fits) return fail(ADST_ERR_UNSUPPORTED, "more rows and channels than a launch holds");

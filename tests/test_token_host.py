@@ -294,3 +294,15 @@ def test_scan_forward_needs_its_rates_without_steps_too(out):
     none = {k: None for k in ("y", "hT", "ck") if k != out}
     kw = dict(x=None, delta=None, A=None, B=None, C=None, **none)
     fails(BAD, adst.adst_selective_scan_forward, *scan_fwd(scan(steps=0), **kw))
+
+
+@pytest.mark.parametrize("over", [
+    dict(groups=1 << 62), dict(groups=1 << 40, batch=1 << 20, steps=1 << 20),
+    dict(groups=1, states=1, batch=1 << 30, steps=1 << 30),
+    dict(groups=(1 << 63) - 1, states=128, batch=(1 << 31) - (1 << 17), steps=1 << 30)])
+def test_scan_extents_without_channels(over):
+    """Their products are refused, not wrapped: no number of channels bounds the groups then."""
+    strides = {"stride_" + k: (0, 0) for k in ("x", "delta", "b", "c", "z", "dy")}
+    p = scan(channels=0, **strides, **over)
+    fails(BIG, adst.adst_selective_scan_plan, p)
+    fails(BIG, adst.adst_selective_scan_vjp, *scan_rev(p))

@@ -175,6 +175,7 @@ adst_status scan_inputs(const adst_scan_problem* p, const adst_scan_inputs* in, 
 adst_status check_xent(const adst_xent_problem* p) {
   if (!p) return fail(ADST_ERR_ARG, "problem is NULL");
   if (!known(p->dtype)) return fail(ADST_ERR_ARG, "unknown dtype %d", p->dtype);
+  if (p->reserved != 0) return fail(ADST_ERR_ARG, "reserved must be 0");
   if (p->rows < 0 || p->width < 1 || p->vocab < 1)
     return fail(ADST_ERR_ARG, "rows must be >= 0, width and vocab >= 1");
   if (p->stride_x < 0 || p->stride_w < 0) return fail(ADST_ERR_ARG, "strides must be >= 0");

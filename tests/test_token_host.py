@@ -306,3 +306,11 @@ def test_scan_extents_without_channels(over):
     p = scan(channels=0, **strides, **over)
     fails(BIG, adst.adst_selective_scan_plan, p)
     fails(BIG, adst.adst_selective_scan_vjp, *scan_rev(p))
+
+
+@pytest.mark.parametrize("reserved", [1, -1, 1 << 30])
+def test_xent_reserved_is_zero(reserved):
+    p = xent(reserved=reserved)
+    fails(BAD, adst.adst_linear_cross_entropy_plan, p)
+    fails(BAD, adst.adst_linear_cross_entropy_forward, *xent_fwd(p))
+    fails(BAD, adst.adst_linear_cross_entropy_vjp, *xent_rev(p))

@@ -88,7 +88,6 @@ template <class T>
 void check(int dtype, int64_t M, int64_t V, int64_t K, int64_t apart, int64_t shift, int tiles,
            int64_t piece, bool uneven, bool at_end) {
   typedef Acc<T> A;
-  const double tol = sizeof(T) == 8 ? 1e-9 : sizeof(T) == 4 ? 3e-5 : 1e-2;
   const int64_t stride = K + apart;
   Guarded xs(((M - 1) * stride + K + shift) * sizeof(T), at_end),
       wsp(((V - 1) * stride + K + shift) * sizeof(T), at_end), labels(M * 4, at_end),
@@ -140,35 +139,79 @@ void check(int dtype, int64_t M, int64_t V, int64_t K, int64_t apart, int64_t sh
     const auto held = place(p, dtype, M, V, K, true, at_end);
     if (vjp_of<T>(a, p, nullptr, nullptr) != hipSuccess) std::exit(3);
   }
-  std::vector<double> want_dx(M * K, 0.0), want_dw(V * K, 0.0), logit(V);
+  // How far a result may be off, with u the type's half step and a the accumulation type's: a
+  // logit of K products, (K + 2) a sum |x w|; lse, that of the largest and (V + 8) a for the sum
+  // and logarithm, a rounding of each size; p = exp(logit - lse), p times its argument's error and
+  // 2 |argument| + 4 roundings; g, the -1, the weight and its scale, 4 a, and u once where it is
+  // held in 16 bits (F16: or 2^-38 of the largest weight, below its normal range); a sum of n
+  // terms, (n + 8) a of their sizes; the result's own rounding, u.
+  const double ua = sizeof(A) == 8 ? 0x1p-53 : 0x1p-24;
+  const double u = sizeof(T) == 8 ? 0x1p-53 : sizeof(T) == 4 ? 0x1p-24
+                   : dtype == ADST_BF16 ? 0x1p-8 : 0x1p-11;
+  const double of_g = sizeof(T) == 2 ? u : 0;
+  double most = 0;
+  for (int64_t m = 0; m < M; ++m) most = std::fmax(most, std::fabs((double)dloss.as<A>()[m]));
+  const double least = dtype == ADST_F16 ? 0x1p-38 * most : 0;
+  struct Sum {
+    double v = 0, size = 0, off = 0;
+    void add(double g, double far, double by) {
+      v += g * by;
+      size += (std::fabs(g) + far) * std::fabs(by);
+      off += far * std::fabs(by);
+    }
+  };
+  std::vector<Sum> want_dx(M * K), want_dw(V * K);
+  std::vector<double> logit(V), size(V);
+  const auto within = [&](const char* name, int64_t i, double got, double want, double bound) {
+    near(name, i, got, want, bound / (1 + std::fabs(want)));
+  };
   for (int64_t m = 0; m < M; ++m) {
-    double top = -INFINITY, sum = 0;
+    double top = -INFINITY, sum = 0, off = 0;
     for (int64_t v = 0; v < V; ++v) {
-      double s = 0;
-      for (int64_t k = 0; k < K; ++k) s += (double)(A)x[m * stride + k] * (double)(A)w[v * stride + k];
+      double s = 0, abs = 0;
+      for (int64_t k = 0; k < K; ++k) {
+        const double term = (double)(A)x[m * stride + k] * (double)(A)w[v * stride + k];
+        s += term;
+        abs += std::fabs(term);
+      }
       logit[v] = s;
       top = std::fmax(top, s);
+      off = std::fmax(off, (K + 2) * ua * abs);
     }
     for (int64_t v = 0; v < V; ++v) sum += std::exp(logit[v] - top);
     const double z = top + std::log(sum);
     const int64_t label = labels.as<int32_t>()[m];
     const bool has = label >= 0 && label < V;
-    // (lse and loss are of the accumulation type)
-    const double fine = sizeof(T) == 8 ? 1e-12 : 2e-5;
-    near("lse", m, (double)lse.as<A>()[m], z, fine);
-    near("loss", m, (double)loss.as<A>()[m], has ? z - logit[label] : 0, fine);
-    if (!has) continue;
-    const double weight = (double)dloss.as<A>()[m];
+    double low = 0;  // the farthest argument of an exponential
+    for (int64_t v = 0; v < V; ++v) low = std::fmax(low, std::fabs(logit[v] - z));
+    const double of_z = off + (V + 8 + 2 * low + 4) * ua + 4 * ua * (std::fabs(z) + std::fabs(top) + 1);
+    within("lse", m, (double)lse.as<A>()[m], z, of_z);
+    const double loss_ = has ? z - logit[label] : 0;
+    within("loss", m, (double)loss.as<A>()[m], loss_,
+           has ? of_z + off + ua * (std::fabs(z) + std::fabs(logit[label])) : 0);
+    const double weight = has ? uneven ? (double)dloss.as<A>()[m] : 1 : 0;
+    if (weight == 0) continue;
     for (int64_t v = 0; v < V; ++v) {
-      const double g = (std::exp(logit[v] - z) - (v == label)) * weight;
+      const double p = std::exp(logit[v] - z), hot = v == label, g = (p - hot) * weight;
+      const double arg = std::fabs(logit[v] - z);
+      double far = (p * (off + of_z + ua * (std::fabs(logit[v]) + std::fabs(z)) + (2 * arg + 4) * ua) +
+                    4 * ua * (p + hot)) * std::fabs(weight);
+      far += of_g * (std::fabs(g) + far) + least;
       for (int64_t k = 0; k < K; ++k) {
-        want_dx[m * K + k] += g * (double)(A)w[v * stride + k];
-        want_dw[v * K + k] += g * (double)(A)x[m * stride + k];
+        want_dx[m * K + k].add(g, far, (double)(A)w[v * stride + k]);
+        want_dw[v * K + k].add(g, far, (double)(A)x[m * stride + k]);
       }
     }
   }
-  for (int64_t i = 0; i < M * K; ++i) near("dx", i, (double)(A)dx.as<T>()[i], want_dx[i], tol);
-  for (int64_t i = 0; i < V * K; ++i) near("dw", i, (double)(A)dw.as<T>()[i], want_dw[i], tol);
+  const auto sums = [&](const char* name, const T* got, const std::vector<Sum>& want, int64_t n) {
+    for (size_t i = 0; i < want.size(); ++i) {
+      const double bound = want[i].off + (n + 8) * ua * want[i].size;
+      within(name, i, (double)(A)got[i], want[i].v, bound + u * (std::fabs(want[i].v) + bound) +
+                                                        (dtype == ADST_F16 ? 0x1p-25 : 0));
+    }
+  };
+  sums("dx", dx.as<T>(), want_dx, V);
+  sums("dw", dw.as<T>(), want_dw, M);
 }
 
 // No rows: through the same call as any other.

@@ -351,6 +351,7 @@ adst_conv_problem conv_problem(const at::Tensor& x, const at::Tensor& w, const a
   adst_conv_problem p{};
   p.dtype = code_of(x);
   p.weight_dtype = code_of(w);
+  need(act == ADST_ACT_NONE || act == ADST_ACT_SILU);
   p.act = (int32_t)act;
   need(w.size(0) >= 1 && w.size(0) <= ADST_CONV_MAX_TAPS);
   p.taps = (int32_t)w.size(0);

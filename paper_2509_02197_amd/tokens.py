@@ -10,9 +10,9 @@ current stream, or on `stream`.
 """
 import ctypes
 
-from . import (ADST_ACT_NONE, ADST_BF16, ADST_CONV_MAX_TAPS, ADST_F16, ADST_F32, _check, _ptr,
-               _stream, adst_conv_problem, adst_scan_gradients, adst_scan_info, adst_scan_inputs,
-               adst_scan_problem, adst_xent_info, adst_xent_problem, lib)
+from . import (ADST_ACT_NONE, ADST_ACT_SILU, ADST_BF16, ADST_CONV_MAX_TAPS, ADST_F16, ADST_F32,
+               _check, _ptr, _stream, adst_conv_problem, adst_scan_gradients, adst_scan_info,
+               adst_scan_inputs, adst_scan_problem, adst_xent_info, adst_xent_problem, lib)
 from .sequence import (_acc, _at, _binding, _bytes, _call, _channels_contiguous, _check_in_place,
                        _code, _codes, _expect, _require)
 
@@ -125,6 +125,12 @@ def _taps(w, D):
     return w.shape[0]
 
 
+def _act(act):
+    if act not in (ADST_ACT_NONE, ADST_ACT_SILU):
+        raise ValueError(f"unknown act {act!r}")
+    return act
+
+
 def _conv_problem(x, w, b, x0, lens, act, dy=None, dxT=None):
     code = _code("x", x)
     sx = _sequence("x", x)
@@ -135,7 +141,7 @@ def _conv_problem(x, w, b, x0, lens, act, dy=None, dxT=None):
     for name, t in (("x0", x0), ("dxT", dxT)):
         _expect(name, t, (B, K - 1, D), x.dtype, x.device)
     _lens(lens, x)
-    return adst_conv_problem(code, wcode, act, K, B, T, D, *sx, *sd)
+    return adst_conv_problem(code, wcode, _act(act), K, B, T, D, *sx, *sd)
 
 
 def causal_conv(x, w, b=None, x0=None, lens=None, act=ADST_ACT_NONE, want_y=True, stream=None):
@@ -221,7 +227,7 @@ def causal_conv_step(x, w, window, b=None, slots=None, act=ADST_ACT_NONE, stream
         raise ValueError(f"window must be [nstates, {K - 1}, {D}], not {tuple(window.shape)}")
     _expect("window", window, window.shape, x.dtype, x.device)
     _expect("slots", slots, (B,), torch.int32, x.device)
-    prob = adst_conv_problem(code, wcode, act, K, B, 1, D, x.stride(0), 0, 0, 0)
+    prob = adst_conv_problem(code, wcode, _act(act), K, B, 1, D, x.stride(0), 0, 0, 0)
 
     def body(handle):
         y = torch.empty_like(x, memory_format=torch.contiguous_format)

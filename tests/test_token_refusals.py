@@ -115,3 +115,12 @@ def test_coefficients_without_the_groups_axis():
 def test_taps(w):
     with pytest.raises((ValueError, TypeError)):
         adst.causal_conv(CONV["x"], w)
+
+
+@pytest.mark.parametrize("act", [2, -1, 1 << 32, (1 << 32) + 1, -(1 << 32), 0.5, None, "silu"])
+@pytest.mark.parametrize("name", ["causal_conv", "causal_conv_vjp", "causal_conv_step"])
+def test_activations(name, act):
+    """None but the two: a number beyond 32 bits is not cut to one of them."""
+    f, args, _ = CALLS[name]
+    with pytest.raises((ValueError, TypeError)):
+        f(**args, act=act)

@@ -825,10 +825,13 @@ adst_status adst_linear_cross_entropy_forward(const adst_xent_problem* prob, con
 /* The vector-Jacobian product, with g_v = (exp(logit_v - lse) - [v = label]) * dloss of
  * a row: dx = sum_v g_v * w[v], dw[v] = sum over rows of g_v * x (each
  * optional). lse: the forward call's. dloss: dL/dloss [rows] in the accumulation
- * type (1 if NULL). The logits are computed again; g is held in 16 bits beside 16-bit
- * inputs, scaled so that the largest |dloss| is a power of two (2^14 in F16,
- * whose least values would be lost otherwise). A row whose dloss is 0, or that has no label, gets a dx of
- * 0 (of a finite w), whatever it holds. Errors: as the forward. */
+ * type (1 if NULL). The logits are computed again. Beside 16-bit inputs g is
+ * held in 16 bits (pass x and w in F32 where that is too few): for dx without
+ * dloss, which a row of dx is multiplied by at its end, and for dw scaled so
+ * that the largest |dloss| is a power of two; both times 2^14 in F16, whose
+ * least values would be lost otherwise. A row whose dloss is 0, or that has no
+ * label, gets a dx of 0 (of a finite w), whatever it holds. Errors: as the
+ * forward. */
 adst_status adst_linear_cross_entropy_vjp(const adst_xent_problem* prob, const void* x,
                                           const void* w, const int32_t* labels, const void* lse,
                                           const void* dloss, void* dx, void* dw, void* ws,

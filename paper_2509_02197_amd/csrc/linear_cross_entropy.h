@@ -12,13 +12,16 @@
 //             written in both orders, rows and columns; then dw of the piece = g^T x and
 //             dx += g w, for which x and the piece of w are transposed once each (a
 //             hundredth of a product's time, against a second kind of product).
-// g is rounded to the element type, which the matrix cores need; each of its elements
-// enters sums of thousands in 32 bits, and its roundings are independent, all but those of
-// the -1 at the labels: there g is close to -dloss, the same in every row of a mean. So beside
-// 16-bit types g is scaled to make the largest |dloss| a power of two, 2^14 for F16,
-// whose range would lose small ones, and the products' results are scaled back. (dw and
-// dx of 4096 x 4096 x 65537 F16 under a mean: 4.0e-4 off without, of which 2.1e-4 are their
-// own rounding.)
+// g is rounded to the element type, which the matrix cores need (a caller who wants 32 bits of it
+// passes x and w in F32); each of its elements enters sums of thousands in 32 bits, and its
+// roundings are independent, all but those of the -1 at the labels: there g is close to -dloss.
+// What leaves -1 exact differs by order. In rows, for dx, g is held without dloss, which a row of
+// dx is multiplied by at its end: -1 and a row's small probabilities do not depend on other rows'
+// weights. In columns, for dw, whose sums go over rows, g has its weight, beside 16-bit types
+// scaled to make the largest |dloss| a power of two, which leaves the -1 exact under a mean. F16's
+// range would lose small probabilities: both orders are held times 2^14. (dw and dx of 4096 x
+// 4096 x 65537 F16 under a mean: 4.0e-4 off without, of which 2.1e-4 are their own rounding. bf16
+// 8192 x 2048 x 32000: the results are as far from 64 bits as with 32 bits of g, 1.7e-3, to 1%.)
 #pragma once
 
 #include "vocab_gemm.h"
@@ -189,6 +192,12 @@ __device__ inline A row_weight(const int32_t* labels, const void* dloss, int64_t
   return dloss ? static_cast<const A*>(dloss)[m] : A(1);
 }
 
+// What g in rows is held times.
+template <class T>
+constexpr float kUnit = 1.0f;
+template <>
+inline constexpr float kUnit<f16> = 0x1p14f;
+
 // scale[0]: what takes the largest finite |dloss| of the rows that take part to `to`;
 // scale[1]: its inverse. One workgroup.
 __global__ __launch_bounds__(1024) void xent_scale(const int32_t* labels, const void* dloss,
@@ -247,8 +256,9 @@ __global__ __launch_bounds__(256) void xent_turn(Rows from, int64_t cols, int64_
   }
 }
 
-// g of a piece of the vocabulary, whose first word is v0: [rows][piece] and, transposed,
-// [piece][m_pad]. Both are whole: zeros beyond the vocabulary and the rows.
+// g of a piece of the vocabulary, whose first word is v0: without weights times kUnit
+// [rows][piece] and, with them and transposed, [piece][m_pad]. Both are whole: zeros beyond the
+// vocabulary and the rows.
 struct GArgs {
   const int32_t* labels;
   const void* lse;
@@ -273,15 +283,18 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad(Rows x, Rows w, Tiles t
   const A scale = q.scale ? (A)q.scale[0] : A(1);
   struct Row {
     A lse, weight;
-    int label, pad;
+    int label;
+    bool in;  // takes part
   };
   Row* const row_of = reinterpret_cast<Row*>(lds);
   for (int row = threadIdx.x; row < S::BM; row += S::kThreads) {
     const int64_t m = m0 + row;
-    Row one = {A(0), A(0), -1, 0};
+    Row one = {A(0), A(0), -1, false};
     if (m < x.n) {
       const int64_t at = q.labels[m] - q.v0 - n0;
-      one.weight = row_weight<A>(q.labels, q.dloss, m, q.V) * scale;
+      const A weight = row_weight<A>(q.labels, q.dloss, m, q.V);
+      one.in = weight != A(0);
+      one.weight = weight * scale;
       one.lse = static_cast<const A*>(q.lse)[m];
       one.label = at >= 0 && at < S::BN ? (int)at : -1;
     }
@@ -297,14 +310,17 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad(Rows x, Rows w, Tiles t
       for (int j = 0; j < S::NT; ++j) {
         const int n = (wn * S::NT + j) * 16 + col;
         A v = A(0);
-        if (row.weight != A(0) && n0 + n < w.n)
-          v = (exp_(s.acc[i][j][r] - row.lse) - (n == row.label ? A(1) : A(0))) * row.weight;
+        if (row.in && n0 + n < w.n)
+          v = exp_(s.acc[i][j][r] - row.lse) - (n == row.label ? A(1) : A(0));
         s.acc[i][j][r] = v;
       }
     }
   // transposed: a lane has four neighbouring rows of a column (every fourth, for F64)
 #pragma unroll
-  for (int i = 0; i < S::MT; ++i)
+  for (int i = 0; i < S::MT; ++i) {
+    A weight[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) weight[r] = row_of[(wm * S::MT + i) * 16 + C::at(lane, r)].weight;
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
       const int64_t n = n0 + (wn * S::NT + j) * 16 + col, m = m0 + (wm * S::MT + i) * 16;
@@ -312,18 +328,34 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad(Rows x, Rows w, Tiles t
       T* const to = static_cast<T*>(q.gt) + n * q.m_pad + m;
       if constexpr (sizeof(T) == 8) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) to[C::at(lane, r)] = down<T>(s.acc[i][j][r]);
+        for (int r = 0; r < 4; ++r) to[C::at(lane, r)] = down<T>(s.acc[i][j][r] * weight[r]);
       } else {
         typedef T Four __attribute__((ext_vector_type(4)));
         Four v;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = down<T>(s.acc[i][j][r]);
+        for (int r = 0; r < 4; ++r) v[r] = down<T>(s.acc[i][j][r] * weight[r]);
         *reinterpret_cast<Four*>(to + C::at(lane, 0)) = v;
       }
     }
+  }
   __syncthreads();
   store_tile<S>(lds, static_cast<T*>(q.g) + m0 * q.piece + n0, q.piece, x.n - m0, q.piece - n0,
-                [&](int i, int r, int j) { return down<T>(s.acc[i][j][r]); });
+                [&](int i, int r, int j) { return down<T>(s.acc[i][j][r] * A(kUnit<T>)); });
+}
+
+// What the rows of a product are multiplied by at its end: for dw what scales it back (1 if
+// NULL), for dx (labels given) the rows' weights and what takes kUnit back.
+struct Back {
+  const float* scale;
+  const int32_t* labels;
+  const void* dloss;
+  int64_t V;
+};
+template <class T>
+__device__ inline Acc<T> back_of(const Back& q, int64_t row) {
+  typedef Acc<T> A;
+  if (q.labels) return row_weight<A>(q.labels, q.dloss, row, q.V) * A(1 / kUnit<T>);
+  return q.scale ? (A)q.scale[1] : A(1);
 }
 
 // C [rows][n] from a product (DIRECT: of whole steps): rounded to `out`, or added to (`add`: after
@@ -331,7 +363,7 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad(Rows x, Rows w, Tiles t
 struct OutArgs {
   void* out;
   void* sums;
-  const float* scale;
+  Back back;
   bool add;
 };
 template <class S, bool DIRECT>
@@ -349,9 +381,17 @@ __global__ __launch_bounds__(S::kThreads) void xent_product(Rows a, Rows b, Tile
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / S::WN, wn = wave % S::WN, col = lane & 15;
   if (q.out) {
-    const A back = q.scale ? (A)q.scale[1] : A(1);
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t m = m0 + (wm * S::MT + i) * 16 + C::at(lane, r);
+        const A back = back_of<T>(q.back, m < a.n ? m : a.n - 1);
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) s.acc[i][j][r] *= back;
+      }
     store_tile<S>(lds, static_cast<T*>(q.out) + m0 * b.n + n0, b.n, a.n - m0, b.n - n0,
-                  [&](int i, int r, int j) { return down<T>(s.acc[i][j][r] * back); });
+                  [&](int i, int r, int j) { return down<T>(s.acc[i][j][r]); });
     return;
   }
   A* const to = static_cast<A*>(q.sums) + (split * a.n + m0) * b.n + n0;
@@ -377,17 +417,17 @@ __global__ __launch_bounds__(S::kThreads) void xent_product(Rows a, Rows b, Tile
   }
 }
 
-// out = the splits' sums added in order, rounded.
+// out [n / width][width] = the splits' sums added in order, rounded.
 template <class T>
-__global__ __launch_bounds__(256) void xent_sum(const void* sums, int64_t n, int64_t splits,
-                                                const float* scale, void* out) {
+__global__ __launch_bounds__(256) void xent_sum(const void* sums, int64_t n, int64_t width,
+                                                int64_t splits, Back back, void* out) {
   typedef Acc<T> A;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   A v = A(0);
 #pragma unroll 4
   for (int64_t k = 0; k < splits; ++k) v += static_cast<const A*>(sums)[k * n + i];
-  static_cast<T*>(out)[i] = down<T>(scale ? v * (A)scale[1] : v);
+  static_cast<T*>(out)[i] = down<T>(v * back_of<T>(back, back.labels ? i / width : 0));
 }
 
 // --------------------------------------------------------------- few logits
@@ -461,17 +501,17 @@ __global__ __launch_bounds__(256) void xent_few_grad(const void* sums, int64_t s
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= q.m_pad * q.piece) return;
   const int64_t m = id / q.piece, n = id % q.piece;
-  A v = A(0);
+  A v = A(0), weight = A(0);
   if (m < M && n < q.V) {
-    const A weight = row_weight<A>(q.labels, q.dloss, m, q.V) * (q.scale ? (A)q.scale[0] : A(1));
+    weight = row_weight<A>(q.labels, q.dloss, m, q.V);
     if (weight != A(0)) {
       const A logit = few_logit(static_cast<const A*>(sums), splits, M * q.V, m * q.V + n);
-      v = (exp_(logit - static_cast<const A*>(q.lse)[m]) - (n == q.labels[m] ? A(1) : A(0))) *
-          weight;
+      v = exp_(logit - static_cast<const A*>(q.lse)[m]) - (n == q.labels[m] ? A(1) : A(0));
     }
   }
-  if (m < M) static_cast<T*>(q.g)[m * q.piece + n] = down<T>(v);
-  static_cast<T*>(q.gt)[n * q.m_pad + m] = down<T>(v);
+  if (m < M) static_cast<T*>(q.g)[m * q.piece + n] = down<T>(v * A(kUnit<T>));
+  const A scale = q.scale ? (A)q.scale[0] : A(1);
+  static_cast<T*>(q.gt)[n * q.m_pad + m] = down<T>(v * (weight * scale));
 }
 
 // ------------------------------------------------------------------ launches
@@ -508,7 +548,7 @@ hipError_t few_logits(const XentArgs& a, const XentPlan& p, const Rows& x, const
     const Tiles t = tiles_of<S>(a.M, a.V, a.K, p.logits.splits);
     return start(direct ? xent_product<S, true> : xent_product<S, false>,
                  dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, x, w, t,
-                 OutArgs{nullptr, sums, nullptr, false});
+                 OutArgs{nullptr, sums, Back{}, false});
   });
 }
 
@@ -547,8 +587,8 @@ hipError_t forward_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_
 template <class T>
 hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st) {
   if (a.M == 0)  // no rows: dw is zero, a sum of nothing
-    return start(xent_sum<T>, dim3((unsigned)parts(a.V * a.K, 256)), 256, st, nullptr, a.V * a.K, 0,
-                 nullptr, a.dw);
+    return start(xent_sum<T>, dim3((unsigned)parts(a.V * a.K, 256)), 256, st, nullptr, a.V * a.K,
+                 a.K, 0, Back{}, a.dw);
   char* const at = static_cast<char*>(ws);
   const Rows x{a.x, a.sx, a.M};
   hipError_t e = hipSuccess;
@@ -556,9 +596,10 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
   if (sizeof(T) == 2) {
     scale = reinterpret_cast<const float*>(at + p.scale);
     e = start(xent_scale, dim3(1), 1024, st, a.labels, a.dloss, a.M, a.V,
-              a.dtype == ADST_F16 ? 0x1p14f : 1.0f, reinterpret_cast<float*>(at + p.scale));
+              kUnit<T>, reinterpret_cast<float*>(at + p.scale));
     if (e != hipSuccess) return e;
   }
+  const Back of_dw{scale, nullptr, nullptr, a.V}, of_dx{nullptr, a.labels, a.dloss, a.V};
   if (a.dw) {
     e = start(xent_turn<T, true>,
               dim3((unsigned)(parts(p.m_pad, kTurn) * parts(a.K, kTurn))), 256, st, x, a.K, p.m_pad,
@@ -594,12 +635,12 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
         typedef decltype(shape) S;
         const Tiles t = tiles_of<S>(words, a.K, p.m_pad, p.dw.splits);
         return start(xent_product<S, true>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, gt,
-                     xt, t, OutArgs{split ? nullptr : out, at + p.dw_sums, scale, false});
+                     xt, t, OutArgs{split ? nullptr : out, at + p.dw_sums, of_dw, false});
       });
       if (e != hipSuccess) return e;
       if (split) {
         e = start(xent_sum<T>, dim3((unsigned)parts(words * a.K, 256)), 256, st, at + p.dw_sums,
-                  words * a.K, p.dw.splits, scale, out);
+                  words * a.K, a.K, p.dw.splits, of_dw, out);
         if (e != hipSuccess) return e;
       }
     }
@@ -613,14 +654,14 @@ hipError_t vjp_of(const XentArgs& a, const XentPlan& p, void* ws, hipStream_t st
         typedef decltype(shape) S;
         const Tiles t = tiles_of<S>(a.M, a.K, p.piece, p.dx.splits);
         return start(xent_product<S, true>, dim3((unsigned)(t.m * t.n * t.splits)), S::kThreads, st, g,
-                     wt, t, OutArgs{p.dx_direct ? a.dx : nullptr, at + p.dx_sums, scale, v0 > 0});
+                     wt, t, OutArgs{p.dx_direct ? a.dx : nullptr, at + p.dx_sums, of_dx, v0 > 0});
       });
       if (e != hipSuccess) return e;
     }
   }
   if (a.dx && !p.dx_direct)
     return start(xent_sum<T>, dim3((unsigned)parts(a.M * a.K, 256)), 256, st, at + p.dx_sums,
-                 a.M * a.K, p.dx.splits, scale, a.dx);
+                 a.M * a.K, a.K, p.dx.splits, of_dx, a.dx);
   return hipSuccess;
 }
 

@@ -279,3 +279,50 @@ def test_no_rows_at_any_width(K, dtype):
     got = run(make(0, K, 20, dtype))
     assert got["loss"].shape == got["lse"].shape == (0,) and got["dx"].shape == (0, K)
     assert got["dw"].shape == (20, K) and bool((got["dw"] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,least", [(torch.bfloat16, 2.0 ** -20), (torch.float16, 2.0 ** -20),
+                                         (torch.float32, 2.0 ** -30)])
+def test_rows_of_unequal_weights(dtype, least):
+    """A row's dx is as exact as it would be alone, however much larger another row's weight is:
+    g of 40000 equal probabilities is off by one rounding to the type, relative to each. Rows
+    of zeros have equal logits, and so p = 1 / V to 4 roundings."""
+    M, K, V = 40, 32, 40000
+    g = torch.Generator().manual_seed(5)
+    x = torch.zeros(M, K, dtype=dtype, device="cuda")
+    w = (torch.rand(V, K, generator=g, dtype=torch.float64) + 0.5).to(dtype).cuda()
+    labels = torch.randint(0, V, (M,), generator=g).to(torch.int32).cuda()
+    dloss = torch.full((M,), least, device="cuda")
+    dloss[7] = 1.0
+    dloss *= 512.0
+    got = adst.linear_cross_entropy_vjp(x, w, labels, adst.linear_cross_entropy(x, w, labels)["lse"],
+                                        dloss)["dx"]
+    wd = w.double()
+    want = (wd.mean(0) - wd[labels.long()]) * dloss.double()[:, None]
+    unit = seq_util.UNIT[dtype] if dtype != torch.float32 else 0.0
+    size = wd.mean(0) + wd[labels.long()]  # sum of |g| w, for a weight of 1
+    bound = (unit + (V + 32) * 2.0 ** -24) * size * dloss.double()[:, None]
+    ref.within(got, want.cpu(), bound.cpu(), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_label_s_entry_is_exact_for_any_weight(dtype):
+    """One word is so likely that the others' probabilities are below the type's roundings of
+    them, and the label is another one: g is then (dloss, -dloss) times 1 to 4 roundings of 32
+    bits, and dx the difference of two words times dloss, whatever the weights."""
+    M, K, V = 30, 64, 70
+    g = torch.Generator().manual_seed(6)
+    w = torch.randn(V, K, generator=g).to(dtype).cuda()
+    w[:, 0] = 0
+    w[5, 0] = 40.0
+    x = torch.zeros(M, K, dtype=dtype, device="cuda")
+    x[:, 0] = 1.0
+    labels = torch.randint(6, V, (M,), generator=g).to(torch.int32).cuda()
+    dloss = (torch.rand(M, generator=g) + 0.1).cuda()
+    lse = adst.linear_cross_entropy(x, w, labels)["lse"]
+    got = adst.linear_cross_entropy_vjp(x, w, labels, lse, dloss, want_dw=False)["dx"]
+    wd, d = w.double(), dloss.double()[:, None]
+    want = (wd[5] - wd[labels.long()]) * d
+    # the others: exp(-40) each; the exponential's argument of 40 is rounded twice
+    bound = ((V + 100) * 2.0 ** -24 + V * 2.0 ** -57) * (wd.abs().max() * 2 * d).expand(M, K)
+    ref.within(got, want.cpu(), bound.cpu(), dtype)

@@ -322,23 +322,24 @@ __global__ __launch_bounds__(kThreads) void conv_rev(ConvArgs a, Layout l, void*
     if (row == 0 && works)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        A v = A(0);
+        double v = 0;
         for (int r = 0; r < rows; ++r) v += part[r * l.columns + column][i];
-        out[k * a.D + d0 + i] = v;
+        out[k * a.D + d0 + i] = (A)v;
       }
   }
 }
 
 // dw and dbias from the workers' sums: 64 columns, four rows of threads that
-// take every fourth worker.
+// take every fourth worker. In 64 bits: threads' sums are of a few segments, what is added up here
+// and over a workgroup's rows may be a thousand times as long (5 x 2049 x 771 F32: dw and db
+// 1.4e-7 off in 32 bits, 1.1e-7 so; 4.2 us both).
 template <class T>
 __global__ __launch_bounds__(kThreads) void conv_sum(const Acc<T>* sums, int64_t workers, int64_t D,
                                                      int taps, void* dw, void* dbias, bool same) {
-  typedef Acc<T> A;
-  __shared__ A part[4][64];
+  __shared__ double part[4][64];
   const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x % 64, all = (taps + 1) * D;
   const int row = threadIdx.x / 64;
-  A v = A(0);
+  double v = 0;
   if (i < all) {
 #pragma unroll 8
     for (int64_t k = row; k < workers; k += 4) v += sums[k * all + i];
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(kThreads) void conv_sum(const Acc<T>* sums, int64_t
   void* const to = i < taps * D ? dw : dbias;
   const int64_t at = i < taps * D ? i : i - taps * D;
   if (!to) return;
-  if (same) static_cast<T*>(to)[at] = down<T>(v);
+  if (same) static_cast<T*>(to)[at] = (T)v;
   else static_cast<float*>(to)[at] = (float)v;
 }
 

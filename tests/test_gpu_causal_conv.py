@@ -187,3 +187,16 @@ def test_gradients_against_differences():
                 L.append(loss())
             flat[i] = keep
             assert abs((L[0] - L[1]) / 2e-6 - float(got[grad].view(-1)[i])) < 1e-6, (name, i)
+
+
+def test_workgroups_sums_are_joined_in_64_bits():
+    """A long row's dw and db: one value of 2^26 at its start, one of -2^26 at its end and 62 ones
+    in between, 8192 steps apart, where workgroups of their own sum them up exactly. 32 bits lose
+    the ones beside 2^26."""
+    far, n = 8192, 64
+    x = torch.ones(1, far * n, 1, device="cuda")
+    dy = torch.zeros_like(x)
+    dy[0, ::far, 0] = 1.0
+    dy[0, 0, 0], dy[0, -far, 0] = 2.0 ** 26, -2.0 ** 26
+    got = adst.causal_conv_vjp(x, dy, torch.ones(1, 1, device="cuda"))
+    assert float(got["db"]) == n - 2 and float(got["dw"]) == n - 2

@@ -971,9 +971,9 @@ __global__ __launch_bounds__(64 * W) void scan_rev(ScanArgs a, ScanGrid g, void*
   __syncthreads();
   if (threadIdx.x < 2 * kSlab && (int)threadIdx.x % kSlab < p.channels) {
     const int which = threadIdx.x / kSlab, c = threadIdx.x % kSlab;
-    A v = A(0);
+    double v = 0;
     for (int r = 0; r < R; ++r) v += rows_of[r][which][c];
-    sums.d[(part * 2 + which) * a.D_ + p.d0 + c] = v;
+    sums.d[(part * 2 + which) * a.D_ + p.d0 + c] = (A)v;
   }
 }
 
@@ -1010,7 +1010,8 @@ __global__ __launch_bounds__(kSumThreads) void scan_sum_bc(ScanArgs a, ScanGrid 
       down<T>(v);
 }
 
-// dA, dD and dbias: over the rows of workgroups and the segments.
+// dA, dD and dbias: over the rows of workgroups and the segments, in 64 bits: a part is a sum over
+// steps already, and what is 2^-24 of another one is not to be lost beside it.
 template <class T>
 __global__ __launch_bounds__(kSumThreads) void scan_sum_a(ScanArgs a, ScanGrid g, void* ws) {
   typedef Acc<T> A;
@@ -1020,9 +1021,10 @@ __global__ __launch_bounds__(kSumThreads) void scan_sum_a(ScanArgs a, ScanGrid g
   const int64_t n = id / a.D_, d = id % a.D_;
   const A* from = n < a.N ? sums.a + n * a.D_ + d : sums.d + (n - a.N) * a.D_ + d;
   const int64_t by = (n < a.N ? a.N : 2) * a.D_;
-  A v = A(0);
+  double sum = 0;
 #pragma unroll 8
-  for (int64_t k = 0; k < parts; ++k) v += from[k * by];
+  for (int64_t k = 0; k < parts; ++k) sum += from[k * by];
+  const A v = (A)sum;
   if (n < a.N) static_cast<A*>(a.out.dA)[d * a.N + n] = v;
   else if (n == a.N && a.out.dD) static_cast<A*>(a.out.dD)[d] = v;
   else if (n > a.N && a.out.ddelta_bias) static_cast<A*>(a.out.ddelta_bias)[d] = v;

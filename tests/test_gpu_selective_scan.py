@@ -260,3 +260,17 @@ def test_gradients_against_differences():
                 L.append(loss())
             flat[i] = keep
             assert abs((L[0] - L[1]) / 2e-6 - float(got["d" + name].reshape(-1)[i])) < 1e-6, (name, i)
+
+
+def test_rows_sums_are_joined_in_64_bits():
+    """dA, dD and the bias' gradient are each the sum of dy over 64 rows of one step (A is 0, all
+    else is 1): 2^26, 62 ones and -2^26, of which 32 bits lose the ones."""
+    n = 64
+    one = torch.ones(n, 1, 1, device="cuda")
+    dy = one.clone()
+    dy[0], dy[-1] = 2.0 ** 26, -2.0 ** 26
+    got = adst.selective_scan_vjp(one, torch.zeros_like(one), torch.zeros(1, 1, device="cuda"), one,
+                                  one, dy, D=torch.ones(1, device="cuda"),
+                                  delta_bias=torch.ones(1, device="cuda"), h0=one)
+    for k in ("dA", "dD", "ddelta_bias"):
+        assert float(got[k]) == n - 2, k

@@ -105,7 +105,7 @@ class TokenLayer:
         labels = want.reshape(-1)
         h, (e, n, x, z, c, delta, Bm, Cm, A, s) = self.forward(given, lens, keep=True)
         f = adst.linear_cross_entropy(h, p["W_head"], labels)
-        scale = (labels >= 0) / (labels >= 0).sum()
+        scale = (labels >= 0) / (labels >= 0).sum().clamp(min=1)
         scale = scale.to(f["loss"].dtype)
 
         g = {}

@@ -246,3 +246,13 @@ def test_refusals():
         adst.selective_scan(x, s["delta"], torch.zeros(4, 129, device="cuda"),
                             torch.zeros(3, 6, 129, dtype=x.dtype, device="cuda"),
                             torch.zeros(3, 6, 129, dtype=x.dtype, device="cuda"))
+
+
+def test_a_batch_without_tokens():
+    """Rows of no tokens alone: the mean over none is 0, and so are the gradients."""
+    tokens = ex.probe_tokens(1, 12, 3, 11)
+    layer = ex.TokenLayer(11, 24)
+    none = torch.zeros(3, dtype=torch.int32, device="cuda")
+    loss, grads = layer.loss_and_gradients(tokens, none)
+    assert float(loss) == 0
+    assert all(bool((g == 0).all()) for g in grads.values())

@@ -314,3 +314,13 @@ def test_xent_reserved_is_zero(reserved):
     fails(BAD, adst.adst_linear_cross_entropy_plan, p)
     fails(BAD, adst.adst_linear_cross_entropy_forward, *xent_fwd(p))
     fails(BAD, adst.adst_linear_cross_entropy_vjp, *xent_rev(p))
+
+
+@pytest.mark.parametrize("dtype,size", [(adst.ADST_F32, 4), (adst.ADST_BF16, 2), (adst.ADST_F16, 2)])
+def test_xent_plan_of_several_pieces(dtype, size):
+    """At the sizes of the GPU's test of several pieces: g of the whole vocabulary in two orders, or
+    in one, would not fit the workspace."""
+    M, K, V = (128 << 20) // size // 1024, 32, 2100
+    i = adst.adst_linear_cross_entropy_plan(xent(dtype=dtype, rows=M, vocab=V, width=K, stride_x=K,
+                                                 stride_w=K))
+    assert i.vjp_workspace_bytes < M * V * size

@@ -811,7 +811,7 @@ typedef struct {
 
 /* Host only. Errors: ADST_ERR_ARG (NULL, unknown dtype, reserved not 0, a bad
  * extent or stride), ADST_ERR_UNSUPPORTED (rows or vocab times width + 64 >=
- * 2^31, or rows * vocab >= 2^35). */
+ * 2^31, or (rows + 256) * (vocab + 256) >= 2^35). */
 adst_status adst_linear_cross_entropy_plan(const adst_xent_problem* prob, adst_xent_info* out);
 
 /* loss and lse [rows] in the accumulation type (each optional). Errors: as the

@@ -30,8 +30,11 @@ struct Count {
   static constexpr int value = K;
 };
 
-// Channels of a thread: as many as leave registers for three waves a SIMD (8 x 4096 x 2048
-// bf16 forward 64 us with 4 channels of 2 bytes, 67 with 8).
+// Channels of a thread. The forward has registers for three waves a SIMD or more with these (8 x
+// 4096 x 2048 bf16 64 us with 4 channels, 67 with 8). The reverse has three up to 4 taps of 16
+// bits, and two from 5 on (bf16 of 8 taps with SiLU one); F32 two at 3 and 4 taps, and above them
+// three, with half the channels (8 x 4096 x 2048 with SiLU: 8 taps 246 us, 295 with 4 channels; 5
+// taps 225 and 200); F64 two from 3 taps on and one from 6.
 template <class T, int K>
 constexpr int lanes_of(bool reverse) {
   return sizeof(T) == 8 || (sizeof(T) == 4 && reverse && K > 4) ? 2 : 4;

@@ -10,8 +10,9 @@ namespace {
 int64_t parts(int64_t n, int64_t by) { return (n + by - 1) / by; }
 int64_t up_to(int64_t n, int64_t by) { return parts(n, by) * by; }
 
-// g of a piece of the vocabulary, one of its two orders, at most: both then stay in the
-// 256 MB cache between the products.
+// g of a piece of the vocabulary, one of its two orders, where a piece has more than 1024 words:
+// both then stay in the 256 MB cache between the products. With more rows than 65536 (16-bit types;
+// 32768 of F32) a piece has 1024 words, whatever they take: 2 GB an order at 2^20 rows of bf16.
 constexpr int64_t kPieceBytes = 128 << 20;
 
 // The tiles of an m x n product, and the parts of its long axis (of `steps` steps) where it

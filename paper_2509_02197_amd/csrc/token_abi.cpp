@@ -186,7 +186,8 @@ adst_status check_xent(const adst_xent_problem* p) {
       Wide(p->rows) * (p->width + 64) >= most || Wide(p->vocab) * (p->width + 64) >= most ||
       Wide(p->rows + 256) * (p->vocab + 256) >= Wide(1) << 35)
     return fail(ADST_ERR_UNSUPPORTED,
-                "rows and vocab times width + 64 must be below 2^31, rows * vocab below 2^35");
+                "rows and vocab times width + 64 must be below 2^31, (rows + 256) * (vocab + 256) "
+                "below 2^35");
   return ADST_OK;
 }
 

@@ -453,7 +453,8 @@ def linear_cross_entropy_vjp(x, w, labels, lse, dloss=None, want_dx=True, want_d
     """The VJP of linear_cross_entropy: lse as it gave it, dloss = dL/dloss [rows] like lse (ones
     if None). Returns a dict: dx and dw like x and w (contiguous), each None unless wanted. A row
     without a label, or whose dloss is 0, adds nothing to dw, whatever it holds. The logits are
-    computed again, for a piece of the vocabulary at a time."""
+    computed again, for a piece of the vocabulary at a time; beside 16-bit types their gradients
+    are rounded to the type (give x and w in float32 for 32 bits of them)."""
     if stream is None:
         done = _binding().linear_cross_entropy_vjp(x, w, labels, lse, dloss, want_dx, want_dw)
         if done is not None:

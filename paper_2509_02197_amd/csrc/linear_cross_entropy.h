@@ -10,8 +10,8 @@
 //             softmax across tiles: a second kernel joins the tiles in order)
 //   reverse   for a piece of the vocabulary at a time, the logits again and from them g,
 //             written in both orders, rows and columns; then dw of the piece = g^T x and
-//             dx += g w, for which x and the piece of w are transposed once each (a
-//             hundredth of a product's time, against a second kind of product).
+//             dx += g w, for which x and the piece of w are transposed once each (with many
+//             rows a hundredth of a product's time, against a second kind of product).
 // g is rounded to the element type, which the matrix cores need (a caller who wants 32 bits of it
 // passes x and w in F32); each of its elements enters sums of thousands in 32 bits, and its
 // roundings are independent, all but those of the -1 at the labels: there g is close to -dloss.
